@@ -57,6 +57,11 @@ extern "C" {
 #define DSVT_FP32 0
 #define DSVT_BF16_FP32ACC 1
 
+/* Storage types of the training operators' rows (dsvt_segment_attention, dsvt_layer_norm and their backward passes). */
+#define DSVT_TYPE_F32 0
+#define DSVT_TYPE_BF16 1
+#define DSVT_TYPE_F16 2
+
 /* Bits of the device status word returned through dsvt_status_sync's `bits`. */
 #define DSVT_STATUS_BAD_COORD 1      /* coordinate or batch index outside the grid (clamped) */
 #define DSVT_STATUS_TABLE_OVERFLOW 2 /* more sets / outputs than the caller's capacity (excess dropped) */
@@ -380,6 +385,91 @@ int dsvt_pool_counted(dsvt_ctx* ctx, const int32_t* coords, const float* feats, 
  */
 int dsvt_bev_scatter(dsvt_ctx* ctx, const int32_t* coords, const float* feats, int32_t n, int32_t C, int32_t batch,
                      const int32_t grid[3], int32_t channels_last, float* out);
+
+/*
+ * Multi-head attention inside segments of the voxels, between projections of the caller's own (Eq. 5's attention as a step of a
+ * training program; the dsvt_layer calls fuse it with their projections and have no backward pass).  Segment s holds the
+ * voxels order[seg_start[s]], ..., order[seg_start[s + 1] - 1].  What dsvt_partition writes fits: perm with set_rowoff (its first
+ * *num_sets + 1 entries) are the sets, perm with win_start the whole windows.  For voxels i, j of a segment and head h
+ *
+ *   z = scale * (q[i] . k[j]),  t = cap * tanh(z / cap) if cap > 0, else z
+ *   s = t + bias[h][bx[dx + L - 1] + by[dy + W - 1] + bz[dz + H - 1]],  (dx, dy, dz) = coords[i] - coords[j], each clipped to
+ *       -(L - 1) ... L - 1 (W, H), (L, W, H) = extent
+ *   out[i] = sum over j of softmax_j(s) v[j]
+ *
+ * A bias entry of -inf masks its pairs, in a row with others one of the lowest float does too; a row whose scores are all
+ * -inf gives zeros (and gets and passes on no gradient), one whose scores are all the lowest float equal weights.  (Finite
+ * entries below -FLT_MAX / log2(e) count as the lowest float.)  A voxel with features that are not finite spoils the rows of its
+ * own segment and no others, in masked pairs too.
+ *
+ *   q, k, v     rows of `type`, row i at q + i * ld_q (elements), channel c of head h at h * head_dim + c; 16-byte aligned, as are
+ *               their row strides.  One projection's output [n][3C] gives q, k = q + C, v = q + 2C, ld = 3C.
+ *   order       int32 [n], or NULL for 0, 1, 2, ...;  no voxel twice.
+ *   seg_start   int32 [cap_segments + 1], ascending, in [0, n]; empty segments are fine.
+ *   num_segments device int32 (at most cap_segments count), or NULL for cap_segments.
+ *   max_len     host upper bound of the segments' lengths (1 ... n; larger values count as n).  A longer segment is left out and
+ *               raises DSVT_STATUS_TABLE_OVERFLOW.  Sets: set_size.  It chooses the kernels: up to 128 voxels stay in shared memory.
+ *   bias        float [heads][buckets], or NULL (then buckets, coords, extent and bucket_of are not looked at).
+ *   coords      int32 [n][4] = (b, x, y, z), magnitudes below 2^30; 16-byte aligned.
+ *   bucket_of   HOST int32 [(2L-1) + (2W-1) + (2H-1)]: bx, by, bz one after the other, every sum of three in [0, buckets).
+ *               T5's buckets (exact for small displacements, then by logarithm) are such tables; so is one bucket per displacement.
+ *   out         rows of `type`, stride ld_out, 16-byte aligned; may not alias the inputs.  Rows of voxels in no segment are
+ *               left as they were.
+ *
+ * Scores, softmax and sums are fp32.  With 16-bit types the weights P (and in the backward pass P and dS) are rounded to the type
+ * for the products with v (do, q, k).  With DSVT_TYPE_F32 operands go through the tensor cores as two tf32 parts (22 bits).
+ *
+ * Needs head_dim % 8 == 0, head_dim <= 128, buckets <= 1024, extents <= 128, heads <= 65535 (else DSVT_ERR_UNSUPPORTED); n <=
+ * max_voxels (else DSVT_ERR_CAPACITY; the number of channels is not limited).  An order entry outside [0, n) is skipped, a
+ * seg_start entry outside [0, n] or below its predecessor drops its segment, both with DSVT_STATUS_BAD_INDEX.
+ */
+typedef struct dsvt_segment_attention_params {
+  int32_t n, heads, head_dim, type;
+  const void *q, *k, *v;
+  int64_t ld_q, ld_k, ld_v;
+  const int32_t* order;
+  const int32_t* seg_start;
+  const int32_t* num_segments;
+  int32_t cap_segments, max_len;
+  float scale, cap;
+  const float* bias;
+  const int32_t* coords;
+  const int32_t* bucket_of;
+  int32_t buckets;
+  int32_t extent[3];
+} dsvt_segment_attention_params;
+int dsvt_segment_attention(dsvt_ctx* ctx, const dsvt_segment_attention_params* params, void* out, int64_t ld_out);
+
+/*
+ * The gradients of dsvt_segment_attention's inputs from that of its output, d_out (rows of `type`, stride ld_dout): dq, dk, dv
+ * (rows of `type`, strides ld_dq, ld_dk, ld_dv, 16-byte aligned, may not alias the inputs or each other) and dbias (float
+ * [heads][buckets]; NULL to leave it out, and without a bias).  The forward pass saves nothing for it.  Rows of voxels in no segment
+ * are left as they were; dbias is written in full.
+ */
+int dsvt_segment_attention_backward(dsvt_ctx* ctx, const dsvt_segment_attention_params* params, const void* d_out,
+                                    int64_t ld_dout, void* dq, int64_t ld_dq, void* dk, int64_t ld_dk, void* dv, int64_t ld_dv,
+                                    float* dbias);
+
+/*
+ * LayerNorm of a residual sum over the C channels with biased variance (Appendix B.1.1's Add & Norm as a step of a training
+ * program): u = x + residual, y = (u - mean) / sqrt(var + eps) * g + b.
+ *
+ *   x, residual, y   rows of `type` [n][C], 16-byte aligned; residual may be NULL; y may be x or residual.
+ *   g, b             float [C], NULL for ones and zeros.
+ *
+ * Sums and statistics are fp32.  A row that is not finite stays in its row.  Needs C <= 8192 (else DSVT_ERR_UNSUPPORTED); n and C are
+ * not limited by the context.
+ */
+int dsvt_layer_norm(dsvt_ctx* ctx, int type, const void* x, const void* residual, int32_t n, int32_t C, const float* g,
+                    const float* b, float eps, void* y);
+
+/*
+ * The gradients of dsvt_layer_norm from that of its output, dy: dx ([n][C] of `type`; the residual's is the same; may be x, residual
+ * or dy), dg and db (float [C], written in full; each may be NULL).  Statistics are taken from x and residual again; the forward
+ * pass saves nothing.  The same inputs give the same bits.
+ */
+int dsvt_layer_norm_backward(dsvt_ctx* ctx, int type, const void* x, const void* residual, const void* dy, int32_t n,
+                             int32_t C, const float* g, float eps, void* dx, float* dg, float* db);
 
 /*
  * A measurement aid (the paper has no counterpart): launches a kernel of `blocks` x `threads` threads that

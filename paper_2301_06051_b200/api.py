@@ -24,7 +24,8 @@ STATUS_BAD_COORD, STATUS_TABLE_OVERFLOW, STATUS_BAD_INDEX, STATUS_DUPLICATE_CELL
 EXPORTS = [
     "dsvt_create", "dsvt_destroy", "dsvt_status_sync", "dsvt_last_cuda_error", "dsvt_error_string",
     "dsvt_launch_count", "dsvt_set_layer_ctas", "dsvt_partition", "dsvt_partition_rotated", "dsvt_partition_shifted", "dsvt_partition_counted", "dsvt_pool_counted", "dsvt_partition_noalloc", "dsvt_set_attention", "dsvt_set_attention_rpb", "dsvt_layer", "dsvt_layers", "dsvt_block", "dsvt_pool",
-    "dsvt_bev_scatter", "dsvt_fma_probe",
+    "dsvt_bev_scatter", "dsvt_fma_probe", "dsvt_segment_attention", "dsvt_segment_attention_backward", "dsvt_layer_norm",
+    "dsvt_layer_norm_backward",
 ]
 
 _lib = None
@@ -57,6 +58,20 @@ class TableRef(C.Structure):
 
 
 MAX_CHAIN_LAYERS = 16
+
+
+class SegmentAttentionParams(C.Structure):
+    """Mirror of dsvt_segment_attention_params."""
+    _fields_ = [("n", C.c_int32), ("heads", C.c_int32), ("head_dim", C.c_int32), ("type", C.c_int32),
+                ("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p),
+                ("ld_q", C.c_int64), ("ld_k", C.c_int64), ("ld_v", C.c_int64),
+                ("order", C.c_void_p), ("seg_start", C.c_void_p), ("num_segments", C.c_void_p),
+                ("cap_segments", C.c_int32), ("max_len", C.c_int32), ("scale", C.c_float), ("cap", C.c_float),
+                ("bias", C.c_void_p), ("coords", C.c_void_p), ("bucket_of", C.c_void_p),
+                ("buckets", C.c_int32), ("extent", C.c_int32 * 3)]
+
+
+TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 
 def load():
@@ -95,6 +110,11 @@ def load():
     lib.dsvt_block.argtypes = [vp, vp, i32, vp, i32, vp, vp, vp, i32, vp, vp, C.POINTER(LayerParams), vp]
     lib.dsvt_pool.argtypes = [vp, vp, vp, i32, i32, i32, p3, p3, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, i32,
                               C.c_int, vp, vp, i32, vp, vp, vp]
+    pp = C.POINTER(SegmentAttentionParams)
+    lib.dsvt_segment_attention.argtypes = [vp, pp, vp, i64]
+    lib.dsvt_segment_attention_backward.argtypes = [vp, pp, vp, i64, vp, i64, vp, i64, vp, i64, vp]
+    lib.dsvt_layer_norm.argtypes = [vp, C.c_int, vp, vp, i32, i32, vp, vp, C.c_float, vp]
+    lib.dsvt_layer_norm_backward.argtypes = [vp, C.c_int, vp, vp, vp, i32, i32, vp, C.c_float, vp, vp, vp]
     for name in EXPORTS:
         if name not in ("dsvt_error_string", "dsvt_launch_count"):
             getattr(lib, name).restype = C.c_int
@@ -107,6 +127,43 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
         return None
     assert t.is_cuda and t.is_contiguous(), "device-resident contiguous tensors only"
     return t.data_ptr()
+
+
+def _type(t: torch.Tensor) -> int:
+    if t.dtype not in TYPES:
+        raise ValueError("rows are float32, bfloat16 or float16")
+    return TYPES[t.dtype]
+
+
+def _rows(t: torch.Tensor, like: torch.Tensor):
+    """Pointer and row stride of rows [n, heads, head_dim] whose heads lie one after the other."""
+    n, heads, dim = t.shape
+    if t.shape != like.shape or t.dtype != like.dtype or not t.is_cuda:
+        raise ValueError("rows of one shape and type, on the device")
+    s = t.stride()
+    if (dim > 1 and s[2] != 1) or (heads > 1 and s[1] != dim):
+        raise ValueError("the heads of a row lie one after the other")
+    return t.data_ptr(), s[0] if n > 1 else heads * dim
+
+
+def _int32(t: Optional[torch.Tensor], shape=None):
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or (shape is not None and tuple(t.shape) != shape):
+        raise ValueError("an int32 tensor%s" % (" of shape %s" % (shape,) if shape else ""))
+    return _ptr(t)
+
+
+def _float(t: Optional[torch.Tensor], size: int):
+    if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != (size,)):
+        raise ValueError("a float32 tensor of %d entries" % size)
+    return _ptr(t)
+
+
+def _same(t: Optional[torch.Tensor], like: torch.Tensor):
+    if t is not None and (t.shape != like.shape or t.dtype != like.dtype):
+        raise ValueError("rows of one shape and type")
+    return _ptr(t)
 
 
 def _i3(v: Sequence[int]):
@@ -165,6 +222,68 @@ class SetTable:
     win_start: Optional[torch.Tensor] = None
     win_count: Optional[torch.Tensor] = None
     win_setoff: Optional[torch.Tensor] = None
+
+
+@dataclass
+class Segments:
+    """Runs of voxels that attend among themselves (dsvt_segment_attention): voxels order[start[s]:start[s + 1]], or without an order
+    the rows start[s]:start[s + 1] themselves.  `num` (device int32) counts the segments where that lives on the device; coords is
+    needed with a bias."""
+    start: torch.Tensor  # int32 [segments + 1]
+    max_len: int
+    order: Optional[torch.Tensor] = None  # int32 [n]
+    coords: Optional[torch.Tensor] = None  # int32 [n, 4]
+    num: Optional[torch.Tensor] = None
+
+    @staticmethod
+    def of_sets(table: SetTable, coords: Optional[torch.Tensor] = None) -> "Segments":
+        """The sets of a partition made with its sorted order (SetTable.perm)."""
+        if table.perm is None:
+            raise ValueError("segments of sets need the partition's sorted order (perm)")
+        return Segments(table.set_rowoff[:table.cap_sets + 1], table.set_size, table.perm, coords, table.num_sets)
+
+    @staticmethod
+    def of_windows(table: SetTable, max_len: int, coords: Optional[torch.Tensor] = None) -> "Segments":
+        """The whole windows of a partition made with its sorted order and window arrays; max_len: at most so many voxels each."""
+        if table.perm is None or table.win_start is None:
+            raise ValueError("segments of windows need the partition's sorted order and window starts (perm, win_start)")
+        return Segments(table.win_start, max_len, table.perm, coords)
+
+
+class BucketBias:
+    """A learned bias by buckets of relative position: table float [heads, buckets] on the device; index int32 on the host, the
+    additive indexes of the displacements along x, y and z one after the other (see dsvt_segment_attention_params.bucket_of)."""
+
+    def __init__(self, table: torch.Tensor, extent: Sequence[int], index):
+        import numpy as np
+
+        self.table = table
+        self.extent = tuple(int(e) for e in extent)
+        self.index = np.ascontiguousarray(index, dtype=np.int32)
+        if len(self.extent) != 3 or self.index.shape != (sum(2 * e - 1 for e in self.extent),):
+            raise ValueError("index has 2 e - 1 entries for each extent e")
+        if table.dim() != 2 or table.dtype != torch.float32:
+            raise ValueError("a bias table is float32 [heads, buckets]")
+
+
+def log_buckets(extent: Sequence[int], near: Sequence[int], sides: Sequence[int]):
+    """Index tables of logarithmic buckets (see BucketBias): along each axis displacements below `near` have buckets of their own,
+    farther ones share `sides` - `near` more for each sign by the logarithm of their distance.  Returns (index, number of buckets);
+    the bucket of a displacement is that of its three axes together."""
+    import math
+
+    import numpy as np
+
+    parts, total = [], 1
+    for e, lo, side in reversed(list(zip(extent, near, sides))):
+        if not 1 <= lo <= side or e < 1:
+            raise ValueError("an axis needs an extent of at least 1 and 1 <= near <= sides")
+        a = np.arange(e)
+        far = lo + np.floor(np.log(np.maximum(a, lo) / lo) / math.log(max(e, lo + 1) / lo) * (side - lo) + 1e-9).astype(np.int64)
+        m = np.minimum(np.where(a < lo, a, far), side - 1)
+        parts.append(total * np.concatenate([side - 1 - m[:0:-1], side - 1 + m]))
+        total *= 2 * side - 1
+    return np.concatenate(parts[::-1]).astype(np.int32), total
 
 
 NOALLOC_MAX_VOXELS = 65536
@@ -365,6 +484,84 @@ class Context:
         rc = self.lib.dsvt_fma_probe(self._h, int(blocks), int(threads), int(iters), _ptr(sink), C.byref(flops))
         self._check(rc, "dsvt_fma_probe")
         return int(flops.value)
+
+    # ---- dsvt_segment_attention ----
+    def _segment_params(self, q, k, v, seg, bias, scale, cap):
+        n, heads, dim = q.shape
+        p = SegmentAttentionParams()
+        p.n, p.heads, p.head_dim, p.type = n, heads, dim, _type(q)
+        p.q, p.ld_q = _rows(q, q)
+        p.k, p.ld_k = _rows(k, q)
+        p.v, p.ld_v = _rows(v, q)
+        p.order, p.seg_start, p.num_segments = _int32(seg.order, (n,)), _int32(seg.start), _int32(seg.num)
+        p.cap_segments, p.max_len = seg.start.numel() - 1, seg.max_len
+        p.scale, p.cap = dim ** -0.5 if scale is None else scale, cap
+        if bias is not None:
+            if bias.table.shape[0] != heads:
+                raise ValueError("a bias for %d heads, and %d heads" % (bias.table.shape[0], heads))
+            if seg.coords is None:
+                raise ValueError("a relative position bias needs the segments' coords")
+            p.bias, p.buckets = _ptr(bias.table), bias.table.shape[1]
+            p.coords, p.bucket_of, p.extent = _int32(seg.coords, (n, 4)), bias.index.ctypes.data, bias.extent
+        return p
+
+    def segment_attention(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, seg: Segments,
+                          bias: Optional[BucketBias] = None, scale: Optional[float] = None, cap: float = 0.0,
+                          out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Attention of [n, heads, head_dim] rows inside the segments; scale None: 1 / sqrt(head_dim).  q, k and v may be slices of
+        one projection's output.  Without `out` the rows of voxels in no segment are not defined."""
+        p = self._segment_params(q, k, v, seg, bias, scale, cap)
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        rc = self.lib.dsvt_segment_attention(self._h, C.byref(p), *_rows(out, q))
+        self._check(rc, "dsvt_segment_attention")
+        return out
+
+    def segment_attention_backward(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, d_out: torch.Tensor, seg: Segments,
+                                   bias: Optional[BucketBias] = None, scale: Optional[float] = None, cap: float = 0.0,
+                                   out: Optional[Sequence[torch.Tensor]] = None, dbias: Optional[torch.Tensor] = None):
+        """(dq, dk, dv, dbias) of segment_attention's inputs; dbias is None without a bias.  `out`: where dq, dk and dv go, which may
+        be slices of one tensor."""
+        p = self._segment_params(q, k, v, seg, bias, scale, cap)
+        if out is None:
+            out = tuple(torch.empty(q.shape, dtype=q.dtype, device=q.device) for _ in range(3))
+        dq, dk, dv = out
+        if bias is not None and dbias is None:
+            dbias = torch.empty_like(bias.table)
+        if dbias is not None and (bias is None or dbias.shape != bias.table.shape or dbias.dtype != torch.float32):
+            raise ValueError("dbias is a float32 tensor of the bias table's shape")
+        rc = self.lib.dsvt_segment_attention_backward(self._h, C.byref(p), *_rows(d_out, q), *_rows(dq, q), *_rows(dk, q),
+                                                      *_rows(dv, q), _ptr(dbias))
+        self._check(rc, "dsvt_segment_attention_backward")
+        return dq, dk, dv, dbias
+
+    # ---- dsvt_layer_norm ----
+    def layer_norm(self, x: torch.Tensor, g: Optional[torch.Tensor], b: Optional[torch.Tensor],
+                   residual: Optional[torch.Tensor] = None, eps: float = 1e-5, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """LayerNorm over the last dimension of x + residual ([n, C]); g and b float32, or None for ones and zeros."""
+        n, Cc = x.shape
+        if out is None:
+            out = torch.empty_like(x)
+        rc = self.lib.dsvt_layer_norm(self._h, _type(x), _ptr(x), _same(residual, x), n, Cc, _float(g, Cc), _float(b, Cc), eps,
+                                      _same(out, x))
+        self._check(rc, "dsvt_layer_norm")
+        return out
+
+    def layer_norm_backward(self, x: torch.Tensor, dy: torch.Tensor, g: Optional[torch.Tensor],
+                            residual: Optional[torch.Tensor] = None, eps: float = 1e-5, out: Optional[torch.Tensor] = None,
+                            dg: Optional[torch.Tensor] = None, db: Optional[torch.Tensor] = None):
+        """(dx, dg, db) of layer_norm(x, g, b, residual); the residual's gradient is dx."""
+        n, Cc = x.shape
+        if out is None:
+            out = torch.empty_like(x)
+        if dg is None:
+            dg = torch.empty(Cc, dtype=torch.float32, device=x.device)
+        if db is None:
+            db = torch.empty(Cc, dtype=torch.float32, device=x.device)
+        rc = self.lib.dsvt_layer_norm_backward(self._h, _type(x), _ptr(x), _same(residual, x), _same(dy, x), n, Cc, _float(g, Cc),
+                                               eps, _same(out, x), _float(dg, Cc), _float(db, Cc))
+        self._check(rc, "dsvt_layer_norm_backward")
+        return out, dg, db
 
     # ---- dsvt_bev_scatter ----
     def bev_scatter(self, coords: torch.Tensor, feats: torch.Tensor, batch: int, grid, channels_last: bool = False,
