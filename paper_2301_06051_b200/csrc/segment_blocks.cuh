@@ -1,0 +1,248 @@
+// Segment attention: what a block works on.  Short segments: all those that start in a block's kRowBlock rows, whole, in shared
+// memory.  Long ones: a tile of the rows of one segment, the segment's other rows passing by in chunks.
+#pragma once
+#include "segment_mma.cuh"
+
+namespace dsvt_train {
+
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kRowBlock = 32;
+constexpr int kShort = 128;                         // most rows of a segment that is held whole
+constexpr int kMaxRows = kRowBlock - 1 + kShort;    // rows of a block
+constexpr int kMaxItems = kRowBlock * (kShort / 16);
+
+// 16 rows of a segment: its first row's place in the block, its length, the tile.
+struct Item { uint8_t at, len, tile, pad; };
+
+struct Plan {
+  int rows, items;
+  uint32_t starts;                        // bit i: a segment starts at place i
+  uint8_t len_at[kRowBlock];
+  uint32_t real[(kMaxRows + 31) / 32 + 3];  // bit i: place i holds a voxel
+  int32_t ids[kMaxRows + 17];
+  Item item[kMaxItems];
+};
+
+// Which entries of seg_start can be of segments that start in rows [from, to): found by 256 probes a round (one for most calls).
+// `first`, `last`: nothing lies before or behind the rows.
+__device__ __forceinline__ int2 segments_near(const SegArgs& a, int from, int to, bool first, bool last) {
+  const int tid = threadIdx.x;
+  int lo = 0, hi = a.cap_segments, end = hi;
+  if (a.num_segments) { const int m = *a.num_segments; end = m < 0 ? 0 : m < end ? m : end; }
+  while (true) {
+    const int span = hi - lo, step = (span + kThreads - 1) / kThreads;
+    const int64_t i = lo + (int64_t)tid * step;
+    const int v = i < hi ? a.seg_start[i] : 0;
+    const bool in = i < hi && i < end;
+    const int below = __syncthreads_count(in && v < from), upto = __syncthreads_count(in && v < to);
+    const int64_t next_hi = lo + (int64_t)upto * step;
+    if (!last && next_hi < hi) hi = (int)next_hi;
+    if (!first && below > 0) lo += (below - 1) * step;
+    if (hi > end) hi = end;
+    if (hi - lo <= 8 * kThreads || hi - lo >= span) break;
+  }
+  return make_int2(lo, hi);
+}
+
+// Copies what every block reads: the index tables of the displacements and its heads' bias, in units of log 2.
+__device__ __forceinline__ void stage_tables(const SegArgs& a, uint16_t* maps, float* bias, int head0, int heads) {
+  if (!a.bias) return;
+  for (int i = threadIdx.x; i < a.maps.at_z + 2 * a.maps.extent[2] - 1; i += kThreads) maps[i] = a.maps.of[i];
+  const int count = min(heads, a.heads - head0) * a.buckets;
+  const float* from = a.bias + (int64_t)head0 * a.buckets;
+  for (int i = threadIdx.x; i < count; i += kThreads) bias[i] = bias_log2(from[i]);
+}
+
+__device__ __forceinline__ int bucket_at(const BucketMaps& m, const uint16_t* maps, int4 i, int4 j) {
+  const int ex = m.extent[0] - 1, ey = m.extent[1] - 1, ez = m.extent[2] - 1;
+  const int dx = min(max(i.y - j.y, -ex), ex) + ex, dy = min(max(i.z - j.z, -ey), ey) + ey + m.at_y, dz = min(max(i.w - j.w, -ez), ez) + ez + m.at_z;
+  return maps[dx] + maps[dy] + maps[dz];
+}
+
+// The block's segments (of at most `limit` rows), their rows' voxels and the list of their tiles.
+__device__ __forceinline__ void make_plan(const SegArgs& a, Plan& p, int4* cells, int block, int blocks, int limit) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, base = block * kRowBlock;
+  if (tid < kRowBlock) p.len_at[tid] = 0;
+  const int2 near = segments_near(a, base, base + kRowBlock, block == 0, block == blocks - 1);
+  __syncthreads();
+  for (int s = near.x + tid; s < near.y; s += kThreads) {
+    const int lo = a.seg_start[s], hi = a.seg_start[s + 1];
+    if (segment_sound(a, lo, hi) && hi - lo <= limit && lo >= base && lo < base + kRowBlock) p.len_at[lo - base] = (uint8_t)(hi - lo);
+  }
+  __syncthreads();
+  if (warp == 0) {
+    const int len = p.len_at[lane], tiles = (len + 15) >> 4;
+    const uint32_t starts = __ballot_sync(kAll, len > 0);
+    int rows = len > 0 ? lane + len : 0, upto = tiles;
+    for (int m = 1; m < 32; m <<= 1) {
+      rows = max(rows, __shfl_xor_sync(kAll, rows, m));
+      const int before = __shfl_up_sync(kAll, upto, m);
+      if (lane >= m) upto += before;
+    }
+    for (int t = 0; t < tiles; ++t) p.item[upto - tiles + t] = Item{(uint8_t)lane, (uint8_t)len, (uint8_t)t, 0};
+    if (lane == 31) p.items = upto;
+    if (lane == 0) { p.rows = rows; p.starts = starts; }
+  }
+  __syncthreads();
+  const int rows = p.rows;
+  const uint32_t starts = p.starts;
+  if (tid < (int)(sizeof(p.real) / 4) * 32) {
+    int id = -1;
+    const uint32_t upto = starts & (tid >= 31 ? kAll : (2u << tid) - 1u);
+    if (tid < rows && upto) {
+      const int at = 31 - __clz(upto);
+      if (tid < at + p.len_at[at]) id = voxel_at(a, base + tid);
+    }
+    const uint32_t real = __ballot_sync(kAll, id >= 0);
+    if (lane == 0) p.real[warp] = real;
+    if (tid < kMaxRows + 17) p.ids[tid] = id;
+    if (a.bias && id >= 0) cells[tid] = a.coords[id];
+  }
+  __syncthreads();
+}
+
+// Bit j: place at + j (j < count <= 64) holds a voxel.
+__device__ __forceinline__ uint64_t real_rows(const Plan& p, int at, int count) {
+  const int w = at >> 5, s = at & 31;
+  const uint64_t lo = (uint64_t)p.real[w] | (uint64_t)p.real[w + 1] << 32;
+  uint64_t v = lo >> s;
+  if (s) v |= (uint64_t)p.real[w + 2] << (64 - s);
+  return count >= 64 ? v : v & (((uint64_t)1 << count) - 1);
+}
+
+// Entries to a row of the bucket tile, for segments of at most `cols` rows: rows of an odd multiple of 16 bytes, so that the eight
+// rows of a score tile's fragment lie in different banks.
+__host__ __device__ constexpr int index_pitch(int cols) { return 8 * (((cols + 15) / 16 * 2) | 1); }
+
+// The buckets of all pairs of the block: index[i][j - first of i's segment].  Columns behind a segment's end stay at 0 or
+// whatever bucket an earlier one left there.
+__device__ __forceinline__ void fill_index(const SegArgs& a, const Plan& p, const int4* cells, const uint16_t* maps, uint16_t* index, int pitch) {
+  const int lane = threadIdx.x & 31;
+  for (int i = threadIdx.x >> 5; i < p.rows; i += kWarps) {
+    const uint32_t upto = p.starts & (i >= 31 ? kAll : (2u << i) - 1u);
+    const int at = upto ? 31 - __clz(upto) : 0, len = p.len_at[at];
+    if (i >= at + len || p.ids[i] < 0) continue;
+    const int4 mine = cells[i];
+    for (int j = lane; j < len; j += 32)
+      if (p.ids[at + j] >= 0) index[i * pitch + j] = (uint16_t)bucket_at(a.maps, maps, mine, cells[at + j]);
+  }
+}
+
+// Rows' parts of a block's heads to shared memory: `chunks` pieces of 16 bytes each, of which the first `real` exist.
+template <typename T>
+__device__ __forceinline__ void load_rows(uint32_t to, uint32_t pitch, const void* from, int64_t ld, const int32_t* ids, int rows, int64_t col, int chunks, int real) {
+  for (int i = threadIdx.x; i < rows * chunks; i += kThreads) {
+    const int r = i / chunks, c = i - r * chunks, id = ids[r];
+    const bool in = id >= 0 && c < real;
+    cp_async16(to + r * pitch + c * 16, (const char*)from + ((in ? (int64_t)id * ld : 0) + col) * (int64_t)sizeof(T) + (in ? c * 16 : 0), in);
+  }
+}
+
+// Rounds two neighbouring channels into a row in shared or global memory.
+template <typename T>
+__device__ __forceinline__ void store2(T* to, float x, float y) {
+  if constexpr (sizeof(T) == 4) *reinterpret_cast<float2*>(to) = make_float2(x, y);
+  else *reinterpret_cast<uint32_t*>(to) = Mma<T>::pack(x, y);
+}
+
+// Scores of queries (rows) and keys (columns) in units of log 2, from products: scale, cap, bias; -inf where a column holds no key.
+// `index`: the fragment's first row's buckets at the chunk's first column (rows g and g + 8 of the tile).
+template <int NP, bool CAP>
+__device__ __forceinline__ void transform(float (&s)[2 * NP][4], float (&slope)[CAP ? 2 * NP : 1][4], const Scoring& sc, const float* bias,
+                                          const uint16_t* index, int pitch, int pairs, uint64_t real) {
+  const int lane = threadIdx.x & 31, q2 = (lane & 3) * 2;
+#pragma unroll
+  for (int t = 0; t < 2 * NP; ++t)
+    if (t / 2 < pairs) {
+      float b[4] = {};
+      if (sc.bias) {
+        const uint32_t i0 = *reinterpret_cast<const uint32_t*>(index + (lane >> 2) * pitch + t * 8 + q2);
+        const uint32_t i1 = *reinterpret_cast<const uint32_t*>(index + ((lane >> 2) + 8) * pitch + t * 8 + q2);
+        b[0] = bias[i0 & 0xffff]; b[1] = bias[i0 >> 16]; b[2] = bias[i1 & 0xffff]; b[3] = bias[i1 >> 16];
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[t][e] = score_of<CAP>(sc, s[t][e], b[e], &slope[CAP ? t : 0][e]);
+      const uint32_t bits = (uint32_t)(real >> (8 * t)) & 0xffu;
+      if (bits != 0xffu) {
+        const uint32_t mine = bits >> q2;
+        if (!(mine & 1)) s[t][0] = s[t][2] = -INFINITY;
+        if (!(mine & 2)) s[t][1] = s[t][3] = -INFINITY;
+      }
+    }
+}
+
+__device__ __forceinline__ float quad_max(float v) {
+  v = fmaxf(v, __shfl_xor_sync(kAll, v, 1));
+  return fmaxf(v, __shfl_xor_sync(kAll, v, 2));
+}
+__device__ __forceinline__ float quad_sum(float v) {
+  v += __shfl_xor_sync(kAll, v, 1);
+  return v + __shfl_xor_sync(kAll, v, 2);
+}
+// 1 / l; a row without keys (l = 0) gives 0.
+__device__ __forceinline__ float inverse(float l) { return l == 0.f ? 0.f : 1.f / l; }
+
+// Running maximum and sum of a fragment's two rows, and the weighted sums.
+template <int DT>
+struct Flow {
+  float m[2], l[2], acc[DT / 8][4];
+  __device__ __forceinline__ void start() {
+    m[0] = m[1] = -INFINITY;
+    l[0] = l[1] = 0.f;
+#pragma unroll
+    for (int n = 0; n < DT / 8; ++n) acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.f;
+  }
+};
+
+// One chunk of keys: s holds the scores, and the weights afterwards.  (l: the lane's share; quad_sum at the end.)
+template <int DT, int NP>
+__device__ __forceinline__ void soften(Flow<DT>& f, float (&s)[2 * NP][4], int pairs) {
+#pragma unroll
+  for (int r = 0; r < 2; ++r) {
+    float m = f.m[r];
+#pragma unroll
+    for (int t = 0; t < 2 * NP; ++t)
+      if (t / 2 < pairs) m = fmaxf(m, fmaxf(s[t][2 * r], s[t][2 * r + 1]));
+    m = quad_max(m);
+    const float base = m == -INFINITY ? 0.f : m, fade = ex2_approx(f.m[r] - base);
+    f.m[r] = m;
+    float l = f.l[r] * fade;
+#pragma unroll
+    for (int t = 0; t < 2 * NP; ++t)
+      if (t / 2 < pairs) {
+        s[t][2 * r] = ex2_approx(s[t][2 * r] - base);
+        s[t][2 * r + 1] = ex2_approx(s[t][2 * r + 1] - base);
+        l += s[t][2 * r] + s[t][2 * r + 1];
+      }
+    f.l[r] = l;
+#pragma unroll
+    for (int n = 0; n < DT / 8; ++n) {
+      f.acc[n][2 * r] *= fade;
+      f.acc[n][2 * r + 1] *= fade;
+    }
+  }
+}
+
+// ---- long segments ---------------------------------------------------------------------------------------------------
+struct Tile { int lo, hi, row; };  // a segment and the first row of a tile of it
+constexpr int kMaxTiles = 4;       // tiles that start in one block's rows (segments of more than 64 rows: at most 3)
+
+// The tiles of `tile` rows of segments longer than `above` that start in rows [base, base + tile).
+__device__ __forceinline__ int find_tiles(const SegArgs& a, Tile* tiles, int* count, int base, int tile, int above) {
+  if (threadIdx.x == 0) *count = 0;
+  const int2 near = segments_near(a, base + 1, base + tile, false, false);
+  __syncthreads();
+  for (int s = near.x + (int)threadIdx.x; s < near.y; s += kThreads) {
+    const int lo = a.seg_start[s], hi = a.seg_start[s + 1];
+    if (lo < 0 || hi > a.n || lo > hi || hi - lo > a.max_len || hi - lo <= above) continue;  // (reported by the short ones' blocks)
+    const int row = lo >= base ? lo : lo + (base - lo + tile - 1) / tile * tile;
+    if (row < hi && row < base + tile) {
+      const int at = atomicAdd(count, 1);
+      if (at < kMaxTiles) tiles[at] = Tile{lo, hi, row};
+    }
+  }
+  __syncthreads();
+  return min(*count, kMaxTiles);
+}
+
+}  // namespace dsvt_train

@@ -1,0 +1,311 @@
+// Segment attention, forward: softmax(q k^T + bias) v inside each segment.
+#pragma once
+#include "segment_blocks.cuh"
+
+namespace dsvt_train {
+
+// Shared memory of a block that holds its segments whole.
+struct ShortLayout {
+  int heads;                                   // of a block
+  int pitch_idx, limit;                        // entries to a row of the bucket tile; longest segment
+  uint32_t pitch, array;                       // bytes of a row and of an array of rows
+  uint32_t maps, bias, cells, index, rows, bytes;
+};
+
+template <typename T, int DT>
+static ShortLayout short_layout(const SegArgs& a, int limit, int arrays) {
+  ShortLayout l = {};
+  l.heads = kHeads<T, DT>;
+  l.limit = limit;
+  const int rows = kRowBlock - 1 + limit + 16;  // (a tile of 16 may begin at the last row)
+  l.pitch = (uint32_t)(l.heads * a.dim * sizeof(T) + 16);
+  l.array = rows * l.pitch;
+  uint32_t at = (sizeof(Plan) + 15) / 16 * 16;
+  auto take = [&](size_t bytes) { const uint32_t was = at; at += (uint32_t)((bytes + 15) / 16 * 16); return was; };
+  if (a.bias) {
+    l.maps = take(sizeof(a.maps.of));
+    l.bias = take((size_t)l.heads * a.buckets * 4);
+    l.cells = take((size_t)(kRowBlock - 1 + limit) * 16);
+    l.pitch_idx = index_pitch(limit);
+    l.index = take((size_t)rows * l.pitch_idx * 2);
+  }
+  l.rows = take((size_t)arrays * l.array + 64);
+  l.bytes = at;
+  return l;
+}
+
+template <typename T, int DT, bool CAP>
+__global__ void __launch_bounds__(kThreads) short_forward_kernel(const __grid_constant__ SegArgs a, const ShortLayout L, const Scoring sc) {
+  extern __shared__ __align__(16) unsigned char smem[];
+  constexpr int HG = kHeads<T, DT>, NP = kPairs<T>;
+  const int dim = kExact<DT> ? DT : a.dim;
+  pdl_enter();
+  Plan& plan = *reinterpret_cast<Plan*>(smem);
+  uint16_t* maps = reinterpret_cast<uint16_t*>(smem + L.maps);
+  float* bias = reinterpret_cast<float*>(smem + L.bias);
+  int4* cells = reinterpret_cast<int4*>(smem + L.cells);
+  uint16_t* index = reinterpret_cast<uint16_t*>(smem + L.index);
+  const int head0 = blockIdx.y * HG, heads = min(HG, a.heads - head0);
+  const uint32_t pitch = kExact<DT> ? HG * DT * sizeof(T) + 16 : L.pitch;
+  const uint32_t q0 = smem_u32(smem + L.rows), k0 = q0 + L.array, v0 = k0 + L.array;
+  stage_tables(a, maps, bias, head0, HG);
+  if (a.bias)
+    for (int i = threadIdx.x; i < (kRowBlock + 15 + L.limit) * L.pitch_idx / 2; i += kThreads) reinterpret_cast<uint32_t*>(index)[i] = 0;
+  make_plan(a, plan, cells, blockIdx.x, gridDim.x, L.limit);
+  const int chunks = HG * dim * (int)sizeof(T) / 16, real = heads * dim * (int)sizeof(T) / 16;
+  const int64_t col = (int64_t)head0 * dim;
+  load_rows<T>(q0, pitch, a.q, a.ld_q, plan.ids, plan.rows, col, chunks, real);
+  load_rows<T>(k0, pitch, a.k, a.ld_k, plan.ids, plan.rows, col, chunks, real);
+  load_rows<T>(v0, pitch, a.v, a.ld_v, plan.ids, plan.rows, col, chunks, real);
+  cp_commit();
+  if (a.bias) fill_index(a, plan, cells, maps, index, L.pitch_idx);
+  cp_wait<0>();
+  __syncthreads();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, h = warp % HG;
+  if (h < heads) {
+    const uint32_t at_head = h * dim * sizeof(T);
+    for (int it = warp / HG; it < plan.items; it += kWarps / HG) {
+      const Item item = plan.item[it];
+      const int row = item.at + 16 * item.tile;
+      const uint32_t qa = q0 + row * pitch + at_head;
+      Flow<DT> f;
+      f.start();
+      for (int j = 0; j < item.len; j += 16 * NP) {
+        const int cols = min(16 * NP, item.len - j), pairs = (cols + 15) >> 4;
+        const uint64_t keys = real_rows(plan, item.at + j, cols);
+        const uint32_t at = (item.at + j) * pitch + at_head;
+        float s[2 * NP][4], none[CAP ? 2 * NP : 1][4];
+        scores<T, DT, NP>(s, qa, k0 + at, pitch, dim, pairs);
+        transform<NP, CAP>(s, none, sc, bias + h * a.buckets, index + row * L.pitch_idx + j, L.pitch_idx, pairs, keys);
+        soften<DT, NP>(f, s, pairs);
+        weigh<T, DT, NP, false>(f.acc, s, v0 + at, pitch, dim, pairs, keys);
+      }
+      // the result takes the place of the queries (this warp's alone: a head's channels of a tile's rows)
+      const float i0 = inverse(quad_sum(f.l[0])), i1 = inverse(quad_sum(f.l[1]));
+      const int r0 = 16 * item.tile + (lane >> 2);
+      T* to = reinterpret_cast<T*>(smem + L.rows + (item.at + r0) * pitch + at_head) + (lane & 3) * 2;
+      __syncwarp();
+#pragma unroll
+      for (int n = 0; n < DT / 8; ++n) {
+        if (!kExact<DT> && n * 8 >= dim) break;
+        if (r0 < item.len) store2<T>(to + n * 8, f.acc[n][0] * i0, f.acc[n][1] * i0);
+        if (r0 + 8 < item.len) store2<T>(reinterpret_cast<T*>(reinterpret_cast<char*>(to) + 8 * pitch) + n * 8, f.acc[n][2] * i1, f.acc[n][3] * i1);
+      }
+    }
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < plan.rows * chunks; i += kThreads) {
+    const int r = i / chunks, c = i - r * chunks, id = plan.ids[r];
+    if (id >= 0 && c < real)
+      *reinterpret_cast<uint4*>((char*)a.out + ((int64_t)id * a.ld_out + col) * (int64_t)sizeof(T) + c * 16) = *reinterpret_cast<const uint4*>(smem + L.rows + r * pitch + c * 16);
+  }
+}
+
+// Shared memory of a tile of a long segment: `own` arrays of the tile's rows, `passing` arrays of two chunks.
+struct LongLayout {
+  int pitch_idx;
+  uint32_t pitch, tile, chunk;  // bytes of a row, of an array of the tile's rows, of an array of a chunk's rows
+  uint32_t maps, bias, cells, passing_cells, ids, index, rows, passing, more, bytes;
+};
+
+template <typename T, int DT>
+struct LongShape {
+  static constexpr int HG = kHeads<T, DT>, WH = HG < 2 ? HG : 2, HPW = HG / WH, rows = 16 * kWarps / WH, chunk = 16 * kPairs<T>;
+};
+
+template <typename T, int DT>
+static LongLayout long_layout(const SegArgs& a, int own, int passing, size_t more) {
+  using S = LongShape<T, DT>;
+  LongLayout l = {};
+  l.pitch = (uint32_t)(S::HG * a.dim * sizeof(T) + 16);
+  l.tile = S::rows * l.pitch;
+  l.chunk = S::chunk * l.pitch;
+  uint32_t at = 0;
+  auto take = [&](size_t bytes) { const uint32_t was = at; at += (uint32_t)((bytes + 15) / 16 * 16); return was; };
+  l.ids = take((size_t)(S::rows + 3 * S::chunk) * 4);
+  if (a.bias) {
+    l.maps = take(sizeof(a.maps.of));
+    l.bias = take((size_t)S::HG * a.buckets * 4);
+    l.cells = take((size_t)S::rows * 16);
+    l.passing_cells = take((size_t)3 * S::chunk * 16);
+    l.pitch_idx = S::chunk + 8;
+    l.index = take((size_t)S::rows * l.pitch_idx * 2);
+  }
+  l.more = take(more);
+  l.rows = take((size_t)own * l.tile + 64);
+  l.passing = take((size_t)2 * passing * l.chunk + 64);
+  l.bytes = at;
+  return l;
+}
+
+// The chunks of a segment's rows on their way through shared memory, one ahead of the one in work.  Rows have two buffers; voxels
+// and cells, which are written before the barrier that frees the chunk before, three.
+template <typename T, int DT>
+struct Passing {
+  using S = LongShape<T, DT>;
+  const SegArgs& a;
+  const LongLayout& L;
+  unsigned char* smem;
+  int lo, hi, mine;  // the segment, and this thread's voxel of the next chunk
+  __device__ __forceinline__ int32_t* ids(int c) const { return reinterpret_cast<int32_t*>(smem + L.ids) + S::rows + c % 3 * S::chunk; }
+  __device__ __forceinline__ int4* cells(int c) const { return reinterpret_cast<int4*>(smem + L.passing_cells) + c % 3 * S::chunk; }
+  __device__ __forceinline__ uint32_t array(int c, int which, int arrays) const { return smem_u32(smem + L.passing) + ((c & 1) * arrays + which) * L.chunk; }
+  __device__ __forceinline__ void fetch_id(int at) {
+    mine = -1;
+    if (threadIdx.x < S::chunk && at + (int)threadIdx.x < hi) mine = voxel_at(a, at + threadIdx.x);
+  }
+};
+
+template <typename T, int DT, bool CAP>
+__global__ void __launch_bounds__(kThreads) long_forward_kernel(const __grid_constant__ SegArgs a, const LongLayout L, const Scoring sc, int above) {
+  extern __shared__ __align__(16) unsigned char smem[];
+  using S = LongShape<T, DT>;
+  constexpr int NP = kPairs<T>;
+  __shared__ Tile tiles[kMaxTiles];
+  __shared__ int tile_count;
+  const int dim = kExact<DT> ? DT : a.dim;
+  pdl_enter();
+  const int found = find_tiles(a, tiles, &tile_count, blockIdx.x * S::rows, S::rows, above);
+  if (found == 0) return;
+  uint16_t* maps = reinterpret_cast<uint16_t*>(smem + L.maps);
+  float* bias = reinterpret_cast<float*>(smem + L.bias);
+  int4* cells = reinterpret_cast<int4*>(smem + L.cells);
+  uint16_t* index = reinterpret_cast<uint16_t*>(smem + L.index);
+  int32_t* ids = reinterpret_cast<int32_t*>(smem + L.ids);
+  const int head0 = blockIdx.y * S::HG, heads = min(S::HG, a.heads - head0);
+  const uint32_t pitch = kExact<DT> ? S::HG * DT * sizeof(T) + 16 : L.pitch;
+  const uint32_t q0 = smem_u32(smem + L.rows);
+  stage_tables(a, maps, bias, head0, S::HG);
+  const int chunks = S::HG * dim * (int)sizeof(T) / 16, real = heads * dim * (int)sizeof(T) / 16;
+  const int64_t col = (int64_t)head0 * dim;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int row = 16 * (warp / S::WH);  // of the warp's tile of 16
+  for (int ti = 0; ti < found; ++ti) {
+    const Tile tile = tiles[ti];
+    const int rows = min(S::rows, tile.hi - tile.row);
+    Passing<T, DT> pass{a, L, smem, tile.lo, tile.hi, -1};
+    __syncthreads();  // (the tile before is done with the shared memory)
+    if (threadIdx.x < S::rows) {
+      const int id = (int)threadIdx.x < rows ? voxel_at(a, tile.row + threadIdx.x) : -1;
+      ids[threadIdx.x] = id;
+      if (a.bias) cells[threadIdx.x] = id >= 0 ? a.coords[id] : make_int4(0, 0, 0, 0);
+    }
+    auto publish = [&](int c) {
+      if (threadIdx.x < S::chunk) {
+        pass.ids(c)[threadIdx.x] = pass.mine;
+        if (a.bias) pass.cells(c)[threadIdx.x] = pass.mine >= 0 ? a.coords[pass.mine] : make_int4(0, 0, 0, 0);
+      }
+    };
+    auto load = [&](int c) {
+      load_rows<T>(pass.array(c, 0, 2), pitch, a.k, a.ld_k, pass.ids(c), S::chunk, col, chunks, real);
+      load_rows<T>(pass.array(c, 1, 2), pitch, a.v, a.ld_v, pass.ids(c), S::chunk, col, chunks, real);
+      cp_commit();
+    };
+    pass.fetch_id(tile.lo);
+    publish(0);
+    pass.fetch_id(tile.lo + S::chunk);
+    __syncthreads();
+    load_rows<T>(q0, pitch, a.q, a.ld_q, ids, S::rows, col, chunks, real);
+    load(0);
+    Flow<DT> f[S::HPW];
+#pragma unroll
+    for (int i = 0; i < S::HPW; ++i) f[i].start();
+    const int parts = (tile.hi - tile.lo + S::chunk - 1) / S::chunk;
+    for (int c = 0; c < parts; ++c) {
+      const int cols = min(S::chunk, tile.hi - tile.lo - c * S::chunk), pairs = (cols + 15) >> 4;
+      if (c + 1 < parts) publish(c + 1);
+      cp_wait<0>();
+      __syncthreads();  // this chunk is there, the other one's buffer free
+      if (c + 1 < parts) {
+        load(c + 1);
+        pass.fetch_id(tile.lo + (c + 2) * S::chunk);
+      }
+      if (a.bias) {
+        for (int i = threadIdx.x; i < S::rows * S::chunk; i += kThreads) {
+          const int r = i / S::chunk, j = i % S::chunk;
+          index[r * L.pitch_idx + j] = (uint16_t)bucket_at(a.maps, maps, cells[r], pass.cells(c)[j]);
+        }
+        __syncthreads();
+      }
+      uint64_t keys = 0;
+      {
+        const int32_t* at = pass.ids(c);
+        keys = __ballot_sync(kAll, at[lane] >= 0);
+        const bool second = 32 + lane < S::chunk && at[32 + lane] >= 0;
+        keys |= (uint64_t)__ballot_sync(kAll, second) << 32;
+      }
+#pragma unroll
+      for (int i = 0; i < S::HPW; ++i) {
+        const int h = (warp % S::WH) * S::HPW + i;
+        if (h < heads && row < rows) {
+          const uint32_t at_head = h * dim * sizeof(T);
+          float s[2 * NP][4], none[CAP ? 2 * NP : 1][4];
+          scores<T, DT, NP>(s, q0 + row * pitch + at_head, pass.array(c, 0, 2) + at_head, pitch, dim, pairs);
+          transform<NP, CAP>(s, none, sc, bias + h * a.buckets, index + row * L.pitch_idx, L.pitch_idx, pairs, keys);
+          soften<DT, NP>(f[i], s, pairs);
+          weigh<T, DT, NP, false>(f[i].acc, s, pass.array(c, 1, 2) + at_head, pitch, dim, pairs, keys);
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < S::HPW; ++i) {
+      const int h = (warp % S::WH) * S::HPW + i;
+      if (h >= heads || row >= rows) continue;
+      const float i0 = inverse(quad_sum(f[i].l[0])), i1 = inverse(quad_sum(f[i].l[1]));
+      const int r0 = row + (lane >> 2), id0 = ids[r0], id1 = ids[r0 + 8];
+      T* to = (T*)a.out + col + h * dim + (lane & 3) * 2;
+#pragma unroll
+      for (int n = 0; n < DT / 8; ++n) {
+        if (!kExact<DT> && n * 8 >= dim) break;
+        if (id0 >= 0) store2<T>(to + id0 * a.ld_out + n * 8, f[i].acc[n][0] * i0, f[i].acc[n][1] * i0);
+        if (id1 >= 0) store2<T>(to + id1 * a.ld_out + n * 8, f[i].acc[n][2] * i1, f[i].acc[n][3] * i1);
+      }
+    }
+  }
+}
+
+// Up to kShort rows a segment is held whole where that leaves room for two blocks on an SM, or at least for one; in calls with longer
+// ones up to 64 rows, and the longer ones go through in tiles.
+constexpr uint32_t kSmemMost = 227 * 1024;
+
+template <typename K>
+static int allow_smem(dsvt_ctx* ctx, K kernel, uint32_t bytes) {
+  if (bytes > 48 * 1024) DSVT_CUDA_TRY(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+  return DSVT_OK;
+}
+
+template <typename T, int DT, bool CAP>
+int forward_of(dsvt_ctx* ctx, const SegArgs& a) {
+  int limit = a.max_len <= kShort ? a.max_len : 64;
+  ShortLayout l = short_layout<T, DT>(a, limit, 3);
+  if (l.bytes > kSmemMost) l = short_layout<T, DT>(a, limit = 64, 3);
+  const Scoring sc = scoring_of(a);
+  const unsigned groups = (unsigned)dsvt_ceil_div(a.heads, kHeads<T, DT>);
+  auto kernel = short_forward_kernel<T, DT, CAP>;
+  int rc = allow_smem(ctx, kernel, l.bytes);
+  if (rc != DSVT_OK) return rc;
+  launch_pdl(kernel, dim3((unsigned)dsvt_ceil_div(a.n, kRowBlock), groups), dim3(kThreads), l.bytes, ctx->stream, a, l, sc);
+  DSVT_LAUNCHED(ctx);
+  if (limit >= a.max_len) return DSVT_OK;
+  using S = LongShape<T, DT>;
+  const LongLayout g = long_layout<T, DT>(a, 1, 2, 0);
+  auto longer = long_forward_kernel<T, DT, CAP>;
+  rc = allow_smem(ctx, longer, g.bytes);
+  if (rc != DSVT_OK) return rc;
+  launch_pdl(longer, dim3((unsigned)dsvt_ceil_div(a.n, S::rows), groups), dim3(kThreads), g.bytes, ctx->stream, a, g, sc, limit);
+  DSVT_LAUNCHED(ctx);
+  return DSVT_OK;
+}
+
+template <typename T>
+int launch_forward(dsvt_ctx* ctx, const SegArgs& a) {
+#define DSVT_FORWARD(DT) return a.cap > 0.f ? forward_of<T, DT, true>(ctx, a) : forward_of<T, DT, false>(ctx, a)
+  if (a.dim == 16) DSVT_FORWARD(16);
+  if (a.dim == 24) DSVT_FORWARD(24);
+  if (a.dim == 32) DSVT_FORWARD(32);
+  if (a.dim <= 64) DSVT_FORWARD(64);
+  DSVT_FORWARD(128);
+#undef DSVT_FORWARD
+}
+
+}  // namespace dsvt_train

@@ -1,0 +1,299 @@
+// Segment attention on the tensor cores: tiles of 16 rows times the rows of a chunk, operands in shared memory.
+//
+// Two products carry every pass.  scores(): C[16][cols] = A B^T over the channels (q k^T, do v^T and their transposes); weigh():
+// acc[16][dim] += W B, where W is a result of scores() in registers (p v, dz k, ...).  A score tile's accumulator layout is the
+// next product's operand layout, so W never leaves the registers; and since a pass exists for either side of the score matrix, none
+// is ever transposed.
+//
+// mma.sync and not tcgen05: a segment has a few dozen to a thousand rows and a head 16 to 64 channels, so that a score takes 2 dim
+// multiply-adds beside a table look-up, an exponential and a dozen other instructions.  m16n8k16 runs at 556 TFLOP/s here (1.1 ns an
+// instruction and SM); the tile's look-ups in shared memory take longer than its products (dim 24: 3.9 ns of products beside 5.2 ns of
+// look-ups).  Tiles of 128 rows in TMEM would leave most of their rows empty in sets of 36 and add a round trip to each score.
+//
+// 16-bit types: products exact, sums fp32, W rounded to the type.  For float16's gradients W goes in as tf32 (same 11 bits, but
+// float's range: dz of large gradients passes 65504), and the other operand, exact in tf32, with it.
+// fp32: both operands as two tf32 parts x = hi + lo (each rounded: |x - hi - lo| <= 2^-22 |x|); hi hi, hi lo and lo hi are formed,
+// lo lo (2^-22) is left out.  The tensor cores truncate when they add, so the small products have accumulators of their own and a
+// chunk's sums meet the running ones in additions that round.
+#pragma once
+#include "segment.cuh"
+#include "tc_ptx.cuh"
+
+namespace dsvt_train {
+
+constexpr unsigned kAll = 0xffffffffu;
+constexpr float kLog2e = 1.4426950408889634f;
+
+using dsvt_tc::ex2_approx;
+using dsvt_tc::smem_u32;
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool real) {
+  const int size = real ? 16 : 0;  // (nothing read: zeros)
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(size) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+__device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t a) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a) : "memory");
+}
+__device__ __forceinline__ void ldsm2(uint32_t& r0, uint32_t& r1, uint32_t a) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x2.shared.b16 {%0,%1}, [%2];" : "=r"(r0), "=r"(r1) : "r"(a) : "memory");
+}
+__device__ __forceinline__ void ldsm4_t(uint32_t (&r)[4], uint32_t a) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a) : "memory");
+}
+__device__ __forceinline__ void ldsm2_t(uint32_t& r0, uint32_t& r1, uint32_t a) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x2.trans.shared.b16 {%0,%1}, [%2];" : "=r"(r0), "=r"(r1) : "r"(a) : "memory");
+}
+__device__ __forceinline__ float lds(uint32_t a) {
+  float v;
+  asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
+  return v;
+}
+
+#define DSVT_MMA16(NAME, TYPE)                                                                                                       \
+  __device__ __forceinline__ void NAME(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) { \
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32." TYPE "." TYPE ".f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"  \
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])                                                                    \
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));                                                            \
+  }                                                                                                                                  \
+  __device__ __forceinline__ void NAME##_k8(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t b0) {                                  \
+    asm volatile("mma.sync.aligned.m16n8k8.row.col.f32." TYPE "." TYPE ".f32 {%0,%1,%2,%3}, {%4,%5}, {%6}, {%0,%1,%2,%3};"            \
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])                                                                    \
+                 : "r"(a0), "r"(a1), "r"(b0));                                                                                       \
+  }
+DSVT_MMA16(mma_bf16, "bf16")
+DSVT_MMA16(mma_f16, "f16")
+__device__ __forceinline__ void mma_tf32(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t tf32(float v) {
+  uint32_t r;
+  asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(r) : "f"(v));
+  return r;
+}
+struct Parts { uint32_t hi, lo; };
+__device__ __forceinline__ Parts split(float v) {
+  Parts p;
+  p.hi = tf32(v);
+  p.lo = tf32(v - __uint_as_float(p.hi));
+  return p;
+}
+
+template <typename T>
+struct Mma;
+template <>
+struct Mma<__nv_bfloat16> {
+  static __device__ __forceinline__ void k16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) { mma_bf16(c, a0, a1, a2, a3, b0, b1); }
+  static __device__ __forceinline__ void k8(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t b0) { mma_bf16_k8(c, a0, a1, b0); }
+  static __device__ __forceinline__ uint32_t pack(float lo, float hi) { return dsvt_tc::pack_bf16(lo, hi); }
+};
+template <>
+struct Mma<__half> {
+  static __device__ __forceinline__ void k16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) { mma_f16(c, a0, a1, a2, a3, b0, b1); }
+  static __device__ __forceinline__ void k8(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t b0) { mma_f16_k8(c, a0, a1, b0); }
+  static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
+    const __half2 h = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+};
+
+// Heads of a block, so that a row's part is 128 to 256 bytes: what one block reads of a row is whole sectors.
+template <typename T, int DT>
+constexpr int kHeads = DT * sizeof(T) <= 32 ? 8 : DT * sizeof(T) <= 64 ? 4 : DT * sizeof(T) <= 128 ? 2 : 1;
+// Pairs of 8 columns of a chunk of scores: what fits in registers beside the accumulators.
+template <typename T>
+constexpr int kPairs = sizeof(T) == 4 ? 3 : 4;
+// DT of 16, 24 and 32 are the channels of a head; 64 and 128 take any multiple of 8 up to them.
+template <int DT>
+constexpr bool kExact = DT <= 32;
+
+// C[i][j] for the 16 rows at a and `pairs` times 16 rows at b; both addresses are of a head's first channel, rows `pitch` bytes apart.
+template <typename T, int DT, int NP>
+__device__ __forceinline__ void scores(float (&c)[2 * NP][4], uint32_t a, uint32_t b, uint32_t pitch, int dim, int pairs) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int t = 0; t < 2 * NP; ++t) c[t][0] = c[t][1] = c[t][2] = c[t][3] = 0.f;
+  if constexpr (sizeof(T) == 2) {
+    const uint32_t ra = a + (lane & 15) * pitch + (lane >> 4) * 16;
+    const uint32_t rb = b + ((lane & 7) + (lane >> 4) * 8) * pitch + ((lane >> 3) & 1) * 16;
+#pragma unroll
+    for (int k = 0; k < (DT + 15) / 16; ++k) {
+      if (!kExact<DT> && k * 16 >= dim) break;
+      if (kExact<DT> ? k * 16 + 16 <= DT : k * 16 + 16 <= dim) {
+        uint32_t f[4];
+        ldsm4(f, ra + k * 32);
+#pragma unroll
+        for (int p = 0; p < NP; ++p)
+          if (p < pairs) {
+            uint32_t g[4];
+            ldsm4(g, rb + p * 16 * pitch + k * 32);
+            Mma<T>::k16(c[2 * p], f[0], f[1], f[2], f[3], g[0], g[1]);
+            Mma<T>::k16(c[2 * p + 1], f[0], f[1], f[2], f[3], g[2], g[3]);
+          }
+      } else {  // the last 8 channels
+        uint32_t f0, f1;
+        ldsm2(f0, f1, a + (lane & 15) * pitch + k * 32);
+#pragma unroll
+        for (int p = 0; p < NP; ++p)
+          if (p < pairs) {
+            uint32_t g0, g1;
+            ldsm2(g0, g1, b + (p * 16 + (lane & 15)) * pitch + k * 32);
+            Mma<T>::k8(c[2 * p], f0, f1, g0);
+            Mma<T>::k8(c[2 * p + 1], f0, f1, g1);
+          }
+      }
+    }
+  } else {
+    float s[2 * NP][4];  // hi lo + lo hi
+#pragma unroll
+    for (int t = 0; t < 2 * NP; ++t) s[t][0] = s[t][1] = s[t][2] = s[t][3] = 0.f;
+    const uint32_t ra = a + (lane >> 2) * pitch + (lane & 3) * 4, rb = b + (lane >> 2) * pitch + (lane & 3) * 4;
+#pragma unroll
+    for (int k = 0; k < DT / 8; ++k) {
+      if (!kExact<DT> && k * 8 >= dim) break;
+      Parts f[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) f[i] = split(lds(ra + (i & 1) * 8 * pitch + k * 32 + (i >> 1) * 16));
+#pragma unroll
+      for (int t = 0; t < 2 * NP; ++t)
+        if (t / 2 < pairs) {
+          const Parts g0 = split(lds(rb + t * 8 * pitch + k * 32)), g1 = split(lds(rb + t * 8 * pitch + k * 32 + 16));
+          mma_tf32(s[t], f[0].lo, f[1].lo, f[2].lo, f[3].lo, g0.hi, g1.hi);
+          mma_tf32(s[t], f[0].hi, f[1].hi, f[2].hi, f[3].hi, g0.lo, g1.lo);
+          mma_tf32(c[t], f[0].hi, f[1].hi, f[2].hi, f[3].hi, g0.hi, g1.hi);
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < 2 * NP; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) c[t][e] += s[t][e];
+  }
+}
+
+// acc += W B: W[i][j] over the `pairs` times 16 rows j at b.  Bit j of `real` says whether row j counts: what lies in the others is
+// not looked at, finite or not.  WIDE: W in tf32 (float16's gradients).
+template <typename T, int DT, int NP, bool WIDE>
+__device__ __forceinline__ void weigh(float (&acc)[DT / 8][4], const float (&w)[2 * NP][4], uint32_t b, uint32_t pitch, int dim, int pairs,
+                                      uint64_t real) {
+  const int lane = threadIdx.x & 31, q2 = (lane & 3) * 2;
+  if constexpr (sizeof(T) == 2) {
+    const uint32_t rb = b + (lane & 15) * pitch + (lane >> 4) * 16;
+#pragma unroll
+    for (int p = 0; p < NP; ++p)
+      if (p < pairs) {
+        const uint32_t bits = (uint32_t)(real >> (16 * p)) & 0xffffu;
+        uint32_t m0 = kAll, m1 = kAll;
+        if (bits != 0xffffu) {
+          const uint32_t mine = bits >> q2;
+          m0 = ((mine & 1) ? 0xffffu : 0u) | ((mine & 2) ? 0xffff0000u : 0u);
+          m1 = ((mine & 0x100) ? 0xffffu : 0u) | ((mine & 0x200) ? 0xffff0000u : 0u);
+        }
+        uint32_t a[4];
+        if (!WIDE) {
+          a[0] = Mma<T>::pack(w[2 * p][0], w[2 * p][1]);
+          a[1] = Mma<T>::pack(w[2 * p][2], w[2 * p][3]);
+          a[2] = Mma<T>::pack(w[2 * p + 1][0], w[2 * p + 1][1]);
+          a[3] = Mma<T>::pack(w[2 * p + 1][2], w[2 * p + 1][3]);
+        }
+        auto tile = [&](int n, uint32_t b0, uint32_t b1) {
+          b0 &= m0;
+          b1 &= m1;
+          if (!WIDE) {
+            Mma<T>::k16(acc[n], a[0], a[1], a[2], a[3], b0, b1);
+          } else {  // eight rows each; their order in the product is that of the accumulators: 0, 2, 4, 6, 1, 3, 5, 7
+            const float2 u = __half22float2(*reinterpret_cast<const __half2*>(&b0)), v = __half22float2(*reinterpret_cast<const __half2*>(&b1));
+            mma_tf32(acc[n], tf32(w[2 * p][0]), tf32(w[2 * p][2]), tf32(w[2 * p][1]), tf32(w[2 * p][3]), __float_as_uint(u.x), __float_as_uint(u.y));
+            mma_tf32(acc[n], tf32(w[2 * p + 1][0]), tf32(w[2 * p + 1][2]), tf32(w[2 * p + 1][1]), tf32(w[2 * p + 1][3]), __float_as_uint(v.x), __float_as_uint(v.y));
+          }
+        };
+#pragma unroll
+        for (int n = 0; n < DT / 8; n += 2) {
+          if (!kExact<DT> && n * 8 >= dim) break;
+          if (kExact<DT> ? n + 2 <= DT / 8 : n * 8 + 16 <= dim) {
+            uint32_t g[4];
+            ldsm4_t(g, rb + p * 16 * pitch + n * 16);
+            tile(n, g[0], g[1]);
+            tile(n + 1, g[2], g[3]);
+          } else {
+            uint32_t g0, g1;
+            ldsm2_t(g0, g1, b + (p * 16 + (lane & 15)) * pitch + n * 16);
+            tile(n, g0, g1);
+          }
+        }
+      }
+  } else {
+    const uint32_t rb = b + q2 * pitch + (lane >> 2) * 4;
+    Parts a[2 * NP][4];
+#pragma unroll
+    for (int t = 0; t < 2 * NP; ++t) {
+      a[t][0] = split(w[t][0]);
+      a[t][1] = split(w[t][2]);
+      a[t][2] = split(w[t][1]);
+      a[t][3] = split(w[t][3]);
+    }
+#pragma unroll
+    for (int n = 0; n < DT / 8; ++n) {
+      if (!kExact<DT> && n * 8 >= dim) break;
+      float c[4] = {}, s[4] = {};
+#pragma unroll
+      for (int t = 0; t < 2 * NP; ++t)
+        if (t / 2 < pairs) {
+          const uint32_t mine = (uint32_t)(real >> (8 * t)) >> q2;
+          const Parts g0 = split((mine & 1) ? lds(rb + t * 8 * pitch + n * 32) : 0.f);
+          const Parts g1 = split((mine & 2) ? lds(rb + (t * 8 + 1) * pitch + n * 32) : 0.f);
+          mma_tf32(s, a[t][0].lo, a[t][1].lo, a[t][2].lo, a[t][3].lo, g0.hi, g1.hi);
+          mma_tf32(s, a[t][0].hi, a[t][1].hi, a[t][2].hi, a[t][3].hi, g0.lo, g1.lo);
+          mma_tf32(c, a[t][0].hi, a[t][1].hi, a[t][2].hi, a[t][3].hi, g0.hi, g1.hi);
+        }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[n][e] += c[e] + s[e];
+    }
+  }
+}
+
+// The scores' transformation: products -> scale, cap, bias, in units of log 2.
+struct Scoring {
+  float scale;   // CAP: of the product to tanh's argument; else to units of log 2
+  float cap;     // cap in units of log 2
+  bool bias;
+};
+static inline Scoring scoring_of(const SegArgs& a) {
+  Scoring s;
+  s.scale = a.cap > 0.f ? a.scale / a.cap : a.scale * kLog2e;
+  s.cap = a.cap * kLog2e;
+  s.bias = a.bias != nullptr;
+  return s;
+}
+// A bias entry in units of log 2.  (Clamped: the lowest float stays the lowest, whatever is added, and differences of two are zero.)
+__device__ __forceinline__ float bias_log2(float b) { return b == -INFINITY ? b : fmaxf(b * kLog2e, -3.402823466e38f); }
+
+template <bool CAP>
+__device__ __forceinline__ float score_of(const Scoring& s, float z, float bias, float* slope) {
+  if (!CAP) return fmaf(z, s.scale, bias);
+  const float t = tanhf(z * s.scale);
+  *slope = fmaf(-t, t, 1.f);
+  return fmaf(t, s.cap, bias);
+}
+
+// ---- loading -------------------------------------------------------------------------------------------------------
+// Smallest s with key <= at[s], or count; a warp together.  (Entries that do not ascend give some s in [0, count].)
+__device__ __forceinline__ int first_not_below(const int32_t* at, int count, int key) {
+  const int lane = threadIdx.x & 31;
+  int lo = 0, hi = count;
+  while (hi - lo > 32) {
+    const int step = (hi - lo + 31) >> 5, i = lo + lane * step;
+    const int below = __popc(__ballot_sync(kAll, i < hi && at[i] < key));
+    if (below == 0) return lo;
+    const int end = lo + below * step;
+    lo += (below - 1) * step + 1;
+    hi = end < hi ? end : hi;
+  }
+  return lo + __popc(__ballot_sync(kAll, lo + lane < hi && at[lo + lane] < key));
+}
+
+}  // namespace dsvt_train

@@ -134,14 +134,6 @@ __global__ void __launch_bounds__(kThreads) rows_kernel(const SegArgs a, float* 
 }  // namespace
 
 template <typename T>
-int launch_forward(dsvt_ctx* ctx, const SegArgs& a) {
-  const int blocks = a.cap_segments < 16 * ctx->sm_count ? a.cap_segments : 16 * ctx->sm_count;
-  rows_kernel<T, 0><<<dim3(blocks, a.heads), kThreads, 0, ctx->stream>>>(a, nullptr);
-  DSVT_LAUNCHED(ctx);
-  return DSVT_OK;
-}
-
-template <typename T>
 int launch_backward(dsvt_ctx* ctx, const SegArgs& a) {
   if ((int64_t)a.n * a.heads * 3 > (int64_t)(4 * ctx->bm_words)) return DSVT_ERR_CAPACITY;
   float* stats = reinterpret_cast<float*>(ctx->bm_zero);
@@ -154,11 +146,8 @@ int launch_backward(dsvt_ctx* ctx, const SegArgs& a) {
   return DSVT_OK;
 }
 
-#define DSVT_SEGMENT_TYPE(T)                                    \
-  template int launch_forward<T>(dsvt_ctx*, const SegArgs&);    \
-  template int launch_backward<T>(dsvt_ctx*, const SegArgs&);
-DSVT_SEGMENT_TYPE(float)
-DSVT_SEGMENT_TYPE(__nv_bfloat16)
-DSVT_SEGMENT_TYPE(__half)
+template int launch_backward<float>(dsvt_ctx*, const SegArgs&);
+template int launch_backward<__nv_bfloat16>(dsvt_ctx*, const SegArgs&);
+template int launch_backward<__half>(dsvt_ctx*, const SegArgs&);
 
 }  // namespace dsvt_train
