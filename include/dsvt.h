@@ -444,7 +444,12 @@ int dsvt_segment_attention(dsvt_ctx* ctx, const dsvt_segment_attention_params* p
  * The gradients of dsvt_segment_attention's inputs from that of its output, d_out (rows of `type`, stride ld_dout): dq, dk, dv
  * (rows of `type`, strides ld_dq, ld_dk, ld_dv, 16-byte aligned, may not alias the inputs or each other) and dbias (float
  * [heads][buckets]; NULL to leave it out, and without a bias).  The forward pass saves nothing for it.  Rows of voxels in no segment
- * are left as they were; dbias is written in full.
+ * are left as they were; dbias is written in full (a value that is not finite makes its entry NaN).  The same inputs give the same bits.
+ *
+ * dbias adds up dS = P (dP - D), D = sum P dP, in whole multiples of at most 2^-33 times the call's largest max_j |P dP| + |D| max_j P.
+ *
+ * Needs heads * buckets <= 2^18 with dbias (else DSVT_ERR_UNSUPPORTED), and n <= 1,700,000 where max_len is above 24 (else
+ * DSVT_ERR_CAPACITY).
  */
 int dsvt_segment_attention_backward(dsvt_ctx* ctx, const dsvt_segment_attention_params* params, const void* d_out,
                                     int64_t ld_dout, void* dq, int64_t ld_dq, void* dk, int64_t ld_dk, void* dv, int64_t ld_dv,

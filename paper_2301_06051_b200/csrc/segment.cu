@@ -88,6 +88,7 @@ extern "C" int dsvt_segment_attention_backward(dsvt_ctx* ctx, const dsvt_segment
   const int rc = check(ctx, params, &a);
   if (rc != DSVT_OK) return rc;
   if (((uintptr_t)dbias & 3) != 0 || (dbias && !a.bias)) return DSVT_ERR_INVALID_ARG;
+  if (dbias && (int64_t)a.heads * a.buckets > kMaxBiasTable) return DSVT_ERR_UNSUPPORTED;
   DeviceGuard on(ctx->device);
   if (a.n > 0) {
     const int64_t width = (int64_t)a.heads * a.dim;

@@ -1,10 +1,13 @@
 // Segment attention: the call as its kernels see it, and the launchers.
 #pragma once
+#include <type_traits>
+
 #include "train_types.cuh"
 
 namespace dsvt_train {
 
 constexpr int kMaxExtent = 128, kMaxBuckets = 1024, kMaxDim = 128;
+constexpr int64_t kMaxBiasTable = 1 << 18;  // entries of a bias whose gradient is asked for: what the workspace has room for
 
 // The additive bucket indexes of the displacements along x, y and z: at [0, 2L-1), [at_y, at_y + 2W-1), [at_z, ...).
 struct BucketMaps {

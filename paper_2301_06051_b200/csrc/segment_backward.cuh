@@ -1,0 +1,728 @@
+// Segment attention, backward: two passes over the scores, each with them in registers the way it needs them.
+//
+//   by queries: maximum, sum and D of a row, then dq = scale dz k
+//   by keys:    p and dz again from those three, dk = scale dz^T q, dv = p^T do, and the bias's gradient
+//
+// Short segments do both in one block, long ones in two kernels.  D = sum_j p dp is formed from the scores and not from the output:
+// the output's rounding to 16 bits would reach the bias's gradient, which is fp32.
+//
+// The bias's gradient adds up ds by bucket, a scatter.  It is held as integers, so that their order does not matter and the same
+// inputs give the same bits: v = (hi 2^-17 + lo 2^-35) limit with |hi|, |lo| <= 2^17, two words of shared memory to a bucket, which
+// take 16,000 values before they are emptied into floats (short: the block's own partial sums) or 64-bit integers in global memory
+// (long).  limit is a power of two that bounds |ds|, from the first pass: |p dp| + |p D| <= max_j |p dp| + |D| max_j p, and at most four
+// times that.  A value is off by 2^-36 of the limit.  Integer additions in shared memory are also the fast ones here: 1.3 ns a warp,
+// fp32's 6 ns, 64-bit 11 ns.
+#pragma once
+#include "segment_forward.cuh"
+
+namespace dsvt_train {
+
+constexpr int kMaxPending = 16000;
+constexpr int kHiBits = 17, kLoBits = 18;
+constexpr float kMagic = 12582912.f;  // 1.5 x 2^23: adding it rounds to a whole number in the low bits
+
+// The context's workspace (the partition's bitmaps and ranks) in 32-bit words.
+constexpr size_t kPartialWords = (size_t)1 << 21, kTotalWords = 4 * (size_t)kMaxBiasTable;
+struct BackWork {
+  float* partial;               // [blocks][table]: the short ones' sums
+  unsigned long long* total;    // [2][table]: the long ones', hi and lo
+  uint32_t* spoilt;             // [table / 32] bits: a value that was not finite
+  uint32_t* bound;              // the long ones' largest |ds| may be, as a float's bits
+  float* stats;                 // [heads of a launch][n][3]
+  int32_t table, blocks, head0, head_end, n;  // (heads of a launch of the long ones)
+};
+
+// A value beyond the limit (which the two passes' roundings of large scores may leave there), or not finite.
+static __device__ __noinline__ void odd_value(int* at, uint32_t* spoilt, int entry, float v) {
+  if (isfinite(v)) atomicAdd(at, v > 0.f ? 1 << kHiBits : -(1 << kHiBits));
+  else atomicOr(spoilt + (entry >> 5), 1u << (entry & 31));
+}
+
+struct Tally {
+  int* hist;           // [heads][2][buckets]
+  uint32_t* spoilt;    // bits [heads][buckets]
+  int buckets;
+  float limit, to_hi;  // to_hi = 2^kHiBits / limit
+  bool on;
+  __device__ __forceinline__ void bound(float b) {
+    int e = (int)((__float_as_uint(b) >> 23) & 255) - 127 + 2;
+    e = min(max(e, -100), 126);
+    limit = __int_as_float((e + 127) << 23);
+    to_hi = __int_as_float((kHiBits - e + 127) << 23);
+  }
+  __device__ __forceinline__ void add(int h, int bucket, float v) const {
+    int* at = hist + 2 * h * buckets + bucket;
+    if (!(fabsf(v) <= limit)) { odd_value(at, spoilt, h * buckets + bucket, v); return; }
+    const float t = fmaf(v, to_hi, kMagic), r = fmaf(v, to_hi, -(t - kMagic)), u = fmaf(r, (float)(1 << kLoBits), kMagic);
+    atomicAdd(at, __float_as_int(t) - __float_as_int(kMagic));
+    atomicAdd(at + buckets, __float_as_int(u) - __float_as_int(kMagic));
+  }
+};
+
+// What the words stand for.
+__device__ __forceinline__ float tally_value(long long hi, long long lo, float limit) {
+  return (float)(((double)hi + (double)lo * (1.0 / (1 << kLoBits))) * (1.0 / (1 << kHiBits)) * (double)limit);
+}
+
+// Columns that hold no row: products of whatever lies there do not count.
+template <int NP>
+__device__ __forceinline__ void clear_columns(float (&c)[2 * NP][4], int pairs, uint64_t real) {
+#pragma unroll
+  for (int t = 0; t < 2 * NP; ++t)
+    if (t / 2 < pairs) {
+      const uint32_t bits = (uint32_t)(real >> (8 * t)) & 0xffu;
+      if (bits != 0xffu) {
+        const uint32_t mine = bits >> ((threadIdx.x & 3) * 2);
+        if (!(mine & 1)) c[t][0] = c[t][2] = 0.f;
+        if (!(mine & 2)) c[t][1] = c[t][3] = 0.f;
+      }
+    }
+}
+
+// A tile's two rows of the first pass: maximum and sum as in Flow, D and the largest |p dp| before they are divided by the sum.
+struct RowSums {
+  float m[2], l[2], d[2], most[2];
+  __device__ __forceinline__ void start() {
+    m[0] = m[1] = -INFINITY;
+    l[0] = l[1] = d[0] = d[1] = most[0] = most[1] = 0.f;
+  }
+};
+// (s: scores, then weights; dp: products of do and v)
+template <int NP>
+__device__ __forceinline__ void sum_rows(RowSums& f, float (&s)[2 * NP][4], const float (&dp)[2 * NP][4], int pairs) {
+#pragma unroll
+  for (int r = 0; r < 2; ++r) {
+    float m = f.m[r];
+#pragma unroll
+    for (int t = 0; t < 2 * NP; ++t)
+      if (t / 2 < pairs) m = fmaxf(m, fmaxf(s[t][2 * r], s[t][2 * r + 1]));
+    m = quad_max(m);
+    const float base = m == -INFINITY ? 0.f : m, fade = ex2_approx(f.m[r] - base);
+    f.m[r] = m;
+    float l = f.l[r] * fade, d = f.d[r] * fade, most = f.most[r] * fade;
+#pragma unroll
+    for (int t = 0; t < 2 * NP; ++t)
+      if (t / 2 < pairs)
+#pragma unroll
+        for (int e = 2 * r; e < 2 * r + 2; ++e) {
+          s[t][e] = ex2_approx(s[t][e] - base);
+          l += s[t][e];
+          const float x = s[t][e] * dp[t][e];
+          d += x;
+          most = fmaxf(most, fabsf(x));
+        }
+    f.l[r] = l; f.d[r] = d; f.most[r] = most;
+  }
+}
+// Row r's maximum, 1 / sum and D, and the bound of its |ds| (0 where it is not finite: such values are counted apart).
+__device__ __forceinline__ float3 row_stats(const RowSums& f, int r, float* bound) {
+  const float inv = inverse(quad_sum(f.l[r])), D = quad_sum(f.d[r]) * inv;
+  const float b = quad_max(f.most[r]) * inv + fabsf(D) * fminf(inv, 1.f);
+  *bound = b <= 3e38f ? b : 0.f;
+  return make_float3(f.m[r] == -INFINITY ? 0.f : f.m[r], inv, D);
+}
+
+// dz of the rows' chunk into dp, from weights relative to the maximum (calls without a cap).
+template <int NP>
+__device__ __forceinline__ void differ_weights(const float (&s)[2 * NP][4], float (&dp)[2 * NP][4], const float3 (&st)[2], int pairs) {
+#pragma unroll
+  for (int t = 0; t < 2 * NP; ++t)
+    if (t / 2 < pairs)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) dp[t][e] = s[t][e] * st[e >> 1].y * (dp[t][e] - st[e >> 1].z);
+}
+
+// The same from products, s = q k.
+template <int NP>
+__device__ __forceinline__ void differ_rows(float (&s)[2 * NP][4], float (&dp)[2 * NP][4], const Scoring& sc, const float* bias, const uint16_t* index, int pitch,
+                                            const float3 (&st)[2], int pairs, uint64_t real) {
+#pragma unroll
+  for (int t = 0; t < 2 * NP; ++t)
+    if (t / 2 < pairs) {
+      float slope[4];
+      score_tile<true>(s[t], slope, sc, bias, index + t * 8, pitch, (uint32_t)(real >> (8 * t)));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) dp[t][e] = ex2_approx(s[t][e] - st[e >> 1].x) * st[e >> 1].y * (dp[t][e] - st[e >> 1].z) * slope[e];
+    }
+}
+
+// The second pass's chunk: rows are keys, columns queries.  s: products k q -> p; dp: products v do -> dz.  `index`: buckets, at the first
+// row and column of the fragment (ROWS: [key][query], else [query][key]); `stats`: the columns' maximum, 1 / sum and D.
+template <int NP, bool ROWS>
+__device__ __forceinline__ void differ_columns(float (&s)[2 * NP][4], float (&dp)[2 * NP][4], const Scoring& sc, const float* bias, const uint16_t* index, int pitch,
+                                               const float4* stats, int pairs, uint64_t real, const Tally& tally, int h, bool count0, bool count1) {
+  const int g = (threadIdx.x & 31) >> 2, q2 = (threadIdx.x & 3) * 2;
+#pragma unroll
+  for (int t = 0; t < 2 * NP; ++t)
+    if (t / 2 < pairs) {
+      int bk[4] = {};
+      float b[4] = {}, slope[4];
+      if (sc.bias) {
+        if (ROWS) {
+          buckets_of(bk, index + t * 8, pitch);
+        } else {
+          const uint16_t* at = index + (t * 8 + q2) * pitch + g;
+          bk[0] = at[0]; bk[1] = at[pitch]; bk[2] = at[8]; bk[3] = at[pitch + 8];
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) b[e] = bias[bk[e]];
+      }
+      score_of<true>(sc, s[t], b, slope);
+      const float4 st[2] = {stats[t * 8 + q2], stats[t * 8 + q2 + 1]};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        s[t][e] = ex2_approx(s[t][e] - st[e & 1].x) * st[e & 1].y;
+        dp[t][e] = s[t][e] * (dp[t][e] - st[e & 1].z);
+      }
+      uint32_t mine = 3;
+      if (((uint32_t)(real >> (8 * t)) & 0xffu) != 0xffu) {  // columns without a query: whatever lies there
+        mine = (uint32_t)(real >> (8 * t)) >> q2;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (!((mine >> (e & 1)) & 1)) s[t][e] = dp[t][e] = slope[e] = 0.f;
+      }
+      if (tally.on)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (e < 2 ? count0 : count1) tally.add(h, bk[e], dp[t][e]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) dp[t][e] *= slope[e];
+    }
+}
+
+// Rows of an accumulator to global memory.
+template <typename T, int DT>
+__device__ __forceinline__ void store_rows(const float (&acc)[DT / 8][4], float scale, void* to, int64_t ld, int64_t col, int dim, int id0, int id1) {
+  T* at = (T*)to + col + (threadIdx.x & 3) * 2;
+#pragma unroll
+  for (int n = 0; n < DT / 8; ++n) {
+    if (!kExact<DT> && n * 8 >= dim) break;
+    if (id0 >= 0) store2<T>(at + id0 * ld + n * 8, acc[n][0] * scale, acc[n][1] * scale);
+    if (id1 >= 0) store2<T>(at + id1 * ld + n * 8, acc[n][2] * scale, acc[n][3] * scale);
+  }
+}
+
+template <int DT>
+__device__ __forceinline__ void clear(float (&acc)[DT / 8][4]) {
+#pragma unroll
+  for (int n = 0; n < DT / 8; ++n) acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.f;
+}
+
+template <typename T>
+constexpr bool kWide = std::is_same<T, __half>::value;
+
+// ---- short segments ------------------------------------------------------------------------------------------------
+struct BackLayout {
+  ShortLayout s;
+  uint32_t stats, hist, spoilt, bytes;
+};
+
+template <typename T, int DT>
+static BackLayout back_layout(const SegArgs& a, int limit) {
+  BackLayout l = {};
+  l.s = short_layout<T, DT>(a, limit, 4);
+  uint32_t at = l.s.bytes;
+  l.stats = at; at += l.s.heads * (kRowBlock + limit + 15) * 16;
+  if (a.dbias) {
+    l.hist = at; at += l.s.heads * 2 * a.buckets * 4;
+    l.spoilt = at; at += (l.s.heads * a.buckets + 31) / 32 * 4;
+  }
+  l.bytes = (at + 15) / 16 * 16;
+  return l;
+}
+
+template <typename T, int DT>
+__global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) short_backward_kernel(const __grid_constant__ SegArgs a, const BackLayout L, const Scoring sc, const BackWork work, int blocks) {
+  extern __shared__ __align__(16) unsigned char smem[];
+  constexpr int HG = kHeads<T, DT>, NP = sizeof(T) == 2 ? 3 : 2, NK = 2;  // pairs of 8 columns in registers, by queries and by keys
+  const int dim = kExact<DT> ? DT : a.dim;
+  __shared__ uint32_t block_bound;
+  pdl_enter();
+  Plan& plan = *reinterpret_cast<Plan*>(smem);
+  uint16_t* maps = reinterpret_cast<uint16_t*>(smem + L.s.maps);
+  float* bias = reinterpret_cast<float*>(smem + L.s.bias);
+  int4* cells = reinterpret_cast<int4*>(smem + L.s.cells);
+  uint16_t* index = reinterpret_cast<uint16_t*>(smem + L.s.index);
+  float4* stats = reinterpret_cast<float4*>(smem + L.stats);
+  const int stat_rows = kRowBlock + L.s.limit + 15;
+  const int head0 = blockIdx.y * HG, heads = min(HG, a.heads - head0);
+  const uint32_t pitch = kExact<DT> ? HG * DT * sizeof(T) + 16 : L.s.pitch;
+  const uint32_t q0 = smem_u32(smem + L.s.rows), k0 = q0 + L.s.array, v0 = k0 + L.s.array, o0 = v0 + L.s.array;
+  Tally tally;
+  tally.hist = reinterpret_cast<int*>(smem + L.hist);
+  tally.spoilt = reinterpret_cast<uint32_t*>(smem + L.spoilt);
+  tally.buckets = a.buckets;
+  tally.on = a.dbias != nullptr;
+  tally.bound(0.f);
+  stage_tables(a, maps, bias, head0, HG);
+  if (a.bias)
+    for (int i = threadIdx.x; i < (kRowBlock + 15 + L.s.limit) * L.s.pitch_idx / 2; i += kThreads) reinterpret_cast<uint32_t*>(index)[i] = 0;
+  float* mine = work.partial + (int64_t)blockIdx.x * work.table + head0 * a.buckets;
+  if (tally.on) {
+    for (int i = threadIdx.x; i < HG * 2 * a.buckets; i += kThreads) tally.hist[i] = 0;
+    for (int i = threadIdx.x; i < (HG * a.buckets + 31) / 32; i += kThreads) tally.spoilt[i] = 0;
+    // what the long segments' kernels add to starts at zero
+    const int first = (blockIdx.y * gridDim.x + blockIdx.x) * kThreads + threadIdx.x, step = gridDim.x * gridDim.y * kThreads;
+    for (int i = first; i < 2 * work.table; i += step) work.total[i] = 0;
+    for (int i = first; i < (work.table + 31) / 32; i += step) work.spoilt[i] = 0;
+    if (first == 0) *work.bound = 0;
+  }
+  bool emptied = false;
+  int pending = 0;
+  auto empty = [&]() {  // all threads; a barrier before and after
+    for (int i = threadIdx.x; i < heads * a.buckets; i += kThreads) {
+      const int h = i / a.buckets, at = 2 * h * a.buckets + i - h * a.buckets;
+      const float v = tally_value(tally.hist[at], tally.hist[at + a.buckets], tally.limit);
+      float sum = emptied ? mine[i] + v : v;
+      if (tally.spoilt[i >> 5] >> (i & 31) & 1) sum = NAN;
+      mine[i] = sum;
+      tally.hist[at] = tally.hist[at + a.buckets] = 0;
+    }
+    emptied = true;
+    pending = 0;
+  };
+  const int chunks = HG * dim * (int)sizeof(T) / 16, real = heads * dim * (int)sizeof(T) / 16;
+  const int64_t col = (int64_t)head0 * dim;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, h = warp % HG, g = lane >> 2;
+  const uint32_t at_head = h * dim * sizeof(T);
+  for (int block = blockIdx.x; block < blocks; block += gridDim.x) {
+    __syncthreads();
+    if (threadIdx.x == 0) block_bound = 0;
+    make_plan(a, plan, cells, block, blocks, L.s.limit);
+    if (plan.items == 0) continue;
+    load_rows<T>(q0, pitch, a.q, a.ld_q, plan.ids, plan.rows, col, chunks, real);
+    load_rows<T>(k0, pitch, a.k, a.ld_k, plan.ids, plan.rows, col, chunks, real);
+    load_rows<T>(v0, pitch, a.v, a.ld_v, plan.ids, plan.rows, col, chunks, real);
+    load_rows<T>(o0, pitch, a.d_out, a.ld_do, plan.ids, plan.rows, col, chunks, real);
+    cp_commit();
+    if (a.bias) fill_index(a, plan, cells, maps, index, L.s.pitch_idx);
+    cp_wait<0>();
+    __syncthreads();
+    if (h < heads) {
+      float most = 0.f;
+      for (int it = warp / HG; it < plan.items; it += kWarps / HG) {
+        const Item item = plan.item[it];
+        const int row = item.at + 16 * item.tile, r0 = 16 * item.tile + g;
+        RowSums f;
+        f.start();
+        float s[2 * NP][4], dp[2 * NP][4];
+        auto products = [&](int j, int pairs, uint64_t keys) {
+          const uint32_t at = (item.at + j) * pitch + at_head;
+          scores<T, DT, NP>(s, q0 + row * pitch + at_head, k0 + at, pitch, dim, pairs);
+          scores<T, DT, NP>(dp, o0 + row * pitch + at_head, v0 + at, pitch, dim, pairs);
+          clear_columns<NP>(dp, pairs, keys);
+        };
+        for (int j = 0; j < item.len; j += 16 * NP) {
+          const int cols = min(16 * NP, item.len - j), pairs = (cols + 15) >> 4;
+          const uint64_t keys = real_rows(plan, item.at + j, cols);
+          products(j, pairs, keys);
+          transform<NP>(s, sc, bias + h * a.buckets, index + row * L.s.pitch_idx + j, L.s.pitch_idx, pairs, keys);
+          sum_rows<NP>(f, s, dp, pairs);
+        }
+        float bound[2];
+        const float3 st[2] = {row_stats(f, 0, &bound[0]), row_stats(f, 1, &bound[1])};
+        const int id0 = r0 < item.len ? plan.ids[item.at + r0] : -1, id1 = r0 + 8 < item.len ? plan.ids[item.at + r0 + 8] : -1;
+        if (id0 >= 0) most = fmaxf(most, bound[0]);
+        if (id1 >= 0) most = fmaxf(most, bound[1]);
+        if ((lane & 3) == 0) {
+          float4* to = stats + h * stat_rows + row + g;
+          if (r0 < item.len) to[0] = make_float4(st[0].x, st[0].y, st[0].z, 0.f);
+          if (r0 + 8 < item.len) to[8] = make_float4(st[1].x, st[1].y, st[1].z, 0.f);
+        }
+        float acc[DT / 8][4];
+        clear<DT>(acc);
+        if (item.len <= 16 * NP && sc.cap == 0.f) {  // the weights are still there
+          const int pairs = (item.len + 15) >> 4;
+          differ_weights<NP>(s, dp, st, pairs);
+          weigh<T, DT, NP, kWide<T>>(acc, dp, k0 + item.at * pitch + at_head, pitch, dim, pairs, real_rows(plan, item.at, item.len));
+        } else {
+          for (int j = 0; j < item.len; j += 16 * NP) {
+            const int cols = min(16 * NP, item.len - j), pairs = (cols + 15) >> 4;
+            const uint64_t keys = real_rows(plan, item.at + j, cols);
+            products(j, pairs, keys);
+            differ_rows<NP>(s, dp, sc, bias + h * a.buckets, index + row * L.s.pitch_idx + j, L.s.pitch_idx, st, pairs, keys);
+            weigh<T, DT, NP, kWide<T>>(acc, dp, k0 + (item.at + j) * pitch + at_head, pitch, dim, pairs, keys);
+          }
+        }
+        store_rows<T, DT>(acc, a.scale, a.dq, a.ld_dq, col + h * dim, dim, id0, id1);
+      }
+      if (tally.on) {
+        for (int m = 16; m > 0; m >>= 1) most = fmaxf(most, __shfl_xor_sync(kAll, most, m));
+        if (lane == 0) atomicMax(&block_bound, __float_as_uint(most));
+      }
+    }
+    __syncthreads();
+    if (tally.on) {
+      const int pairs = plan.pairs;
+      const float b = __uint_as_float(block_bound);
+      if (2.f * b > tally.limit || pending + pairs > kMaxPending) {  // (a value of the second pass may round to more than the bound)
+        if (pending > 0) empty();
+        if (2.f * b > tally.limit) tally.bound(b);
+        __syncthreads();
+      }
+      pending += pairs;
+    }
+    if (h < heads) {
+      for (int it = warp / HG; it < plan.items; it += kWarps / HG) {
+        const Item item = plan.item[it];
+        const int row = item.at + 16 * item.tile, r0 = 16 * item.tile + g;
+        const int id0 = r0 < item.len ? plan.ids[item.at + r0] : -1, id1 = r0 + 8 < item.len ? plan.ids[item.at + r0 + 8] : -1;
+        float dk[DT / 8][4], dv[DT / 8][4];
+        clear<DT>(dk);
+        clear<DT>(dv);
+        for (int j = 0; j < item.len; j += 16 * NK) {
+          const int cols = min(16 * NK, item.len - j), pairs = (cols + 15) >> 4;
+          const uint64_t queries = real_rows(plan, item.at + j, cols);
+          const uint32_t at = (item.at + j) * pitch + at_head;
+          float s[2 * NK][4], dp[2 * NK][4];
+          scores<T, DT, NK>(s, k0 + row * pitch + at_head, q0 + at, pitch, dim, pairs);
+          scores<T, DT, NK>(dp, v0 + row * pitch + at_head, o0 + at, pitch, dim, pairs);
+          differ_columns<NK, false>(s, dp, sc, bias + h * a.buckets, index + (item.at + j) * L.s.pitch_idx + 16 * item.tile, L.s.pitch_idx,
+                                         stats + h * stat_rows + item.at + j, pairs, queries, tally, h, id0 >= 0, id1 >= 0);
+          weigh<T, DT, NK, kWide<T>>(dk, dp, q0 + at, pitch, dim, pairs, queries);
+          weigh<T, DT, NK, false>(dv, s, o0 + at, pitch, dim, pairs, queries);
+        }
+        store_rows<T, DT>(dk, a.scale, a.dk, a.ld_dk, col + h * dim, dim, id0, id1);
+        store_rows<T, DT>(dv, 1.f, a.dv, a.ld_dv, col + h * dim, dim, id0, id1);
+      }
+    }
+  }
+  if (tally.on) {
+    __syncthreads();
+    empty();
+  }
+}
+
+// ---- long segments -------------------------------------------------------------------------------------------------
+template <typename T, int DT>
+struct BackShape {
+  static constexpr int HG = kHeads<T, DT> < 4 ? kHeads<T, DT> : 4, WH = HG < 2 ? HG : 2, HPW = HG / WH, rows = 16 * kWarps / WH;
+  static constexpr int chunk = sizeof(T) == 2 ? 64 : DT <= 64 ? 32 : 16, NP = chunk < 32 ? 1 : 2;  // rows that pass at a time; of these in registers
+};
+
+struct BackLongLayout {
+  int pitch_idx;
+  uint32_t pitch, tile, chunk;
+  uint32_t maps, bias, cells, passing_cells, ids, index, stats, hist, spoilt, rows, passing, bytes;
+};
+
+template <typename T, int DT>
+static BackLongLayout back_long_layout(const SegArgs& a, bool by_keys) {
+  using S = BackShape<T, DT>;
+  BackLongLayout l = {};
+  l.pitch = (uint32_t)(S::HG * a.dim * sizeof(T) + 16);
+  l.tile = S::rows * l.pitch;
+  l.chunk = S::chunk * l.pitch;
+  uint32_t at = 0;
+  auto take = [&](size_t bytes) { const uint32_t was = at; at += (uint32_t)((bytes + 15) / 16 * 16); return was; };
+  l.ids = take((size_t)(S::rows + 3 * S::chunk) * 4);
+  if (a.bias) {
+    l.maps = take(sizeof(a.maps.of));
+    l.bias = take((size_t)S::HG * a.buckets * 4);
+    l.cells = take((size_t)S::rows * 16);
+    l.passing_cells = take((size_t)3 * S::chunk * 16);
+    l.pitch_idx = S::chunk + 8;
+    l.index = take((size_t)S::rows * l.pitch_idx * 2);
+  }
+  if (by_keys) {
+    l.stats = take((size_t)3 * S::HG * S::chunk * 16);
+    if (a.dbias) {
+      l.hist = take((size_t)S::HG * 2 * a.buckets * 4);
+      l.spoilt = take((size_t)(S::HG * a.buckets + 31) / 32 * 4);
+    }
+  }
+  l.rows = take((size_t)2 * l.tile + 64);
+  l.passing = take((size_t)4 * l.chunk + 64);
+  l.bytes = at;
+  return l;
+}
+
+// A tile of a long segment's queries (BY_KEYS: keys) against all of the segment's keys (queries).
+template <typename T, int DT, bool BY_KEYS>
+__global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) long_backward_kernel(const __grid_constant__ SegArgs a, const BackLongLayout L, const Scoring sc, const BackWork work, int above) {
+  extern __shared__ __align__(16) unsigned char smem[];
+  using S = BackShape<T, DT>;
+  constexpr int NP = S::NP, HPW = S::HPW;
+  __shared__ Tile tiles[kMaxTiles];
+  __shared__ int tile_count;
+  const int dim = kExact<DT> ? DT : a.dim;
+  pdl_enter();
+  const int found = find_tiles(a, tiles, &tile_count, blockIdx.x * S::rows, S::rows, above);
+  if (found == 0) return;
+  uint16_t* maps = reinterpret_cast<uint16_t*>(smem + L.maps);
+  float* bias = reinterpret_cast<float*>(smem + L.bias);
+  int4* cells = reinterpret_cast<int4*>(smem + L.cells);
+  uint16_t* index = reinterpret_cast<uint16_t*>(smem + L.index);
+  int32_t* ids = reinterpret_cast<int32_t*>(smem + L.ids);
+  const int head0 = work.head0 + blockIdx.y * S::HG, heads = min(S::HG, work.head_end - head0);
+  const uint32_t pitch = kExact<DT> ? S::HG * DT * sizeof(T) + 16 : L.pitch;
+  const uint32_t own0 = smem_u32(smem + L.rows), own1 = own0 + L.tile;
+  Tally tally;
+  tally.hist = reinterpret_cast<int*>(smem + L.hist);
+  tally.spoilt = reinterpret_cast<uint32_t*>(smem + L.spoilt);
+  tally.buckets = a.buckets;
+  tally.on = BY_KEYS && a.dbias != nullptr;
+  if (tally.on) {
+    tally.bound(__uint_as_float(*work.bound));
+    for (int i = threadIdx.x; i < S::HG * 2 * a.buckets; i += kThreads) tally.hist[i] = 0;
+    for (int i = threadIdx.x; i < (S::HG * a.buckets + 31) / 32; i += kThreads) tally.spoilt[i] = 0;
+  }
+  auto empty = [&]() {  // all threads; a barrier before and after
+    for (int i = threadIdx.x; i < heads * a.buckets; i += kThreads) {
+      const int h = i / a.buckets, at = 2 * h * a.buckets + i - h * a.buckets;
+      const long long hi = tally.hist[at], lo = tally.hist[at + a.buckets];
+      unsigned long long* to = work.total + head0 * a.buckets + i;
+      if (hi) atomicAdd(to, (unsigned long long)hi);
+      if (lo) atomicAdd(to + work.table, (unsigned long long)lo);
+      if (tally.spoilt[i >> 5] >> (i & 31) & 1) { const int w = head0 * a.buckets + i; atomicOr(work.spoilt + (w >> 5), 1u << (w & 31)); }
+      tally.hist[at] = tally.hist[at + a.buckets] = 0;
+    }
+  };
+  stage_tables(a, maps, bias, head0, S::HG);
+  const int chunks = S::HG * dim * (int)sizeof(T) / 16, real = heads * dim * (int)sizeof(T) / 16;
+  const int64_t col = (int64_t)head0 * dim;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2;
+  const int row = 16 * (warp / S::WH);
+  float most = 0.f;
+  for (int ti = 0; ti < found; ++ti) {
+    const Tile tile = tiles[ti];
+    const int rows = min(S::rows, tile.hi - tile.row);
+    const int parts = (tile.hi - tile.lo + S::chunk - 1) / S::chunk;
+    auto ids_of = [&](int c) { return ids + S::rows + c % 3 * S::chunk; };
+    auto cells_of = [&](int c) { return reinterpret_cast<int4*>(smem + L.passing_cells) + c % 3 * S::chunk; };
+    auto stats_of = [&](int c) { return reinterpret_cast<float4*>(smem + L.stats) + c % 3 * S::HG * S::chunk; };
+    auto array = [&](int c, int which) { return smem_u32(smem + L.passing) + ((c & 1) * 2 + which) * L.chunk; };
+    __syncthreads();  // (the tile before is done with the shared memory)
+    if (threadIdx.x < S::rows) {
+      const int id = (int)threadIdx.x < rows ? voxel_at(a, tile.row + threadIdx.x) : -1;
+      ids[threadIdx.x] = id;
+      if (a.bias) cells[threadIdx.x] = id >= 0 ? a.coords[id] : make_int4(0, 0, 0, 0);
+    }
+    int next = -1;  // this thread's voxel of the next chunk
+    auto fetch_id = [&](int c) {
+      const int at = tile.lo + c * S::chunk + (int)threadIdx.x;
+      next = threadIdx.x < S::chunk && at < tile.hi ? voxel_at(a, at) : -1;
+    };
+    auto publish = [&](int c) {
+      if (threadIdx.x < S::chunk) {
+        ids_of(c)[threadIdx.x] = next;
+        if (a.bias) cells_of(c)[threadIdx.x] = next >= 0 ? a.coords[next] : make_int4(0, 0, 0, 0);
+      }
+      if (BY_KEYS)
+        for (int i = threadIdx.x; i < heads * S::chunk; i += kThreads) {
+          const int h = i / S::chunk, j = i % S::chunk, at = tile.lo + c * S::chunk + j;
+          float4 st = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (at < tile.hi) {
+            const float* from = work.stats + ((int64_t)(head0 - work.head0 + h) * work.n + at) * 3;
+            st = make_float4(from[0], from[1], from[2], 0.f);
+          }
+          stats_of(c)[h * S::chunk + j] = st;
+        }
+    };
+    auto load = [&](int c) {
+      load_rows<T>(array(c, 0), pitch, BY_KEYS ? a.q : a.k, BY_KEYS ? a.ld_q : a.ld_k, ids_of(c), S::chunk, col, chunks, real);
+      load_rows<T>(array(c, 1), pitch, BY_KEYS ? a.d_out : a.v, BY_KEYS ? a.ld_do : a.ld_v, ids_of(c), S::chunk, col, chunks, real);
+      cp_commit();
+    };
+    RowSums f[BY_KEYS ? 1 : HPW];
+    float3 st[BY_KEYS ? 1 : HPW][2];
+    float acc[HPW][DT / 8][4], dv[BY_KEYS ? HPW : 1][DT / 8][4];
+#pragma unroll
+    for (int i = 0; i < HPW; ++i) {
+      if (!BY_KEYS) f[i].start();
+      clear<DT>(acc[i]);
+      if (BY_KEYS) clear<DT>(dv[i]);
+    }
+    int pending = 0;
+    for (int sweep = BY_KEYS ? 1 : 0; sweep < 2; ++sweep) {
+      fetch_id(0);
+      __syncthreads();
+      publish(0);
+      fetch_id(1);
+      __syncthreads();
+      if (BY_KEYS || sweep == 0) {
+        load_rows<T>(own0, pitch, BY_KEYS ? a.k : a.q, BY_KEYS ? a.ld_k : a.ld_q, ids, S::rows, col, chunks, real);
+        load_rows<T>(own1, pitch, BY_KEYS ? a.v : a.d_out, BY_KEYS ? a.ld_v : a.ld_do, ids, S::rows, col, chunks, real);
+      }
+      load(0);
+      for (int c = 0; c < parts; ++c) {
+        const int all = min(S::chunk, tile.hi - tile.lo - c * S::chunk);
+        if (c + 1 < parts) publish(c + 1);
+        cp_wait<0>();
+        __syncthreads();  // this chunk is there, the other one's buffer free
+        if (c + 1 < parts) {
+          load(c + 1);
+          fetch_id(c + 2);
+        }
+        if (tally.on && pending + S::rows * S::chunk > kMaxPending) {
+          empty();
+          pending = 0;  // (the barrier behind the buckets comes before the next addition)
+        }
+        pending += S::rows * S::chunk;
+        if (a.bias) {
+          for (int i = threadIdx.x; i < S::rows * S::chunk; i += kThreads) {
+            const int r = i / S::chunk, j = i % S::chunk;
+            index[r * L.pitch_idx + j] = (uint16_t)(BY_KEYS ? bucket_at(a.maps, maps, cells_of(c)[j], cells[r]) : bucket_at(a.maps, maps, cells[r], cells_of(c)[j]));
+          }
+          __syncthreads();
+        }
+        uint64_t there = __ballot_sync(kAll, lane < S::chunk && ids_of(c)[lane] >= 0);
+        if (S::chunk > 32) there |= (uint64_t)__ballot_sync(kAll, ids_of(c)[32 + lane] >= 0) << 32;
+#pragma unroll
+        for (int i = 0; i < HPW; ++i) {
+          const int h = (warp % S::WH) * HPW + i;
+          if (h >= heads || row >= rows) continue;
+          const uint32_t at_head = h * dim * sizeof(T);
+          for (int j = 0; j < all; j += 16 * NP) {
+            const int cols = min(16 * NP, all - j), pairs = (cols + 15) >> 4;
+            const uint64_t bits = there >> j & (((uint64_t)1 << (16 * NP)) - 1);
+            const uint32_t a0 = array(c, 0) + j * pitch + at_head, a1 = array(c, 1) + j * pitch + at_head;
+            float s[2 * NP][4], dp[2 * NP][4];
+            scores<T, DT, NP>(s, own0 + row * pitch + at_head, a0, pitch, dim, pairs);
+            scores<T, DT, NP>(dp, own1 + row * pitch + at_head, a1, pitch, dim, pairs);
+            const uint16_t* at = index + row * L.pitch_idx + j;
+            if constexpr (!BY_KEYS) {
+              clear_columns<NP>(dp, pairs, bits);
+              if (sweep == 0) {
+                transform<NP>(s, sc, bias + h * a.buckets, at, L.pitch_idx, pairs, bits);
+                sum_rows<NP>(f[i], s, dp, pairs);
+              } else {
+                differ_rows<NP>(s, dp, sc, bias + h * a.buckets, at, L.pitch_idx, st[i], pairs, bits);
+                weigh<T, DT, NP, kWide<T>>(acc[i], dp, a0, pitch, dim, pairs, bits);
+              }
+            } else {
+              differ_columns<NP, true>(s, dp, sc, bias + h * a.buckets, at, L.pitch_idx, stats_of(c) + h * S::chunk + j, pairs, bits, tally, h, ids[row + g] >= 0,
+                                            ids[row + g + 8] >= 0);
+              weigh<T, DT, NP, kWide<T>>(acc[i], dp, a0, pitch, dim, pairs, bits);
+              weigh<T, DT, NP, false>(dv[i], s, a1, pitch, dim, pairs, bits);
+            }
+          }
+        }
+      }
+      if (!BY_KEYS && sweep == 0) {
+#pragma unroll
+        for (int i = 0; i < HPW; ++i) {
+          const int h = (warp % S::WH) * HPW + i;
+          float bound[2];
+          st[i][0] = row_stats(f[i], 0, &bound[0]);
+          st[i][1] = row_stats(f[i], 1, &bound[1]);
+          if (h < heads && row < rows)
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+              if (ids[row + g + 8 * r] < 0) continue;
+              most = fmaxf(most, bound[r]);
+              if ((lane & 3) == 0) {
+                float* to = work.stats + ((int64_t)(head0 - work.head0 + h) * work.n + tile.row + row + g + 8 * r) * 3;
+                to[0] = st[i][r].x; to[1] = st[i][r].y; to[2] = st[i][r].z;
+              }
+            }
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < HPW; ++i) {
+      const int h = (warp % S::WH) * HPW + i;
+      if (h >= heads || row >= rows) continue;
+      const int id0 = ids[row + g], id1 = ids[row + g + 8];
+      store_rows<T, DT>(acc[i], a.scale, BY_KEYS ? a.dk : a.dq, BY_KEYS ? a.ld_dk : a.ld_dq, col + h * dim, dim, id0, id1);
+      if (BY_KEYS) store_rows<T, DT>(dv[i], 1.f, a.dv, a.ld_dv, col + h * dim, dim, id0, id1);
+    }
+    if (tally.on) {
+      __syncthreads();
+      empty();
+    }
+  }
+  if (!BY_KEYS && a.dbias) {
+    for (int m = 16; m > 0; m >>= 1) most = fmaxf(most, __shfl_xor_sync(kAll, most, m));
+    if (lane == 0 && most > 0.f) atomicMax(work.bound, __float_as_uint(most));
+  }
+}
+
+// dbias: the blocks' partial sums in a fixed order, and the long segments' integers.  32 entries to a block, a warp a share of the blocks.
+static __global__ void __launch_bounds__(kThreads) bias_grad_kernel(const BackWork work, bool longer, float* dbias) {
+  __shared__ float part[kWarps][32];
+  pdl_enter();
+  const int at = blockIdx.x * 32 + (threadIdx.x & 31), warp = threadIdx.x >> 5;
+  float s = 0.f;
+  if (at < work.table)
+#pragma unroll 4
+    for (int p = warp; p < work.blocks; p += kWarps) s += work.partial[(int64_t)p * work.table + at];
+  part[warp][threadIdx.x & 31] = s;
+  __syncthreads();
+  if (warp != 0 || at >= work.table) return;
+  for (int i = 1; i < kWarps; ++i) s += part[i][threadIdx.x];
+  if (longer) {
+    Tally t;
+    t.bound(__uint_as_float(*work.bound));
+    s += tally_value((long long)work.total[at], (long long)work.total[at + work.table], t.limit);
+    if (work.spoilt[at >> 5] >> (at & 31) & 1) s = NAN;
+  }
+  dbias[at] = s;
+}
+
+template <typename T, int DT>
+int backward_of(dsvt_ctx* ctx, const SegArgs& a) {
+  int limit = a.max_len <= kShort ? a.max_len : 64;
+  BackLayout l = back_layout<T, DT>(a, limit);
+  while (l.bytes > kSmemMost) l = back_layout<T, DT>(a, limit = limit > 64 ? 64 : limit / 2);
+  const Scoring sc = scoring_of(a);
+  const int groups = (int)dsvt_ceil_div(a.heads, kHeads<T, DT>), blocks = (int)dsvt_ceil_div(a.n, kRowBlock);
+  BackWork w = {};
+  uint32_t* base = reinterpret_cast<uint32_t*>(ctx->bm_zero);
+  w.partial = reinterpret_cast<float*>(base);
+  w.total = reinterpret_cast<unsigned long long*>(base + kPartialWords);
+  w.spoilt = base + kPartialWords + kTotalWords;
+  w.bound = w.spoilt + kMaxBiasTable / 32;
+  w.stats = reinterpret_cast<float*>(w.bound + 64);
+  const int64_t stat_words = (int64_t)(4 * ctx->bm_words) - (w.stats - reinterpret_cast<float*>(base));
+  w.table = a.dbias ? a.heads * a.buckets : 0;
+  w.n = a.n;
+  // blocks that stay: two to an SM where they fit, and as many as have room for their partial sums
+  const int per_sm = DT <= 32 && l.bytes <= kSmemMost / 2 ? 2 : 1;
+  int64_t stay = dsvt_ceil_div(per_sm * ctx->sm_count, groups);
+  if (w.table > 0 && stay > (int64_t)kPartialWords / w.table) stay = kPartialWords / w.table;
+  if (stay > blocks) stay = blocks;
+  w.blocks = (int)stay;
+  auto kernel = short_backward_kernel<T, DT>;
+  int rc = allow_smem(ctx, kernel, l.bytes);
+  if (rc != DSVT_OK) return rc;
+  launch_pdl(kernel, dim3((unsigned)stay, groups), dim3(kThreads), l.bytes, ctx->stream, a, l, sc, w, blocks);
+  DSVT_LAUNCHED(ctx);
+  const bool longer = limit < a.max_len;
+  if (longer) {
+    using S = BackShape<T, DT>;
+    const BackLongLayout lq = back_long_layout<T, DT>(a, false), lk = back_long_layout<T, DT>(a, true);
+    auto by_queries = long_backward_kernel<T, DT, false>;
+    auto by_keys = long_backward_kernel<T, DT, true>;
+    if ((rc = allow_smem(ctx, by_queries, lq.bytes)) != DSVT_OK || (rc = allow_smem(ctx, by_keys, lk.bytes)) != DSVT_OK) return rc;
+    // as many heads to a launch as the workspace has room for the statistics of, whole blocks' if it can be
+    int64_t at_once = stat_words / ((int64_t)3 * a.n);
+    if (at_once < 1) return DSVT_ERR_CAPACITY;
+    if (at_once > S::HG) at_once = at_once / S::HG * S::HG;
+    for (int h = 0; h < a.heads; h += (int)at_once) {
+      w.head0 = h;
+      w.head_end = (int)(h + at_once < a.heads ? h + at_once : a.heads);
+      const dim3 grid((unsigned)dsvt_ceil_div(a.n, S::rows), (unsigned)dsvt_ceil_div(w.head_end - h, S::HG));
+      launch_pdl(by_queries, grid, dim3(kThreads), lq.bytes, ctx->stream, a, lq, sc, w, limit);
+      DSVT_LAUNCHED(ctx);
+      launch_pdl(by_keys, grid, dim3(kThreads), lk.bytes, ctx->stream, a, lk, sc, w, limit);
+      DSVT_LAUNCHED(ctx);
+    }
+  }
+  if (a.dbias) {
+    launch_pdl(bias_grad_kernel, dim3((unsigned)dsvt_ceil_div(w.table, 32)), dim3(kThreads), 0, ctx->stream, w, longer, a.dbias);
+    DSVT_LAUNCHED(ctx);
+  }
+  return DSVT_OK;
+}
+
+template <typename T>
+int launch_backward(dsvt_ctx* ctx, const SegArgs& a) {
+  if (a.dim == 16) return backward_of<T, 16>(ctx, a);
+  if (a.dim == 24) return backward_of<T, 24>(ctx, a);
+  if (a.dim == 32) return backward_of<T, 32>(ctx, a);
+  if (a.dim <= 64) return backward_of<T, 64>(ctx, a);
+  return backward_of<T, 128>(ctx, a);
+}
+
+}  // namespace dsvt_train

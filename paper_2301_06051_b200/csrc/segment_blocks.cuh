@@ -15,7 +15,7 @@ constexpr int kMaxItems = kRowBlock * (kShort / 16);
 struct Item { uint8_t at, len, tile, pad; };
 
 struct Plan {
-  int rows, items;
+  int rows, items, pairs;  // (pairs: of queries and keys)
   uint32_t starts;                        // bit i: a segment starts at place i
   uint8_t len_at[kRowBlock];
   uint32_t real[(kMaxRows + 31) / 32 + 3];  // bit i: place i holds a voxel
@@ -73,15 +73,16 @@ __device__ __forceinline__ void make_plan(const SegArgs& a, Plan& p, int4* cells
   if (warp == 0) {
     const int len = p.len_at[lane], tiles = (len + 15) >> 4;
     const uint32_t starts = __ballot_sync(kAll, len > 0);
-    int rows = len > 0 ? lane + len : 0, upto = tiles;
+    int rows = len > 0 ? lane + len : 0, upto = tiles, pairs = len * len;
     for (int m = 1; m < 32; m <<= 1) {
       rows = max(rows, __shfl_xor_sync(kAll, rows, m));
+      pairs += __shfl_xor_sync(kAll, pairs, m);
       const int before = __shfl_up_sync(kAll, upto, m);
       if (lane >= m) upto += before;
     }
     for (int t = 0; t < tiles; ++t) p.item[upto - tiles + t] = Item{(uint8_t)lane, (uint8_t)len, (uint8_t)t, 0};
     if (lane == 31) p.items = upto;
-    if (lane == 0) { p.rows = rows; p.starts = starts; }
+    if (lane == 0) { p.rows = rows; p.pairs = pairs; p.starts = starts; }
   }
   __syncthreads();
   const int rows = p.rows;
@@ -145,30 +146,45 @@ __device__ __forceinline__ void store2(T* to, float x, float y) {
   else *reinterpret_cast<uint32_t*>(to) = Mma<T>::pack(x, y);
 }
 
-// Scores of queries (rows) and keys (columns) in units of log 2, from products: scale, cap, bias; -inf where a column holds no key.
+// The buckets of a tile's four pairs; `index`: at its first row and column.
+__device__ __forceinline__ void buckets_of(int (&bk)[4], const uint16_t* index, int pitch) {
+  const int lane = threadIdx.x & 31;
+  const uint16_t* at = index + (lane >> 2) * pitch + (lane & 3) * 2;
+  const uint32_t i0 = *reinterpret_cast<const uint32_t*>(at), i1 = *reinterpret_cast<const uint32_t*>(at + 8 * pitch);
+  bk[0] = i0 & 0xffff; bk[1] = i0 >> 16; bk[2] = i1 & 0xffff; bk[3] = i1 >> 16;
+}
+
+// A tile of scores of queries (rows) and keys (columns) from products; -inf where a column holds no key.
+template <bool SLOPE>
+__device__ __forceinline__ void score_tile(float (&s)[4], float (&slope)[4], const Scoring& sc, const float* bias, const uint16_t* index, int pitch, uint32_t bits) {
+  float b[4] = {};
+  if (sc.bias) {
+    int bk[4];
+    buckets_of(bk, index, pitch);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) b[e] = bias[bk[e]];
+  }
+  score_of<SLOPE>(sc, s, b, slope);
+  if ((bits & 0xffu) != 0xffu) {
+    const uint32_t mine = bits >> ((threadIdx.x & 3) * 2);
+    if (!(mine & 1)) {
+      s[0] = s[2] = -INFINITY;
+      if (SLOPE) slope[0] = slope[2] = 0.f;
+    }
+    if (!(mine & 2)) {
+      s[1] = s[3] = -INFINITY;
+      if (SLOPE) slope[1] = slope[3] = 0.f;
+    }
+  }
+}
+
 // `index`: the fragment's first row's buckets at the chunk's first column (rows g and g + 8 of the tile).
-template <int NP, bool CAP>
-__device__ __forceinline__ void transform(float (&s)[2 * NP][4], float (&slope)[CAP ? 2 * NP : 1][4], const Scoring& sc, const float* bias,
-                                          const uint16_t* index, int pitch, int pairs, uint64_t real) {
-  const int lane = threadIdx.x & 31, q2 = (lane & 3) * 2;
+template <int NP>
+__device__ __forceinline__ void transform(float (&s)[2 * NP][4], const Scoring& sc, const float* bias, const uint16_t* index, int pitch, int pairs, uint64_t real) {
+  float none[4];
 #pragma unroll
   for (int t = 0; t < 2 * NP; ++t)
-    if (t / 2 < pairs) {
-      float b[4] = {};
-      if (sc.bias) {
-        const uint32_t i0 = *reinterpret_cast<const uint32_t*>(index + (lane >> 2) * pitch + t * 8 + q2);
-        const uint32_t i1 = *reinterpret_cast<const uint32_t*>(index + ((lane >> 2) + 8) * pitch + t * 8 + q2);
-        b[0] = bias[i0 & 0xffff]; b[1] = bias[i0 >> 16]; b[2] = bias[i1 & 0xffff]; b[3] = bias[i1 >> 16];
-      }
-#pragma unroll
-      for (int e = 0; e < 4; ++e) s[t][e] = score_of<CAP>(sc, s[t][e], b[e], &slope[CAP ? t : 0][e]);
-      const uint32_t bits = (uint32_t)(real >> (8 * t)) & 0xffu;
-      if (bits != 0xffu) {
-        const uint32_t mine = bits >> q2;
-        if (!(mine & 1)) s[t][0] = s[t][2] = -INFINITY;
-        if (!(mine & 2)) s[t][1] = s[t][3] = -INFINITY;
-      }
-    }
+    if (t / 2 < pairs) score_tile<false>(s[t], none, sc, bias, index + t * 8, pitch, (uint32_t)(real >> (8 * t)));
 }
 
 __device__ __forceinline__ float quad_max(float v) {
@@ -225,7 +241,7 @@ __device__ __forceinline__ void soften(Flow<DT>& f, float (&s)[2 * NP][4], int p
 
 // ---- long segments ---------------------------------------------------------------------------------------------------
 struct Tile { int lo, hi, row; };  // a segment and the first row of a tile of it
-constexpr int kMaxTiles = 4;       // tiles that start in one block's rows (segments of more than 64 rows: at most 3)
+constexpr int kMaxTiles = 8;       // tiles that start in one block's rows (at most 128, of segments of more than 24 rows)
 
 // The tiles of `tile` rows of segments longer than `above` that start in rows [base, base + tile).
 __device__ __forceinline__ int find_tiles(const SegArgs& a, Tile* tiles, int* count, int base, int tile, int above) {

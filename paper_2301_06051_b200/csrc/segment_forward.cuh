@@ -34,7 +34,7 @@ static ShortLayout short_layout(const SegArgs& a, int limit, int arrays) {
   return l;
 }
 
-template <typename T, int DT, bool CAP>
+template <typename T, int DT>
 __global__ void __launch_bounds__(kThreads) short_forward_kernel(const __grid_constant__ SegArgs a, const ShortLayout L, const Scoring sc) {
   extern __shared__ __align__(16) unsigned char smem[];
   constexpr int HG = kHeads<T, DT>, NP = kPairs<T>;
@@ -74,9 +74,9 @@ __global__ void __launch_bounds__(kThreads) short_forward_kernel(const __grid_co
         const int cols = min(16 * NP, item.len - j), pairs = (cols + 15) >> 4;
         const uint64_t keys = real_rows(plan, item.at + j, cols);
         const uint32_t at = (item.at + j) * pitch + at_head;
-        float s[2 * NP][4], none[CAP ? 2 * NP : 1][4];
+        float s[2 * NP][4];
         scores<T, DT, NP>(s, qa, k0 + at, pitch, dim, pairs);
-        transform<NP, CAP>(s, none, sc, bias + h * a.buckets, index + row * L.pitch_idx + j, L.pitch_idx, pairs, keys);
+        transform<NP>(s, sc, bias + h * a.buckets, index + row * L.pitch_idx + j, L.pitch_idx, pairs, keys);
         soften<DT, NP>(f, s, pairs);
         weigh<T, DT, NP, false>(f.acc, s, v0 + at, pitch, dim, pairs, keys);
       }
@@ -156,7 +156,7 @@ struct Passing {
   }
 };
 
-template <typename T, int DT, bool CAP>
+template <typename T, int DT>
 __global__ void __launch_bounds__(kThreads) long_forward_kernel(const __grid_constant__ SegArgs a, const LongLayout L, const Scoring sc, int above) {
   extern __shared__ __align__(16) unsigned char smem[];
   using S = LongShape<T, DT>;
@@ -239,9 +239,9 @@ __global__ void __launch_bounds__(kThreads) long_forward_kernel(const __grid_con
         const int h = (warp % S::WH) * S::HPW + i;
         if (h < heads && row < rows) {
           const uint32_t at_head = h * dim * sizeof(T);
-          float s[2 * NP][4], none[CAP ? 2 * NP : 1][4];
+          float s[2 * NP][4];
           scores<T, DT, NP>(s, q0 + row * pitch + at_head, pass.array(c, 0, 2) + at_head, pitch, dim, pairs);
-          transform<NP, CAP>(s, none, sc, bias + h * a.buckets, index + row * L.pitch_idx, L.pitch_idx, pairs, keys);
+          transform<NP>(s, sc, bias + h * a.buckets, index + row * L.pitch_idx, L.pitch_idx, pairs, keys);
           soften<DT, NP>(f[i], s, pairs);
           weigh<T, DT, NP, false>(f[i].acc, s, pass.array(c, 1, 2) + at_head, pitch, dim, pairs, keys);
         }
@@ -274,14 +274,14 @@ static int allow_smem(dsvt_ctx* ctx, K kernel, uint32_t bytes) {
   return DSVT_OK;
 }
 
-template <typename T, int DT, bool CAP>
+template <typename T, int DT>
 int forward_of(dsvt_ctx* ctx, const SegArgs& a) {
   int limit = a.max_len <= kShort ? a.max_len : 64;
   ShortLayout l = short_layout<T, DT>(a, limit, 3);
   if (l.bytes > kSmemMost) l = short_layout<T, DT>(a, limit = 64, 3);
   const Scoring sc = scoring_of(a);
   const unsigned groups = (unsigned)dsvt_ceil_div(a.heads, kHeads<T, DT>);
-  auto kernel = short_forward_kernel<T, DT, CAP>;
+  auto kernel = short_forward_kernel<T, DT>;
   int rc = allow_smem(ctx, kernel, l.bytes);
   if (rc != DSVT_OK) return rc;
   launch_pdl(kernel, dim3((unsigned)dsvt_ceil_div(a.n, kRowBlock), groups), dim3(kThreads), l.bytes, ctx->stream, a, l, sc);
@@ -289,7 +289,7 @@ int forward_of(dsvt_ctx* ctx, const SegArgs& a) {
   if (limit >= a.max_len) return DSVT_OK;
   using S = LongShape<T, DT>;
   const LongLayout g = long_layout<T, DT>(a, 1, 2, 0);
-  auto longer = long_forward_kernel<T, DT, CAP>;
+  auto longer = long_forward_kernel<T, DT>;
   rc = allow_smem(ctx, longer, g.bytes);
   if (rc != DSVT_OK) return rc;
   launch_pdl(longer, dim3((unsigned)dsvt_ceil_div(a.n, S::rows), groups), dim3(kThreads), g.bytes, ctx->stream, a, g, sc, limit);
@@ -299,13 +299,11 @@ int forward_of(dsvt_ctx* ctx, const SegArgs& a) {
 
 template <typename T>
 int launch_forward(dsvt_ctx* ctx, const SegArgs& a) {
-#define DSVT_FORWARD(DT) return a.cap > 0.f ? forward_of<T, DT, true>(ctx, a) : forward_of<T, DT, false>(ctx, a)
-  if (a.dim == 16) DSVT_FORWARD(16);
-  if (a.dim == 24) DSVT_FORWARD(24);
-  if (a.dim == 32) DSVT_FORWARD(32);
-  if (a.dim <= 64) DSVT_FORWARD(64);
-  DSVT_FORWARD(128);
-#undef DSVT_FORWARD
+  if (a.dim == 16) return forward_of<T, 16>(ctx, a);
+  if (a.dim == 24) return forward_of<T, 24>(ctx, a);
+  if (a.dim == 32) return forward_of<T, 32>(ctx, a);
+  if (a.dim <= 64) return forward_of<T, 64>(ctx, a);
+  return forward_of<T, 128>(ctx, a);
 }
 
 }  // namespace dsvt_train

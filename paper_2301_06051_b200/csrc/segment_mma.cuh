@@ -258,8 +258,8 @@ __device__ __forceinline__ void weigh(float (&acc)[DT / 8][4], const float (&w)[
 
 // The scores' transformation: products -> scale, cap, bias, in units of log 2.
 struct Scoring {
-  float scale;   // CAP: of the product to tanh's argument; else to units of log 2
-  float cap;     // cap in units of log 2
+  float scale;   // of the product, to tanh's argument with a cap, else to units of log 2
+  float cap;     // in units of log 2, or 0
   bool bias;
 };
 static inline Scoring scoring_of(const SegArgs& a) {
@@ -269,15 +269,38 @@ static inline Scoring scoring_of(const SegArgs& a) {
   s.bias = a.bias != nullptr;
   return s;
 }
+// tanh without a branch, off by 3e-7 of the value at most: near 0 the first five terms of its series (the next one is 1e-8 of the value at
+// 1/4), else (1 - e) / (1 + e) with e = exp(-2 |x|).
+__device__ __forceinline__ float tanh_of(float x) {
+  const float y = x * x, a = fabsf(x);
+  float near = fmaf(y, 62.f / 2835.f, -17.f / 315.f);
+  near = fmaf(y, near, 2.f / 15.f);
+  near = fmaf(y, near, -1.f / 3.f);
+  near = fmaf(y * near, x, x);
+  const float e = ex2_approx(a * (-2.f * kLog2e));
+  const float far = copysignf(__fdividef(1.f - e, 1.f + e), x);
+  return a < 0.25f ? near : far;  // (NaN: far)
+}
 // A bias entry in units of log 2.  (Clamped: the lowest float stays the lowest, whatever is added, and differences of two are zero.)
 __device__ __forceinline__ float bias_log2(float b) { return b == -INFINITY ? b : fmaxf(b * kLog2e, -3.402823466e38f); }
 
-template <bool CAP>
-__device__ __forceinline__ float score_of(const Scoring& s, float z, float bias, float* slope) {
-  if (!CAP) return fmaf(z, s.scale, bias);
-  const float t = tanhf(z * s.scale);
-  *slope = fmaf(-t, t, 1.f);
-  return fmaf(t, s.cap, bias);
+// A tile's four scores; with `slope`, the derivative of the cap too.
+template <bool SLOPE>
+__device__ __forceinline__ void score_of(const Scoring& s, float (&z)[4], const float (&bias)[4], float (&slope)[4]) {
+  if (s.cap == 0.f) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      z[e] = fmaf(z[e], s.scale, bias[e]);
+      if (SLOPE) slope[e] = 1.f;
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float t = tanh_of(z[e] * s.scale);
+      if (SLOPE) slope[e] = fmaf(-t, t, 1.f);
+      z[e] = fmaf(t, s.cap, bias[e]);
+    }
+  }
 }
 
 // ---- loading -------------------------------------------------------------------------------------------------------

@@ -243,6 +243,89 @@ def test_nothing_to_do(ctx):
     assert ctx.status_sync() == 0
 
 
+def test_same_inputs_same_bits(ctx):
+    p = Problem([36, 20, 200, 1, 50, 300], 8, 24, torch.bfloat16, seed=8)
+    first = [t.clone() for t in p.backward(ctx)]
+    p.forward(ctx)
+    for _ in range(3):
+        assert all(torch.equal(a, b) for a, b in zip(p.backward(ctx), first))
+    x = torch.randn((5000, 192), device="cuda")
+    first = [t.clone() for t in ctx.layer_norm_backward(x, x, None)]
+    assert all(torch.equal(a, b) for a, b in zip(ctx.layer_norm_backward(x, x, None), first))
+
+
+def test_strides_beyond_32_bits(ctx):
+    """Rows so far apart that their offsets pass 2^31 elements."""
+    n, ld = 260, 9000000
+    big = torch.empty((n - 1) * ld + 2 * 16, dtype=torch.bfloat16, device="cuda")
+    far = lambda: big.as_strided((n, 2, 16), (ld, 16, 1))
+    p = Problem([n - 40, 40], 2, 16, torch.bfloat16, seed=4, packed=False)
+    plain = p.forward(ctx).clone()
+    grads = [g.clone() for g in p.backward(ctx)]
+    assert (n - 1) * ld > 2 ** 31
+    for name in ("q", "k", "v"):
+        was = getattr(p, name)
+        far().copy_(was)
+        setattr(p, name, far())
+        assert torch.equal(p.forward(ctx), plain)
+        assert all(torch.equal(a, b) for a, b in zip(p.backward(ctx), grads))
+        setattr(p, name, was)
+    p.forward(ctx, far())
+    assert torch.equal(far().contiguous(), plain)
+    small = [torch.empty_like(plain) for _ in range(3)]
+    for i in range(3):
+        p.backward(ctx, small[:i] + [far()] + small[i + 1:])
+        assert torch.equal(far().contiguous(), grads[i])
+    far().copy_(p.do)
+    p.do = far()
+    assert all(torch.equal(a, b) for a, b in zip(p.backward(ctx), grads))
+
+
+def test_a_context_on_its_own_stream_and_captured_graphs():
+    """Calls on a context whose stream is not the current one, captured and replayed with new inputs."""
+    stream = torch.cuda.Stream()
+    own = api.Context(2000, 64, 256, stream=stream)
+    p = Problem([36, 20, 200, 1, 50], 8, 24, torch.bfloat16, seed=8, packed=False)
+    x = torch.randn((307, 192), device="cuda")
+    g, b = torch.randn(192, device="cuda"), torch.randn(192, device="cuda")
+    out, y = torch.zeros_like(p.do), torch.zeros_like(x)
+    grads = [torch.zeros_like(p.do) for _ in range(3)]
+    dbias, dx, dg, db = torch.zeros_like(p.rel.table), torch.zeros_like(x), torch.zeros_like(g), torch.zeros_like(b)
+
+    def step():
+        own.segment_attention(p.q, p.k, p.v, p.seg, bias=p.rel, out=out)
+        own.segment_attention_backward(p.q, p.k, p.v, p.do, p.seg, bias=p.rel, out=grads, dbias=dbias)
+        own.layer_norm(x, g, b, out=y)
+        own.layer_norm_backward(x, y, g, out=dx, dg=dg, db=db)
+
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        step()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        step()
+    results = []
+    for seed in (1, 2):
+        gen = torch.Generator("cuda").manual_seed(seed)
+        for t in (p.q, p.k, p.v, p.do, x):
+            t.copy_(torch.randn(t.shape, generator=gen, device="cuda"))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        replayed = [t.clone() for t in (out, *grads, dbias, y, dx, dg, db)]
+        for t in (out, *grads, dbias, y, dx, dg, db):
+            t.zero_()
+        torch.cuda.synchronize()
+        step()
+        stream.synchronize()
+        assert all(torch.equal(a, c) for a, c in zip(replayed, (out, *grads, dbias, y, dx, dg, db)))
+        results.append(replayed)
+    assert not torch.equal(results[0][0], results[1][0])
+    assert own.status_sync() == 0
+    del graph
+    own.close()
+
+
 def test_refusals(ctx):
     lib, h = ctx.lib, ctx._h
     p = Problem([5, 6], 2, 16, torch.bfloat16, seed=1, packed=False)

@@ -34,8 +34,11 @@ def attention(q, k, v, segments, scale, cap=0.0, bias=None, buckets=None, d_out=
     tol = {m: torch.zeros_like(val[m]) for m in names}
     if back and bias is not None:
         val["dbias"], tol["dbias"] = torch.zeros_like(bias), torch.zeros_like(bias)
+        most, counts = 0.0, torch.zeros(bias.shape[1], dtype=torch.float64, device=device)
     covered = torch.zeros(n, dtype=torch.bool)
     low = -float(np.finfo(np.float32).max)
+    # float16 weights below 2^-14 are multiples of 2^-24, off by half of that whatever their size
+    low_weight = 2.0 ** -25 if eps == 2.0 ** -10 else 0.0
     for ids in segments:
         if len(ids) == 0:
             continue
@@ -69,7 +72,7 @@ def attention(q, k, v, segments, scale, cap=0.0, bias=None, buckets=None, d_out=
         if not back:
             o, oa = p @ c, p @ c.abs()
             val["out"][rows] = o.transpose(0, 1)
-            tol["out"][rows] = ((r + eps / 2 + (L + 8) * U) * oa * (1 + eps) + eps / 2 * o.abs()).transpose(0, 1)
+            tol["out"][rows] = ((r + eps / 2 + (L + 8) * U) * oa * (1 + eps) + eps / 2 * o.abs() + low_weight * c.abs().sum(1, keepdim=True)).transpose(0, 1)
             continue
         do = d_out.to(device)[rows].transpose(0, 1)
         dp = do @ c.transpose(1, 2)
@@ -82,6 +85,9 @@ def attention(q, k, v, segments, scale, cap=0.0, bias=None, buckets=None, d_out=
             flat = w.reshape(-1)
             val["dbias"].index_add_(1, flat, ds.reshape(heads, -1))
             tol["dbias"].index_add_(1, flat, (dse + 64 * U * ds.abs()).reshape(heads, -1))
+            # the header: multiples of 2^-33 of the call's largest bound, each value off by half of one
+            most = max(most, float(((p * dp).abs().amax(2, keepdim=True) + D.abs() * p.amax(2, keepdim=True)).max()))
+            counts.index_add_(0, flat, torch.ones_like(flat, dtype=torch.float64))
         slope = 1 - t * t if cap > 0 else torch.ones_like(ds)
         dz = ds * slope * scale
         # (the slope's own error: t's, doubled)
@@ -91,11 +97,13 @@ def attention(q, k, v, segments, scale, cap=0.0, bias=None, buckets=None, d_out=
             g = w1 @ other
             ga = w1e @ other.abs() + (L + 8) * U * (w1.abs() @ other.abs())
             val[name][rows] = g.transpose(0, 1)
+            if name == "dv":
+                ga = ga + low_weight * other.abs().sum(1, keepdim=True)
             tol[name][rows] = (ga * (1 + eps) + eps / 2 * g.abs()).transpose(0, 1)
     # results below the type's normal range round to multiples of its smallest step
     floor = {0.0: 1e-37}.get(eps, 2.0 ** -24 if eps == 2.0 ** -10 else 1e-37)
     if "dbias" in tol:
-        tol["dbias"] = tol["dbias"] + 2 * L_SUM * val["dbias"].abs()
+        tol["dbias"] = tol["dbias"] + 2 * L_SUM * val["dbias"].abs() + 2.0 ** -34 * most * counts
     return {m: (val[m].cpu(), tol[m].cpu() + (floor if m != "dbias" else 1e-37)) for m in val}, covered
 
 
