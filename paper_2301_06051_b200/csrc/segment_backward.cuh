@@ -50,9 +50,10 @@ struct Tally {
     limit = __int_as_float((e + 127) << 23);
     to_hi = __int_as_float((kHiBits - e + 127) << 23);
   }
-  __device__ __forceinline__ void add(int h, int bucket, float v) const {
-    int* at = hist + 2 * h * buckets + bucket;
-    if (!(fabsf(v) <= limit)) { odd_value(at, spoilt, h * buckets + bucket, v); return; }
+  // (bk: the bucket times 4)
+  __device__ __forceinline__ void add(int h, int bk, float v) const {
+    int* at = reinterpret_cast<int*>(reinterpret_cast<char*>(hist + 2 * h * buckets) + bk);
+    if (!(fabsf(v) <= limit)) { odd_value(at, spoilt, h * buckets + (bk >> 2), v); return; }
     const float t = fmaf(v, to_hi, kMagic), r = fmaf(v, to_hi, -(t - kMagic)), u = fmaf(r, (float)(1 << kLoBits), kMagic);
     atomicAdd(at, __float_as_int(t) - __float_as_int(kMagic));
     atomicAdd(at + buckets, __float_as_int(u) - __float_as_int(kMagic));
@@ -64,19 +65,19 @@ __device__ __forceinline__ float tally_value(long long hi, long long lo, float l
   return (float)(((double)hi + (double)lo * (1.0 / (1 << kLoBits))) * (1.0 / (1 << kHiBits)) * (double)limit);
 }
 
+template <int NT>
+__device__ __forceinline__ bool all_real(uint64_t real) { return real == (NT == 8 ? ~(uint64_t)0 : ((uint64_t)1 << (8 * NT & 63)) - 1); }
+
 // Columns that hold no row: products of whatever lies there do not count.
-template <int NP>
-__device__ __forceinline__ void clear_columns(float (&c)[2 * NP][4], int pairs, uint64_t real) {
+template <int NT>
+__device__ __forceinline__ void clear_columns(float (&c)[NT][4], uint64_t real) {
+  if (all_real<NT>(real)) return;
+  const uint64_t mine = real >> ((threadIdx.x & 3) * 2);
 #pragma unroll
-  for (int t = 0; t < 2 * NP; ++t)
-    if (t / 2 < pairs) {
-      const uint32_t bits = (uint32_t)(real >> (8 * t)) & 0xffu;
-      if (bits != 0xffu) {
-        const uint32_t mine = bits >> ((threadIdx.x & 3) * 2);
-        if (!(mine & 1)) c[t][0] = c[t][2] = 0.f;
-        if (!(mine & 2)) c[t][1] = c[t][3] = 0.f;
-      }
-    }
+  for (int t = 0; t < NT; ++t) {
+    if (!(mine >> (8 * t) & 1)) c[t][0] = c[t][2] = 0.f;
+    if (!(mine >> (8 * t + 1) & 1)) c[t][1] = c[t][3] = 0.f;
+  }
 }
 
 // A tile's two rows of the first pass: maximum and sum as in Flow, D and the largest |p dp| before they are divided by the sum.
@@ -88,29 +89,27 @@ struct RowSums {
   }
 };
 // (s: scores, then weights; dp: products of do and v)
-template <int NP>
-__device__ __forceinline__ void sum_rows(RowSums& f, float (&s)[2 * NP][4], const float (&dp)[2 * NP][4], int pairs) {
+template <int NT>
+__device__ __forceinline__ void sum_rows(RowSums& f, float (&s)[NT][4], const float (&dp)[NT][4]) {
 #pragma unroll
   for (int r = 0; r < 2; ++r) {
     float m = f.m[r];
 #pragma unroll
-    for (int t = 0; t < 2 * NP; ++t)
-      if (t / 2 < pairs) m = fmaxf(m, fmaxf(s[t][2 * r], s[t][2 * r + 1]));
+    for (int t = 0; t < NT; ++t) m = fmaxf(m, fmaxf(s[t][2 * r], s[t][2 * r + 1]));
     m = quad_max(m);
     const float base = m == -INFINITY ? 0.f : m, fade = ex2_approx(f.m[r] - base);
     f.m[r] = m;
     float l = f.l[r] * fade, d = f.d[r] * fade, most = f.most[r] * fade;
 #pragma unroll
-    for (int t = 0; t < 2 * NP; ++t)
-      if (t / 2 < pairs)
+    for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int e = 2 * r; e < 2 * r + 2; ++e) {
-          s[t][e] = ex2_approx(s[t][e] - base);
-          l += s[t][e];
-          const float x = s[t][e] * dp[t][e];
-          d += x;
-          most = fmaxf(most, fabsf(x));
-        }
+      for (int e = 2 * r; e < 2 * r + 2; ++e) {
+        s[t][e] = ex2_approx(s[t][e] - base);
+        l += s[t][e];
+        const float x = s[t][e] * dp[t][e];
+        d += x;
+        most = fmaxf(most, fabsf(x));
+      }
     f.l[r] = l; f.d[r] = d; f.most[r] = most;
   }
 }
@@ -123,71 +122,67 @@ __device__ __forceinline__ float3 row_stats(const RowSums& f, int r, float* boun
 }
 
 // dz of the rows' chunk into dp, from weights relative to the maximum (calls without a cap).
-template <int NP>
-__device__ __forceinline__ void differ_weights(const float (&s)[2 * NP][4], float (&dp)[2 * NP][4], const float3 (&st)[2], int pairs) {
+template <int NT>
+__device__ __forceinline__ void differ_weights(const float (&s)[NT][4], float (&dp)[NT][4], const float3 (&st)[2]) {
 #pragma unroll
-  for (int t = 0; t < 2 * NP; ++t)
-    if (t / 2 < pairs)
+  for (int t = 0; t < NT; ++t)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) dp[t][e] = s[t][e] * st[e >> 1].y * (dp[t][e] - st[e >> 1].z);
+    for (int e = 0; e < 4; ++e) dp[t][e] = s[t][e] * st[e >> 1].y * (dp[t][e] - st[e >> 1].z);
 }
 
 // The same from products, s = q k.
-template <int NP>
-__device__ __forceinline__ void differ_rows(float (&s)[2 * NP][4], float (&dp)[2 * NP][4], const Scoring& sc, const float* bias, const uint16_t* index, int pitch,
-                                            const float3 (&st)[2], int pairs, uint64_t real) {
+template <int NT>
+__device__ __forceinline__ void differ_rows(float (&s)[NT][4], float (&dp)[NT][4], const Scoring& sc, const float* bias, const uint16_t* index, int pitch,
+                                            const float3 (&st)[2], uint64_t real) {
 #pragma unroll
-  for (int t = 0; t < 2 * NP; ++t)
-    if (t / 2 < pairs) {
-      float slope[4];
-      score_tile<true>(s[t], slope, sc, bias, index + t * 8, pitch, (uint32_t)(real >> (8 * t)));
+  for (int t = 0; t < NT; ++t) {
+    float slope[4];
+    score_tile<true>(s[t], slope, sc, bias, index + t * 8, pitch, (uint32_t)(real >> (8 * t)));
 #pragma unroll
-      for (int e = 0; e < 4; ++e) dp[t][e] = ex2_approx(s[t][e] - st[e >> 1].x) * st[e >> 1].y * (dp[t][e] - st[e >> 1].z) * slope[e];
-    }
+    for (int e = 0; e < 4; ++e) dp[t][e] = ex2_approx(s[t][e] - st[e >> 1].x) * st[e >> 1].y * (dp[t][e] - st[e >> 1].z) * slope[e];
+  }
 }
 
 // The second pass's chunk: rows are keys, columns queries.  s: products k q -> p; dp: products v do -> dz.  `index`: buckets, at the first
 // row and column of the fragment (ROWS: [key][query], else [query][key]); `stats`: the columns' maximum, 1 / sum and D.
-template <int NP, bool ROWS>
-__device__ __forceinline__ void differ_columns(float (&s)[2 * NP][4], float (&dp)[2 * NP][4], const Scoring& sc, const float* bias, const uint16_t* index, int pitch,
-                                               const float4* stats, int pairs, uint64_t real, const Tally& tally, int h, bool count0, bool count1) {
+template <int NT, bool ROWS>
+__device__ __forceinline__ void differ_columns(float (&s)[NT][4], float (&dp)[NT][4], const Scoring& sc, const float* bias, const uint16_t* index, int pitch,
+                                               const float4* stats, uint64_t real, const Tally& tally, int h, bool count0, bool count1) {
   const int g = (threadIdx.x & 31) >> 2, q2 = (threadIdx.x & 3) * 2;
 #pragma unroll
-  for (int t = 0; t < 2 * NP; ++t)
-    if (t / 2 < pairs) {
-      int bk[4] = {};
-      float b[4] = {}, slope[4];
-      if (sc.bias) {
-        if (ROWS) {
-          buckets_of(bk, index + t * 8, pitch);
-        } else {
-          const uint16_t* at = index + (t * 8 + q2) * pitch + g;
-          bk[0] = at[0]; bk[1] = at[pitch]; bk[2] = at[8]; bk[3] = at[pitch + 8];
-        }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) b[e] = bias[bk[e]];
+  for (int t = 0; t < NT; ++t) {
+    int bk[4] = {};
+    float b[4] = {}, slope[4];
+    if (sc.bias) {
+      if (ROWS) {
+        buckets_of(bk, index + t * 8, pitch);
+      } else {
+        const uint16_t* at = index + (t * 8 + q2) * pitch + g;
+        bk[0] = at[0]; bk[1] = at[pitch]; bk[2] = at[8]; bk[3] = at[pitch + 8];
       }
-      score_of<true>(sc, s[t], b, slope);
-      const float4 st[2] = {stats[t * 8 + q2], stats[t * 8 + q2 + 1]};
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        s[t][e] = ex2_approx(s[t][e] - st[e & 1].x) * st[e & 1].y;
-        dp[t][e] = s[t][e] * (dp[t][e] - st[e & 1].z);
-      }
-      uint32_t mine = 3;
-      if (((uint32_t)(real >> (8 * t)) & 0xffu) != 0xffu) {  // columns without a query: whatever lies there
-        mine = (uint32_t)(real >> (8 * t)) >> q2;
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (!((mine >> (e & 1)) & 1)) s[t][e] = dp[t][e] = slope[e] = 0.f;
-      }
-      if (tally.on)
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (e < 2 ? count0 : count1) tally.add(h, bk[e], dp[t][e]);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) dp[t][e] *= slope[e];
+      for (int e = 0; e < 4; ++e) b[e] = bias_at(bias, bk[e]);
     }
+    score_of<true>(sc, s[t], b, slope);
+    const float4 st[2] = {stats[t * 8 + q2], stats[t * 8 + q2 + 1]};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      s[t][e] = ex2_approx(s[t][e] - st[e & 1].x) * st[e & 1].y;
+      dp[t][e] = s[t][e] * (dp[t][e] - st[e & 1].z);
+    }
+    if (((uint32_t)(real >> (8 * t)) & 0xffu) != 0xffu) {  // columns without a query: whatever lies there
+      const uint32_t mine = (uint32_t)(real >> (8 * t)) >> q2;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (!((mine >> (e & 1)) & 1)) s[t][e] = dp[t][e] = slope[e] = 0.f;
+    }
+    if (tally.on)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (e < 2 ? count0 : count1) tally.add(h, bk[e], dp[t][e]);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) dp[t][e] *= slope[e];
+  }
 }
 
 // Rows of an accumulator to global memory.
@@ -211,6 +206,73 @@ __device__ __forceinline__ void clear(float (&acc)[DT / 8][4]) {
 template <typename T>
 constexpr bool kWide = std::is_same<T, __half>::value;
 
+// Heads of a block that holds its segments whole.
+template <typename T, int DT>
+constexpr int kBackHeads = DT * sizeof(T) <= 32 ? 8 : DT * sizeof(T) <= 64 ? 4 : DT * sizeof(T) <= 128 ? 2 : 1;
+
+// A tile of 16 rows against a chunk of its segment's rows, in one block's shared memory: addresses of a head's first channel.
+struct Operands {
+  uint32_t q, k, v, o;          // at the tile's first row
+  uint32_t cq, ck, cv, co;      // at the chunk's
+  const float* bias;
+  const uint16_t* index;        // at the tile's first row and the chunk's first column (by keys: the chunk's first row, the tile's first column)
+  int pitch_idx;
+  uint32_t pitch;
+  int dim;
+};
+
+// By queries: products into s and dp.
+template <typename T, int DT, int NT>
+__device__ __forceinline__ void products(float (&s)[NT][4], float (&dp)[NT][4], const Operands& x, uint64_t keys) {
+  scores<T, DT, NT>(s, x.q, x.ck, x.pitch, x.dim);
+  scores<T, DT, NT>(dp, x.o, x.cv, x.pitch, x.dim);
+  clear_columns<NT>(dp, keys);
+}
+// A segment whose keys are one chunk: everything of the tile's rows at once.
+template <typename T, int DT, int NT>
+__device__ __forceinline__ void rows_at_once(float (&acc)[DT / 8][4], float3 (&st)[2], float (&bound)[2], const Operands& x, const Scoring& sc, uint64_t keys) {
+  float s[NT][4], dp[NT][4];
+  products<T, DT, NT>(s, dp, x, keys);
+  transform<NT>(s, sc, x.bias, x.index, x.pitch_idx, keys);
+  RowSums f;
+  f.start();
+  sum_rows<NT>(f, s, dp);
+  st[0] = row_stats(f, 0, &bound[0]);
+  st[1] = row_stats(f, 1, &bound[1]);
+  if (sc.cap == 0.f) {
+    differ_weights<NT>(s, dp, st);
+  } else {
+    scores<T, DT, NT>(s, x.q, x.ck, x.pitch, x.dim);
+    differ_rows<NT>(s, dp, sc, x.bias, x.index, x.pitch_idx, st, keys);
+  }
+  weigh<T, DT, NT, kWide<T>>(acc, dp, x.ck, x.pitch, x.dim, keys);
+}
+template <typename T, int DT, int NT>
+__device__ __forceinline__ void rows_first(RowSums& f, const Operands& x, const Scoring& sc, uint64_t keys) {
+  float s[NT][4], dp[NT][4];
+  products<T, DT, NT>(s, dp, x, keys);
+  transform<NT>(s, sc, x.bias, x.index, x.pitch_idx, keys);
+  sum_rows<NT>(f, s, dp);
+}
+template <typename T, int DT, int NT>
+__device__ __forceinline__ void rows_second(float (&acc)[DT / 8][4], const float3 (&st)[2], const Operands& x, const Scoring& sc, uint64_t keys) {
+  float s[NT][4], dp[NT][4];
+  products<T, DT, NT>(s, dp, x, keys);
+  differ_rows<NT>(s, dp, sc, x.bias, x.index, x.pitch_idx, st, keys);
+  weigh<T, DT, NT, kWide<T>>(acc, dp, x.ck, x.pitch, x.dim, keys);
+}
+// By keys.
+template <typename T, int DT, int NT, bool ROWS>
+__device__ __forceinline__ void columns(float (&dk)[DT / 8][4], float (&dv)[DT / 8][4], const Operands& x, const Scoring& sc, const float4* stats, uint64_t queries,
+                                        const Tally& tally, int h, bool count0, bool count1) {
+  float s[NT][4], dp[NT][4];
+  scores<T, DT, NT>(s, x.k, x.cq, x.pitch, x.dim);
+  scores<T, DT, NT>(dp, x.v, x.co, x.pitch, x.dim);
+  differ_columns<NT, ROWS>(s, dp, sc, x.bias, x.index, x.pitch_idx, stats, queries, tally, h, count0, count1);
+  weigh<T, DT, NT, kWide<T>>(dk, dp, x.cq, x.pitch, x.dim, queries);
+  weigh<T, DT, NT, false>(dv, s, x.co, x.pitch, x.dim, queries);
+}
+
 // ---- short segments ------------------------------------------------------------------------------------------------
 struct BackLayout {
   ShortLayout s;
@@ -220,7 +282,7 @@ struct BackLayout {
 template <typename T, int DT>
 static BackLayout back_layout(const SegArgs& a, int limit) {
   BackLayout l = {};
-  l.s = short_layout<T, DT>(a, limit, 4);
+  l.s = short_layout<T>(a, kBackHeads<T, DT>, limit, 4);
   uint32_t at = l.s.bytes;
   l.stats = at; at += l.s.heads * (kRowBlock + limit + 15) * 16;
   if (a.dbias) {
@@ -234,7 +296,7 @@ static BackLayout back_layout(const SegArgs& a, int limit) {
 template <typename T, int DT>
 __global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) short_backward_kernel(const __grid_constant__ SegArgs a, const BackLayout L, const Scoring sc, const BackWork work, int blocks) {
   extern __shared__ __align__(16) unsigned char smem[];
-  constexpr int HG = kHeads<T, DT>, NP = sizeof(T) == 2 ? 3 : 2, NK = 2;  // pairs of 8 columns in registers, by queries and by keys
+  constexpr int HG = kBackHeads<T, DT>;
   const int dim = kExact<DT> ? DT : a.dim;
   __shared__ uint32_t block_bound;
   pdl_enter();
@@ -256,7 +318,7 @@ __global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) short_backward_ker
   tally.bound(0.f);
   stage_tables(a, maps, bias, head0, HG);
   if (a.bias)
-    for (int i = threadIdx.x; i < (kRowBlock + 15 + L.s.limit) * L.s.pitch_idx / 2; i += kThreads) reinterpret_cast<uint32_t*>(index)[i] = 0;
+    for (int i = threadIdx.x; i < L.s.index_words; i += kThreads) reinterpret_cast<uint32_t*>(index)[i] = 0;
   float* mine = work.partial + (int64_t)blockIdx.x * work.table + head0 * a.buckets;
   if (tally.on) {
     for (int i = threadIdx.x; i < HG * 2 * a.buckets; i += kThreads) tally.hist[i] = 0;
@@ -285,15 +347,17 @@ __global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) short_backward_ker
   const int64_t col = (int64_t)head0 * dim;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, h = warp % HG, g = lane >> 2;
   const uint32_t at_head = h * dim * sizeof(T);
+  const Rows<4> src = {{first_head<T>(a.q, col), first_head<T>(a.k, col), first_head<T>(a.v, col), first_head<T>(a.d_out, col)},
+                       {a.ld_q * (int64_t)sizeof(T), a.ld_k * (int64_t)sizeof(T), a.ld_v * (int64_t)sizeof(T), a.ld_do * (int64_t)sizeof(T)}};
+  Operands x = {};
+  x.bias = bias + h * a.buckets;
+  x.pitch_idx = L.s.pitch_idx; x.pitch = pitch; x.dim = dim;
   for (int block = blockIdx.x; block < blocks; block += gridDim.x) {
     __syncthreads();
     if (threadIdx.x == 0) block_bound = 0;
     make_plan(a, plan, cells, block, blocks, L.s.limit);
     if (plan.items == 0) continue;
-    load_rows<T>(q0, pitch, a.q, a.ld_q, plan.ids, plan.rows, col, chunks, real);
-    load_rows<T>(k0, pitch, a.k, a.ld_k, plan.ids, plan.rows, col, chunks, real);
-    load_rows<T>(v0, pitch, a.v, a.ld_v, plan.ids, plan.rows, col, chunks, real);
-    load_rows<T>(o0, pitch, a.d_out, a.ld_do, plan.ids, plan.rows, col, chunks, real);
+    load_rows<T, 4>(q0, L.s.array, pitch, src, plan.ids, plan.rows, chunks, real);
     cp_commit();
     if (a.bias) fill_index(a, plan, cells, maps, index, L.s.pitch_idx);
     cp_wait<0>();
@@ -303,24 +367,39 @@ __global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) short_backward_ker
       for (int it = warp / HG; it < plan.items; it += kWarps / HG) {
         const Item item = plan.item[it];
         const int row = item.at + 16 * item.tile, r0 = 16 * item.tile + g;
-        RowSums f;
-        f.start();
-        float s[2 * NP][4], dp[2 * NP][4];
-        auto products = [&](int j, int pairs, uint64_t keys) {
+        x.q = q0 + row * pitch + at_head; x.o = o0 + row * pitch + at_head;
+        auto to_chunk = [&](int j) {
           const uint32_t at = (item.at + j) * pitch + at_head;
-          scores<T, DT, NP>(s, q0 + row * pitch + at_head, k0 + at, pitch, dim, pairs);
-          scores<T, DT, NP>(dp, o0 + row * pitch + at_head, v0 + at, pitch, dim, pairs);
-          clear_columns<NP>(dp, pairs, keys);
+          x.ck = k0 + at; x.cv = v0 + at;
+          x.index = index + row * L.s.pitch_idx + j;
         };
-        for (int j = 0; j < item.len; j += 16 * NP) {
-          const int cols = min(16 * NP, item.len - j), pairs = (cols + 15) >> 4;
-          const uint64_t keys = real_rows(plan, item.at + j, cols);
-          products(j, pairs, keys);
-          transform<NP>(s, sc, bias + h * a.buckets, index + row * L.s.pitch_idx + j, L.s.pitch_idx, pairs, keys);
-          sum_rows<NP>(f, s, dp, pairs);
+        float acc[DT / 8][4], bound[2];
+        float3 st[2];
+        clear<DT>(acc);
+        to_chunk(0);
+        if (item.len <= 40) {
+          const uint64_t keys = real_rows(plan, item.at, item.len);
+          switch ((item.len + 7) >> 3) {
+            case 1: rows_at_once<T, DT, 1>(acc, st, bound, x, sc, keys); break;
+            case 2: rows_at_once<T, DT, 2>(acc, st, bound, x, sc, keys); break;
+            case 3: rows_at_once<T, DT, 3>(acc, st, bound, x, sc, keys); break;
+            case 4: rows_at_once<T, DT, 4>(acc, st, bound, x, sc, keys); break;
+            default: rows_at_once<T, DT, 5>(acc, st, bound, x, sc, keys);
+          }
+        } else {
+          RowSums f;
+          f.start();
+          for (int j = 0; j < item.len; j += 32) {
+            to_chunk(j);
+            rows_first<T, DT, 4>(f, x, sc, real_rows(plan, item.at + j, min(32, item.len - j)));
+          }
+          st[0] = row_stats(f, 0, &bound[0]);
+          st[1] = row_stats(f, 1, &bound[1]);
+          for (int j = 0; j < item.len; j += 32) {
+            to_chunk(j);
+            rows_second<T, DT, 4>(acc, st, x, sc, real_rows(plan, item.at + j, min(32, item.len - j)));
+          }
         }
-        float bound[2];
-        const float3 st[2] = {row_stats(f, 0, &bound[0]), row_stats(f, 1, &bound[1])};
         const int id0 = r0 < item.len ? plan.ids[item.at + r0] : -1, id1 = r0 + 8 < item.len ? plan.ids[item.at + r0 + 8] : -1;
         if (id0 >= 0) most = fmaxf(most, bound[0]);
         if (id1 >= 0) most = fmaxf(most, bound[1]);
@@ -328,21 +407,6 @@ __global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) short_backward_ker
           float4* to = stats + h * stat_rows + row + g;
           if (r0 < item.len) to[0] = make_float4(st[0].x, st[0].y, st[0].z, 0.f);
           if (r0 + 8 < item.len) to[8] = make_float4(st[1].x, st[1].y, st[1].z, 0.f);
-        }
-        float acc[DT / 8][4];
-        clear<DT>(acc);
-        if (item.len <= 16 * NP && sc.cap == 0.f) {  // the weights are still there
-          const int pairs = (item.len + 15) >> 4;
-          differ_weights<NP>(s, dp, st, pairs);
-          weigh<T, DT, NP, kWide<T>>(acc, dp, k0 + item.at * pitch + at_head, pitch, dim, pairs, real_rows(plan, item.at, item.len));
-        } else {
-          for (int j = 0; j < item.len; j += 16 * NP) {
-            const int cols = min(16 * NP, item.len - j), pairs = (cols + 15) >> 4;
-            const uint64_t keys = real_rows(plan, item.at + j, cols);
-            products(j, pairs, keys);
-            differ_rows<NP>(s, dp, sc, bias + h * a.buckets, index + row * L.s.pitch_idx + j, L.s.pitch_idx, st, pairs, keys);
-            weigh<T, DT, NP, kWide<T>>(acc, dp, k0 + (item.at + j) * pitch + at_head, pitch, dim, pairs, keys);
-          }
         }
         store_rows<T, DT>(acc, a.scale, a.dq, a.ld_dq, col + h * dim, dim, id0, id1);
       }
@@ -370,17 +434,20 @@ __global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) short_backward_ker
         float dk[DT / 8][4], dv[DT / 8][4];
         clear<DT>(dk);
         clear<DT>(dv);
-        for (int j = 0; j < item.len; j += 16 * NK) {
-          const int cols = min(16 * NK, item.len - j), pairs = (cols + 15) >> 4;
+        x.k = k0 + row * pitch + at_head; x.v = v0 + row * pitch + at_head;
+        for (int j = 0; j < item.len; j += 32) {
+          const int cols = min(32, item.len - j);
           const uint64_t queries = real_rows(plan, item.at + j, cols);
           const uint32_t at = (item.at + j) * pitch + at_head;
-          float s[2 * NK][4], dp[2 * NK][4];
-          scores<T, DT, NK>(s, k0 + row * pitch + at_head, q0 + at, pitch, dim, pairs);
-          scores<T, DT, NK>(dp, v0 + row * pitch + at_head, o0 + at, pitch, dim, pairs);
-          differ_columns<NK, false>(s, dp, sc, bias + h * a.buckets, index + (item.at + j) * L.s.pitch_idx + 16 * item.tile, L.s.pitch_idx,
-                                         stats + h * stat_rows + item.at + j, pairs, queries, tally, h, id0 >= 0, id1 >= 0);
-          weigh<T, DT, NK, kWide<T>>(dk, dp, q0 + at, pitch, dim, pairs, queries);
-          weigh<T, DT, NK, false>(dv, s, o0 + at, pitch, dim, pairs, queries);
+          const float4* from = stats + h * stat_rows + item.at + j;
+          x.cq = q0 + at; x.co = o0 + at;
+          x.index = index + (item.at + j) * L.s.pitch_idx + 16 * item.tile;
+          switch ((cols + 7) >> 3) {
+            case 1: columns<T, DT, 1, false>(dk, dv, x, sc, from, queries, tally, h, id0 >= 0, id1 >= 0); break;
+            case 2: columns<T, DT, 2, false>(dk, dv, x, sc, from, queries, tally, h, id0 >= 0, id1 >= 0); break;
+            case 3: columns<T, DT, 3, false>(dk, dv, x, sc, from, queries, tally, h, id0 >= 0, id1 >= 0); break;
+            default: columns<T, DT, 4, false>(dk, dv, x, sc, from, queries, tally, h, id0 >= 0, id1 >= 0);
+          }
         }
         store_rows<T, DT>(dk, a.scale, a.dk, a.ld_dk, col + h * dim, dim, id0, id1);
         store_rows<T, DT>(dv, 1.f, a.dv, a.ld_dv, col + h * dim, dim, id0, id1);
@@ -396,8 +463,8 @@ __global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) short_backward_ker
 // ---- long segments -------------------------------------------------------------------------------------------------
 template <typename T, int DT>
 struct BackShape {
-  static constexpr int HG = kHeads<T, DT> < 4 ? kHeads<T, DT> : 4, WH = HG < 2 ? HG : 2, HPW = HG / WH, rows = 16 * kWarps / WH;
-  static constexpr int chunk = sizeof(T) == 2 ? 64 : DT <= 64 ? 32 : 16, NP = chunk < 32 ? 1 : 2;  // rows that pass at a time; of these in registers
+  static constexpr int HG = DT * sizeof(T) <= 64 ? 4 : DT * sizeof(T) <= 128 ? 2 : 1, WH = HG < 2 ? HG : 2, HPW = HG / WH, rows = 16 * kWarps / WH;
+  static constexpr int chunk = sizeof(T) == 2 ? 64 : DT <= 64 ? 32 : 16, NT = chunk < 32 ? 2 : 4;  // rows that pass at a time; tiles of 8 of them in registers
 };
 
 struct BackLongLayout {
@@ -442,7 +509,7 @@ template <typename T, int DT, bool BY_KEYS>
 __global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) long_backward_kernel(const __grid_constant__ SegArgs a, const BackLongLayout L, const Scoring sc, const BackWork work, int above) {
   extern __shared__ __align__(16) unsigned char smem[];
   using S = BackShape<T, DT>;
-  constexpr int NP = S::NP, HPW = S::HPW;
+  constexpr int NT = S::NT, HPW = S::HPW;
   __shared__ Tile tiles[kMaxTiles];
   __shared__ int tile_count;
   const int dim = kExact<DT> ? DT : a.dim;
@@ -483,6 +550,9 @@ __global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) long_backward_kern
   const int64_t col = (int64_t)head0 * dim;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2;
   const int row = 16 * (warp / S::WH);
+  const Rows<2> by_q = {{first_head<T>(a.q, col), first_head<T>(a.d_out, col)}, {a.ld_q * (int64_t)sizeof(T), a.ld_do * (int64_t)sizeof(T)}};
+  const Rows<2> by_k = {{first_head<T>(a.k, col), first_head<T>(a.v, col)}, {a.ld_k * (int64_t)sizeof(T), a.ld_v * (int64_t)sizeof(T)}};
+  const Rows<2>&own = BY_KEYS ? by_k : by_q, &passing = BY_KEYS ? by_q : by_k;
   float most = 0.f;
   for (int ti = 0; ti < found; ++ti) {
     const Tile tile = tiles[ti];
@@ -520,8 +590,7 @@ __global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) long_backward_kern
         }
     };
     auto load = [&](int c) {
-      load_rows<T>(array(c, 0), pitch, BY_KEYS ? a.q : a.k, BY_KEYS ? a.ld_q : a.ld_k, ids_of(c), S::chunk, col, chunks, real);
-      load_rows<T>(array(c, 1), pitch, BY_KEYS ? a.d_out : a.v, BY_KEYS ? a.ld_do : a.ld_v, ids_of(c), S::chunk, col, chunks, real);
+      load_rows<T, 2>(array(c, 0), L.chunk, pitch, passing, ids_of(c), S::chunk, chunks, real);
       cp_commit();
     };
     RowSums f[BY_KEYS ? 1 : HPW];
@@ -541,8 +610,7 @@ __global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) long_backward_kern
       fetch_id(1);
       __syncthreads();
       if (BY_KEYS || sweep == 0) {
-        load_rows<T>(own0, pitch, BY_KEYS ? a.k : a.q, BY_KEYS ? a.ld_k : a.ld_q, ids, S::rows, col, chunks, real);
-        load_rows<T>(own1, pitch, BY_KEYS ? a.v : a.d_out, BY_KEYS ? a.ld_v : a.ld_do, ids, S::rows, col, chunks, real);
+        load_rows<T, 2>(own0, L.tile, pitch, own, ids, S::rows, chunks, real);
       }
       load(0);
       for (int c = 0; c < parts; ++c) {
@@ -573,28 +641,21 @@ __global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) long_backward_kern
           const int h = (warp % S::WH) * HPW + i;
           if (h >= heads || row >= rows) continue;
           const uint32_t at_head = h * dim * sizeof(T);
-          for (int j = 0; j < all; j += 16 * NP) {
-            const int cols = min(16 * NP, all - j), pairs = (cols + 15) >> 4;
-            const uint64_t bits = there >> j & (((uint64_t)1 << (16 * NP)) - 1);
-            const uint32_t a0 = array(c, 0) + j * pitch + at_head, a1 = array(c, 1) + j * pitch + at_head;
-            float s[2 * NP][4], dp[2 * NP][4];
-            scores<T, DT, NP>(s, own0 + row * pitch + at_head, a0, pitch, dim, pairs);
-            scores<T, DT, NP>(dp, own1 + row * pitch + at_head, a1, pitch, dim, pairs);
-            const uint16_t* at = index + row * L.pitch_idx + j;
-            if constexpr (!BY_KEYS) {
-              clear_columns<NP>(dp, pairs, bits);
-              if (sweep == 0) {
-                transform<NP>(s, sc, bias + h * a.buckets, at, L.pitch_idx, pairs, bits);
-                sum_rows<NP>(f[i], s, dp, pairs);
-              } else {
-                differ_rows<NP>(s, dp, sc, bias + h * a.buckets, at, L.pitch_idx, st[i], pairs, bits);
-                weigh<T, DT, NP, kWide<T>>(acc[i], dp, a0, pitch, dim, pairs, bits);
-              }
+          Operands x = {};
+          x.bias = bias + h * a.buckets;
+          x.pitch_idx = L.pitch_idx; x.pitch = pitch; x.dim = dim;
+          x.q = x.k = own0 + row * pitch + at_head;
+          x.o = x.v = own1 + row * pitch + at_head;
+          for (int j = 0; j < all; j += 8 * NT) {
+            const uint64_t bits = there >> j & (((uint64_t)1 << (8 * NT)) - 1);
+            x.cq = x.ck = array(c, 0) + j * pitch + at_head;
+            x.co = x.cv = array(c, 1) + j * pitch + at_head;
+            x.index = index + row * L.pitch_idx + j;
+            if constexpr (BY_KEYS) {
+              columns<T, DT, NT, true>(acc[i], dv[i], x, sc, stats_of(c) + h * S::chunk + j, bits, tally, h, ids[row + g] >= 0, ids[row + g + 8] >= 0);
             } else {
-              differ_columns<NP, true>(s, dp, sc, bias + h * a.buckets, at, L.pitch_idx, stats_of(c) + h * S::chunk + j, pairs, bits, tally, h, ids[row + g] >= 0,
-                                            ids[row + g + 8] >= 0);
-              weigh<T, DT, NP, kWide<T>>(acc[i], dp, a0, pitch, dim, pairs, bits);
-              weigh<T, DT, NP, false>(dv[i], s, a1, pitch, dim, pairs, bits);
+              if (sweep == 0) rows_first<T, DT, NT>(f[i], x, sc, bits);
+              else rows_second<T, DT, NT>(acc[i], st[i], x, sc, bits);
             }
           }
         }
@@ -666,7 +727,7 @@ int backward_of(dsvt_ctx* ctx, const SegArgs& a) {
   BackLayout l = back_layout<T, DT>(a, limit);
   while (l.bytes > kSmemMost) l = back_layout<T, DT>(a, limit = limit > 64 ? 64 : limit / 2);
   const Scoring sc = scoring_of(a);
-  const int groups = (int)dsvt_ceil_div(a.heads, kHeads<T, DT>), blocks = (int)dsvt_ceil_div(a.n, kRowBlock);
+  const int groups = (int)dsvt_ceil_div(a.heads, kBackHeads<T, DT>), blocks = (int)dsvt_ceil_div(a.n, kRowBlock);
   BackWork w = {};
   uint32_t* base = reinterpret_cast<uint32_t*>(ctx->bm_zero);
   w.partial = reinterpret_cast<float*>(base);

@@ -47,7 +47,7 @@ __device__ __forceinline__ int2 segments_near(const SegArgs& a, int from, int to
 // Copies what every block reads: the index tables of the displacements and its heads' bias, in units of log 2.
 __device__ __forceinline__ void stage_tables(const SegArgs& a, uint16_t* maps, float* bias, int head0, int heads) {
   if (!a.bias) return;
-  for (int i = threadIdx.x; i < a.maps.at_z + 2 * a.maps.extent[2] - 1; i += kThreads) maps[i] = a.maps.of[i];
+  for (int i = threadIdx.x; i < a.maps.at_z + 2 * a.maps.extent[2] - 1; i += kThreads) maps[i] = (uint16_t)(4 * a.maps.of[i]);
   const int count = min(heads, a.heads - head0) * a.buckets;
   const float* from = a.bias + (int64_t)head0 * a.buckets;
   for (int i = threadIdx.x; i < count; i += kThreads) bias[i] = bias_log2(from[i]);
@@ -56,7 +56,7 @@ __device__ __forceinline__ void stage_tables(const SegArgs& a, uint16_t* maps, f
 __device__ __forceinline__ int bucket_at(const BucketMaps& m, const uint16_t* maps, int4 i, int4 j) {
   const int ex = m.extent[0] - 1, ey = m.extent[1] - 1, ez = m.extent[2] - 1;
   const int dx = min(max(i.y - j.y, -ex), ex) + ex, dy = min(max(i.z - j.z, -ey), ey) + ey + m.at_y, dz = min(max(i.w - j.w, -ez), ez) + ez + m.at_z;
-  return maps[dx] + maps[dy] + maps[dz];
+  return maps[dx] + maps[dy] + maps[dz];  // (the maps in shared memory hold four times the index: a bias's offset)
 }
 
 // The block's segments (of at most `limit` rows), their rows' voxels and the list of their tiles.
@@ -129,15 +129,32 @@ __device__ __forceinline__ void fill_index(const SegArgs& a, const Plan& p, cons
   }
 }
 
-// Rows' parts of a block's heads to shared memory: `chunks` pieces of 16 bytes each, of which the first `real` exist.
-template <typename T>
-__device__ __forceinline__ void load_rows(uint32_t to, uint32_t pitch, const void* from, int64_t ld, const int32_t* ids, int rows, int64_t col, int chunks, int real) {
-  for (int i = threadIdx.x; i < rows * chunks; i += kThreads) {
-    const int r = i / chunks, c = i - r * chunks, id = ids[r];
-    const bool in = id >= 0 && c < real;
-    cp_async16(to + r * pitch + c * 16, (const char*)from + ((in ? (int64_t)id * ld : 0) + col) * (int64_t)sizeof(T) + (in ? c * 16 : 0), in);
+// Rows' parts of a block's heads to shared memory, N arrays of them: `chunks` pieces of 16 bytes to a row, of which the first `real`
+// exist.  Eight threads to a row.
+template <int N>
+struct Rows {
+  const char* from[N];  // at the block's first head
+  int64_t ld[N];        // bytes
+};
+template <typename T, int N>
+__device__ __forceinline__ void load_rows(uint32_t to, uint32_t array, uint32_t pitch, const Rows<N>& src, const int32_t* ids, int rows, int chunks, int real) {
+  const int part = threadIdx.x & 7;
+  for (int r = threadIdx.x >> 3; r < rows; r += kThreads / 8) {
+    const int id = ids[r];
+    const char* at[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) at[i] = src.from[i] + (id < 0 ? 0 : id) * src.ld[i];
+    const uint32_t dst = to + r * pitch;
+#pragma unroll 4
+    for (int c = part; c < chunks; c += 8) {
+      const bool in = id >= 0 && c < real;
+#pragma unroll
+      for (int i = 0; i < N; ++i) cp_async16(dst + i * array + c * 16, at[i] + (in ? c * 16 : 0), in);
+    }
   }
 }
+template <typename T>
+__device__ __forceinline__ const char* first_head(const void* p, int64_t col) { return reinterpret_cast<const char*>(p) + col * (int64_t)sizeof(T); }
 
 // Rounds two neighbouring channels into a row in shared or global memory.
 template <typename T>
@@ -146,13 +163,14 @@ __device__ __forceinline__ void store2(T* to, float x, float y) {
   else *reinterpret_cast<uint32_t*>(to) = Mma<T>::pack(x, y);
 }
 
-// The buckets of a tile's four pairs; `index`: at its first row and column.
+// The buckets of a tile's four pairs, times 4; `index`: at its first row and column.
 __device__ __forceinline__ void buckets_of(int (&bk)[4], const uint16_t* index, int pitch) {
   const int lane = threadIdx.x & 31;
   const uint16_t* at = index + (lane >> 2) * pitch + (lane & 3) * 2;
   const uint32_t i0 = *reinterpret_cast<const uint32_t*>(at), i1 = *reinterpret_cast<const uint32_t*>(at + 8 * pitch);
   bk[0] = i0 & 0xffff; bk[1] = i0 >> 16; bk[2] = i1 & 0xffff; bk[3] = i1 >> 16;
 }
+__device__ __forceinline__ float bias_at(const float* bias, int bk) { return *reinterpret_cast<const float*>(reinterpret_cast<const char*>(bias) + bk); }
 
 // A tile of scores of queries (rows) and keys (columns) from products; -inf where a column holds no key.
 template <bool SLOPE>
@@ -162,7 +180,7 @@ __device__ __forceinline__ void score_tile(float (&s)[4], float (&slope)[4], con
     int bk[4];
     buckets_of(bk, index, pitch);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) b[e] = bias[bk[e]];
+    for (int e = 0; e < 4; ++e) b[e] = bias_at(bias, bk[e]);
   }
   score_of<SLOPE>(sc, s, b, slope);
   if ((bits & 0xffu) != 0xffu) {
@@ -179,12 +197,30 @@ __device__ __forceinline__ void score_tile(float (&s)[4], float (&slope)[4], con
 }
 
 // `index`: the fragment's first row's buckets at the chunk's first column (rows g and g + 8 of the tile).
-template <int NP>
-__device__ __forceinline__ void transform(float (&s)[2 * NP][4], const Scoring& sc, const float* bias, const uint16_t* index, int pitch, int pairs, uint64_t real) {
+template <int NT>
+__device__ __forceinline__ void transform(float (&s)[NT][4], const Scoring& sc, const float* bias, const uint16_t* index, int pitch, uint64_t real) {
+  float b[NT][4];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    b[t][0] = b[t][1] = b[t][2] = b[t][3] = 0.f;
+    if (sc.bias) {
+      int bk[4];
+      buckets_of(bk, index + t * 8, pitch);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) b[t][e] = bias_at(bias, bk[e]);
+    }
+  }
   float none[4];
 #pragma unroll
-  for (int t = 0; t < 2 * NP; ++t)
-    if (t / 2 < pairs) score_tile<false>(s[t], none, sc, bias, index + t * 8, pitch, (uint32_t)(real >> (8 * t)));
+  for (int t = 0; t < NT; ++t) score_of<false>(sc, s[t], b[t], none);
+  if (real != (NT == 8 ? ~(uint64_t)0 : ((uint64_t)1 << (8 * NT & 63)) - 1)) {
+    const uint64_t mine = real >> ((threadIdx.x & 3) * 2);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      if (!(mine >> (8 * t) & 1)) s[t][0] = s[t][2] = -INFINITY;
+      if (!(mine >> (8 * t + 1) & 1)) s[t][1] = s[t][3] = -INFINITY;
+    }
+  }
 }
 
 __device__ __forceinline__ float quad_max(float v) {
@@ -210,32 +246,34 @@ struct Flow {
   }
 };
 
-// One chunk of keys: s holds the scores, and the weights afterwards.  (l: the lane's share; quad_sum at the end.)
-template <int DT, int NP>
-__device__ __forceinline__ void soften(Flow<DT>& f, float (&s)[2 * NP][4], int pairs) {
+// One chunk of keys: s holds the scores, and the weights afterwards.  (l: the lane's share; quad_sum at the end.)  FIRST: of a row.
+template <bool FIRST, int DT, int NT>
+__device__ __forceinline__ void soften(Flow<DT>& f, float (&s)[NT][4]) {
 #pragma unroll
   for (int r = 0; r < 2; ++r) {
-    float m = f.m[r];
+    float m = FIRST ? -INFINITY : f.m[r];
 #pragma unroll
-    for (int t = 0; t < 2 * NP; ++t)
-      if (t / 2 < pairs) m = fmaxf(m, fmaxf(s[t][2 * r], s[t][2 * r + 1]));
+    for (int t = 0; t < NT; ++t) m = fmaxf(m, fmaxf(s[t][2 * r], s[t][2 * r + 1]));
     m = quad_max(m);
-    const float base = m == -INFINITY ? 0.f : m, fade = ex2_approx(f.m[r] - base);
-    f.m[r] = m;
-    float l = f.l[r] * fade;
+    const float base = m == -INFINITY ? 0.f : m;
+    float l = 0.f;
+    if (!FIRST) {
+      const float fade = ex2_approx(f.m[r] - base);
+      l = f.l[r] * fade;
 #pragma unroll
-    for (int t = 0; t < 2 * NP; ++t)
-      if (t / 2 < pairs) {
-        s[t][2 * r] = ex2_approx(s[t][2 * r] - base);
-        s[t][2 * r + 1] = ex2_approx(s[t][2 * r + 1] - base);
-        l += s[t][2 * r] + s[t][2 * r + 1];
+      for (int n = 0; n < DT / 8; ++n) {
+        f.acc[n][2 * r] *= fade;
+        f.acc[n][2 * r + 1] *= fade;
       }
-    f.l[r] = l;
-#pragma unroll
-    for (int n = 0; n < DT / 8; ++n) {
-      f.acc[n][2 * r] *= fade;
-      f.acc[n][2 * r + 1] *= fade;
     }
+    f.m[r] = m;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      s[t][2 * r] = ex2_approx(s[t][2 * r] - base);
+      s[t][2 * r + 1] = ex2_approx(s[t][2 * r + 1] - base);
+      l += s[t][2 * r] + s[t][2 * r + 1];
+    }
+    f.l[r] = l;
   }
 }
 

@@ -4,40 +4,57 @@
 
 namespace dsvt_train {
 
-// Shared memory of a block that holds its segments whole.
+// Heads of a block that holds its segments whole: rows of at most 400 bytes, which leaves room for two blocks of 36-voxel sets.
+template <typename T, int DT>
+constexpr int kHeads = DT * sizeof(T) <= 48 ? 8 : DT * sizeof(T) <= 96 ? 4 : DT * sizeof(T) <= 128 ? 2 : 1;
+
 struct ShortLayout {
   int heads;                                   // of a block
-  int pitch_idx, limit;                        // entries to a row of the bucket tile; longest segment
+  int pitch_idx, limit, index_words;           // entries to a row of the bucket tile; longest segment; the bucket tile's size
   uint32_t pitch, array;                       // bytes of a row and of an array of rows
   uint32_t maps, bias, cells, index, rows, bytes;
 };
 
-template <typename T, int DT>
-static ShortLayout short_layout(const SegArgs& a, int limit, int arrays) {
+template <typename T>
+static ShortLayout short_layout(const SegArgs& a, int heads, int limit, int arrays) {
   ShortLayout l = {};
-  l.heads = kHeads<T, DT>;
+  l.heads = heads;
   l.limit = limit;
-  const int rows = kRowBlock - 1 + limit + 16;  // (a tile of 16 may begin at the last row)
-  l.pitch = (uint32_t)(l.heads * a.dim * sizeof(T) + 16);
+  const int rows = kRowBlock - 1 + limit;
+  l.pitch = (uint32_t)(heads * a.dim * sizeof(T) + 16);
   l.array = rows * l.pitch;
   uint32_t at = (sizeof(Plan) + 15) / 16 * 16;
   auto take = [&](size_t bytes) { const uint32_t was = at; at += (uint32_t)((bytes + 15) / 16 * 16); return was; };
   if (a.bias) {
     l.maps = take(sizeof(a.maps.of));
-    l.bias = take((size_t)l.heads * a.buckets * 4);
-    l.cells = take((size_t)(kRowBlock - 1 + limit) * 16);
+    l.bias = take((size_t)heads * a.buckets * 4);
+    l.cells = take((size_t)rows * 16);
     l.pitch_idx = index_pitch(limit);
-    l.index = take((size_t)rows * l.pitch_idx * 2);
+    l.index_words = (rows + 16) * l.pitch_idx / 2 + 32;
+    l.index = take((size_t)l.index_words * 4);
   }
-  l.rows = take((size_t)arrays * l.array + 64);
+  // A tile of 16 rows may begin at an array's last row, and segments of more than 40 rows go in chunks of up to 40: what follows the
+  // rows is read, and not used.
+  l.rows = take((size_t)arrays * l.array + (limit <= 40 ? 16 : 40) * l.pitch);
   l.bytes = at;
   return l;
 }
 
+// A tile of 16 queries against its segment's keys, NT tiles of them at a time: all of them where ONLY.
+template <typename T, int DT, int NT, bool ONLY>
+__device__ __forceinline__ void attend_tile(Flow<DT>& f, uint32_t q, uint32_t k, uint32_t v, uint32_t pitch, int dim, const Scoring& sc, const float* bias,
+                                            const uint16_t* index, int pitch_idx, uint64_t keys) {
+  float s[NT][4];
+  scores<T, DT, NT>(s, q, k, pitch, dim);
+  transform<NT>(s, sc, bias, index, pitch_idx, keys);
+  soften<ONLY>(f, s);
+  weigh<T, DT, NT, false>(f.acc, s, v, pitch, dim, keys);
+}
+
 template <typename T, int DT>
-__global__ void __launch_bounds__(kThreads) short_forward_kernel(const __grid_constant__ SegArgs a, const ShortLayout L, const Scoring sc) {
+__global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) short_forward_kernel(const __grid_constant__ SegArgs a, const ShortLayout L, const Scoring sc) {
   extern __shared__ __align__(16) unsigned char smem[];
-  constexpr int HG = kHeads<T, DT>, NP = kPairs<T>;
+  constexpr int HG = kHeads<T, DT>;
   const int dim = kExact<DT> ? DT : a.dim;
   pdl_enter();
   Plan& plan = *reinterpret_cast<Plan*>(smem);
@@ -50,13 +67,13 @@ __global__ void __launch_bounds__(kThreads) short_forward_kernel(const __grid_co
   const uint32_t q0 = smem_u32(smem + L.rows), k0 = q0 + L.array, v0 = k0 + L.array;
   stage_tables(a, maps, bias, head0, HG);
   if (a.bias)
-    for (int i = threadIdx.x; i < (kRowBlock + 15 + L.limit) * L.pitch_idx / 2; i += kThreads) reinterpret_cast<uint32_t*>(index)[i] = 0;
+    for (int i = threadIdx.x; i < L.index_words; i += kThreads) reinterpret_cast<uint32_t*>(index)[i] = 0;
   make_plan(a, plan, cells, blockIdx.x, gridDim.x, L.limit);
   const int chunks = HG * dim * (int)sizeof(T) / 16, real = heads * dim * (int)sizeof(T) / 16;
   const int64_t col = (int64_t)head0 * dim;
-  load_rows<T>(q0, pitch, a.q, a.ld_q, plan.ids, plan.rows, col, chunks, real);
-  load_rows<T>(k0, pitch, a.k, a.ld_k, plan.ids, plan.rows, col, chunks, real);
-  load_rows<T>(v0, pitch, a.v, a.ld_v, plan.ids, plan.rows, col, chunks, real);
+  const Rows<3> src = {{first_head<T>(a.q, col), first_head<T>(a.k, col), first_head<T>(a.v, col)},
+                       {a.ld_q * (int64_t)sizeof(T), a.ld_k * (int64_t)sizeof(T), a.ld_v * (int64_t)sizeof(T)}};
+  load_rows<T, 3>(q0, L.array, pitch, src, plan.ids, plan.rows, chunks, real);
   cp_commit();
   if (a.bias) fill_index(a, plan, cells, maps, index, L.pitch_idx);
   cp_wait<0>();
@@ -64,22 +81,27 @@ __global__ void __launch_bounds__(kThreads) short_forward_kernel(const __grid_co
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, h = warp % HG;
   if (h < heads) {
     const uint32_t at_head = h * dim * sizeof(T);
+    const float* mine = bias + h * a.buckets;
     for (int it = warp / HG; it < plan.items; it += kWarps / HG) {
       const Item item = plan.item[it];
       const int row = item.at + 16 * item.tile;
-      const uint32_t qa = q0 + row * pitch + at_head;
+      const uint32_t q = q0 + row * pitch + at_head, k = k0 + item.at * pitch + at_head, v = v0 + item.at * pitch + at_head;
+      const uint16_t* at = index + row * L.pitch_idx;
       Flow<DT> f;
       f.start();
-      for (int j = 0; j < item.len; j += 16 * NP) {
-        const int cols = min(16 * NP, item.len - j), pairs = (cols + 15) >> 4;
-        const uint64_t keys = real_rows(plan, item.at + j, cols);
-        const uint32_t at = (item.at + j) * pitch + at_head;
-        float s[2 * NP][4];
-        scores<T, DT, NP>(s, qa, k0 + at, pitch, dim, pairs);
-        transform<NP>(s, sc, bias + h * a.buckets, index + row * L.pitch_idx + j, L.pitch_idx, pairs, keys);
-        soften<DT, NP>(f, s, pairs);
-        weigh<T, DT, NP, false>(f.acc, s, v0 + at, pitch, dim, pairs, keys);
+      const uint64_t keys = real_rows(plan, item.at, item.len);
+#define DSVT_ATTEND(NT) attend_tile<T, DT, NT, true>(f, q, k, v, pitch, dim, sc, mine, at, L.pitch_idx, keys)
+      if (item.len <= 16) {
+        if (item.len <= 8) DSVT_ATTEND(1);
+        else DSVT_ATTEND(2);
+      } else if (item.len <= 32) {
+        if (item.len <= 24) DSVT_ATTEND(3);
+        else DSVT_ATTEND(4);
+      } else {
+        for (int j = 0; j < item.len; j += 40)
+          attend_tile<T, DT, 5, false>(f, q, k + j * pitch, v + j * pitch, pitch, dim, sc, mine, at + j, L.pitch_idx, real_rows(plan, item.at + j, min(40, item.len - j)));
       }
+#undef DSVT_ATTEND
       // the result takes the place of the queries (this warp's alone: a head's channels of a tile's rows)
       const float i0 = inverse(quad_sum(f.l[0])), i1 = inverse(quad_sum(f.l[1]));
       const int r0 = 16 * item.tile + (lane >> 2);
@@ -94,10 +116,13 @@ __global__ void __launch_bounds__(kThreads) short_forward_kernel(const __grid_co
     }
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < plan.rows * chunks; i += kThreads) {
-    const int r = i / chunks, c = i - r * chunks, id = plan.ids[r];
-    if (id >= 0 && c < real)
-      *reinterpret_cast<uint4*>((char*)a.out + ((int64_t)id * a.ld_out + col) * (int64_t)sizeof(T) + c * 16) = *reinterpret_cast<const uint4*>(smem + L.rows + r * pitch + c * 16);
+  const int part = threadIdx.x & 7;
+  for (int r = threadIdx.x >> 3; r < plan.rows; r += kThreads / 8) {
+    const int id = plan.ids[r];
+    if (id < 0) continue;
+    char* to = (char*)a.out + (id * a.ld_out + col) * (int64_t)sizeof(T);
+#pragma unroll 4
+    for (int c = part; c < real; c += 8) *reinterpret_cast<uint4*>(to + c * 16) = *reinterpret_cast<const uint4*>(smem + L.rows + r * pitch + c * 16);
   }
 }
 
@@ -110,7 +135,8 @@ struct LongLayout {
 
 template <typename T, int DT>
 struct LongShape {
-  static constexpr int HG = kHeads<T, DT>, WH = HG < 2 ? HG : 2, HPW = HG / WH, rows = 16 * kWarps / WH, chunk = 16 * kPairs<T>;
+  static constexpr int HG = DT * sizeof(T) <= 64 ? 4 : DT * sizeof(T) <= 128 ? 2 : 1, WH = HG < 2 ? HG : 2, HPW = HG / WH, rows = 16 * kWarps / WH;
+  static constexpr int NT = sizeof(T) == 2 ? 8 : 6, chunk = 8 * NT;
 };
 
 template <typename T, int DT>
@@ -160,7 +186,6 @@ template <typename T, int DT>
 __global__ void __launch_bounds__(kThreads) long_forward_kernel(const __grid_constant__ SegArgs a, const LongLayout L, const Scoring sc, int above) {
   extern __shared__ __align__(16) unsigned char smem[];
   using S = LongShape<T, DT>;
-  constexpr int NP = kPairs<T>;
   __shared__ Tile tiles[kMaxTiles];
   __shared__ int tile_count;
   const int dim = kExact<DT> ? DT : a.dim;
@@ -178,6 +203,8 @@ __global__ void __launch_bounds__(kThreads) long_forward_kernel(const __grid_con
   stage_tables(a, maps, bias, head0, S::HG);
   const int chunks = S::HG * dim * (int)sizeof(T) / 16, real = heads * dim * (int)sizeof(T) / 16;
   const int64_t col = (int64_t)head0 * dim;
+  const Rows<1> own = {{first_head<T>(a.q, col)}, {a.ld_q * (int64_t)sizeof(T)}};
+  const Rows<2> passing = {{first_head<T>(a.k, col), first_head<T>(a.v, col)}, {a.ld_k * (int64_t)sizeof(T), a.ld_v * (int64_t)sizeof(T)}};
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int row = 16 * (warp / S::WH);  // of the warp's tile of 16
   for (int ti = 0; ti < found; ++ti) {
@@ -197,22 +224,20 @@ __global__ void __launch_bounds__(kThreads) long_forward_kernel(const __grid_con
       }
     };
     auto load = [&](int c) {
-      load_rows<T>(pass.array(c, 0, 2), pitch, a.k, a.ld_k, pass.ids(c), S::chunk, col, chunks, real);
-      load_rows<T>(pass.array(c, 1, 2), pitch, a.v, a.ld_v, pass.ids(c), S::chunk, col, chunks, real);
+      load_rows<T, 2>(pass.array(c, 0, 2), L.chunk, pitch, passing, pass.ids(c), S::chunk, chunks, real);
       cp_commit();
     };
     pass.fetch_id(tile.lo);
     publish(0);
     pass.fetch_id(tile.lo + S::chunk);
     __syncthreads();
-    load_rows<T>(q0, pitch, a.q, a.ld_q, ids, S::rows, col, chunks, real);
+    load_rows<T, 1>(q0, 0, pitch, own, ids, S::rows, chunks, real);
     load(0);
     Flow<DT> f[S::HPW];
 #pragma unroll
     for (int i = 0; i < S::HPW; ++i) f[i].start();
     const int parts = (tile.hi - tile.lo + S::chunk - 1) / S::chunk;
     for (int c = 0; c < parts; ++c) {
-      const int cols = min(S::chunk, tile.hi - tile.lo - c * S::chunk), pairs = (cols + 15) >> 4;
       if (c + 1 < parts) publish(c + 1);
       cp_wait<0>();
       __syncthreads();  // this chunk is there, the other one's buffer free
@@ -239,11 +264,8 @@ __global__ void __launch_bounds__(kThreads) long_forward_kernel(const __grid_con
         const int h = (warp % S::WH) * S::HPW + i;
         if (h < heads && row < rows) {
           const uint32_t at_head = h * dim * sizeof(T);
-          float s[2 * NP][4];
-          scores<T, DT, NP>(s, q0 + row * pitch + at_head, pass.array(c, 0, 2) + at_head, pitch, dim, pairs);
-          transform<NP>(s, sc, bias + h * a.buckets, index + row * L.pitch_idx, L.pitch_idx, pairs, keys);
-          soften<DT, NP>(f[i], s, pairs);
-          weigh<T, DT, NP, false>(f[i].acc, s, pass.array(c, 1, 2) + at_head, pitch, dim, pairs, keys);
+          attend_tile<T, DT, S::NT, false>(f[i], q0 + row * pitch + at_head, pass.array(c, 0, 2) + at_head, pass.array(c, 1, 2) + at_head, pitch, dim, sc,
+                                           bias + h * a.buckets, index + row * L.pitch_idx, L.pitch_idx, keys);
         }
       }
     }
@@ -277,14 +299,13 @@ static int allow_smem(dsvt_ctx* ctx, K kernel, uint32_t bytes) {
 template <typename T, int DT>
 int forward_of(dsvt_ctx* ctx, const SegArgs& a) {
   int limit = a.max_len <= kShort ? a.max_len : 64;
-  ShortLayout l = short_layout<T, DT>(a, limit, 3);
-  if (l.bytes > kSmemMost) l = short_layout<T, DT>(a, limit = 64, 3);
+  ShortLayout l = short_layout<T>(a, kHeads<T, DT>, limit, 3);
+  if (l.bytes > kSmemMost) l = short_layout<T>(a, kHeads<T, DT>, limit = 64, 3);
   const Scoring sc = scoring_of(a);
-  const unsigned groups = (unsigned)dsvt_ceil_div(a.heads, kHeads<T, DT>);
   auto kernel = short_forward_kernel<T, DT>;
   int rc = allow_smem(ctx, kernel, l.bytes);
   if (rc != DSVT_OK) return rc;
-  launch_pdl(kernel, dim3((unsigned)dsvt_ceil_div(a.n, kRowBlock), groups), dim3(kThreads), l.bytes, ctx->stream, a, l, sc);
+  launch_pdl(kernel, dim3((unsigned)dsvt_ceil_div(a.n, kRowBlock), (unsigned)dsvt_ceil_div(a.heads, kHeads<T, DT>)), dim3(kThreads), l.bytes, ctx->stream, a, l, sc);
   DSVT_LAUNCHED(ctx);
   if (limit >= a.max_len) return DSVT_OK;
   using S = LongShape<T, DT>;
@@ -292,7 +313,7 @@ int forward_of(dsvt_ctx* ctx, const SegArgs& a) {
   auto longer = long_forward_kernel<T, DT>;
   rc = allow_smem(ctx, longer, g.bytes);
   if (rc != DSVT_OK) return rc;
-  launch_pdl(longer, dim3((unsigned)dsvt_ceil_div(a.n, S::rows), groups), dim3(kThreads), g.bytes, ctx->stream, a, g, sc, limit);
+  launch_pdl(longer, dim3((unsigned)dsvt_ceil_div(a.n, S::rows), (unsigned)dsvt_ceil_div(a.heads, S::HG)), dim3(kThreads), g.bytes, ctx->stream, a, g, sc, limit);
   DSVT_LAUNCHED(ctx);
   return DSVT_OK;
 }

@@ -41,6 +41,11 @@ __device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t a) {
 __device__ __forceinline__ void ldsm2(uint32_t& r0, uint32_t& r1, uint32_t a) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x2.shared.b16 {%0,%1}, [%2];" : "=r"(r0), "=r"(r1) : "r"(a) : "memory");
 }
+__device__ __forceinline__ uint32_t ldsm1(uint32_t a) {
+  uint32_t r;
+  asm volatile("ldmatrix.sync.aligned.m8n8.x1.shared.b16 {%0}, [%1];" : "=r"(r) : "r"(a) : "memory");
+  return r;
+}
 __device__ __forceinline__ void ldsm4_t(uint32_t (&r)[4], uint32_t a) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a) : "memory");
 }
@@ -102,25 +107,20 @@ struct Mma<__half> {
   }
 };
 
-// Heads of a block, so that a row's part is 128 to 256 bytes: what one block reads of a row is whole sectors.
-template <typename T, int DT>
-constexpr int kHeads = DT * sizeof(T) <= 32 ? 8 : DT * sizeof(T) <= 64 ? 4 : DT * sizeof(T) <= 128 ? 2 : 1;
-// Pairs of 8 columns of a chunk of scores: what fits in registers beside the accumulators.
-template <typename T>
-constexpr int kPairs = sizeof(T) == 4 ? 3 : 4;
 // DT of 16, 24 and 32 are the channels of a head; 64 and 128 take any multiple of 8 up to them.
 template <int DT>
 constexpr bool kExact = DT <= 32;
 
-// C[i][j] for the 16 rows at a and `pairs` times 16 rows at b; both addresses are of a head's first channel, rows `pitch` bytes apart.
-template <typename T, int DT, int NP>
-__device__ __forceinline__ void scores(float (&c)[2 * NP][4], uint32_t a, uint32_t b, uint32_t pitch, int dim, int pairs) {
+// C[i][j] for the 16 rows at a and the 8 NT rows at b; both addresses are of a head's first channel, rows `pitch` bytes apart.
+template <typename T, int DT, int NT>
+__device__ __forceinline__ void scores(float (&c)[NT][4], uint32_t a, uint32_t b, uint32_t pitch, int dim) {
   const int lane = threadIdx.x & 31;
 #pragma unroll
-  for (int t = 0; t < 2 * NP; ++t) c[t][0] = c[t][1] = c[t][2] = c[t][3] = 0.f;
+  for (int t = 0; t < NT; ++t) c[t][0] = c[t][1] = c[t][2] = c[t][3] = 0.f;
   if constexpr (sizeof(T) == 2) {
     const uint32_t ra = a + (lane & 15) * pitch + (lane >> 4) * 16;
-    const uint32_t rb = b + ((lane & 7) + (lane >> 4) * 8) * pitch + ((lane >> 3) & 1) * 16;
+    const uint32_t rb = b + ((lane & 7) + (lane >> 4) * 8) * pitch + ((lane >> 3) & 1) * 16;  // (two tiles; the last of an odd number: its own)
+    const uint32_t rl = b + ((NT - 1) * 8 + (lane & 7)) * pitch + ((lane >> 3) & 1) * 16;
 #pragma unroll
     for (int k = 0; k < (DT + 15) / 16; ++k) {
       if (!kExact<DT> && k * 16 >= dim) break;
@@ -128,30 +128,40 @@ __device__ __forceinline__ void scores(float (&c)[2 * NP][4], uint32_t a, uint32
         uint32_t f[4];
         ldsm4(f, ra + k * 32);
 #pragma unroll
-        for (int p = 0; p < NP; ++p)
-          if (p < pairs) {
-            uint32_t g[4];
-            ldsm4(g, rb + p * 16 * pitch + k * 32);
-            Mma<T>::k16(c[2 * p], f[0], f[1], f[2], f[3], g[0], g[1]);
-            Mma<T>::k16(c[2 * p + 1], f[0], f[1], f[2], f[3], g[2], g[3]);
-          }
+        for (int p = 0; p < NT / 2; ++p) {
+          uint32_t g[4];
+          ldsm4(g, rb + p * 16 * pitch + k * 32);
+          Mma<T>::k16(c[2 * p], f[0], f[1], f[2], f[3], g[0], g[1]);
+          Mma<T>::k16(c[2 * p + 1], f[0], f[1], f[2], f[3], g[2], g[3]);
+        }
+        if (NT & 1) {
+          uint32_t g0, g1;
+          ldsm2(g0, g1, rl + k * 32);
+          Mma<T>::k16(c[NT - 1], f[0], f[1], f[2], f[3], g0, g1);
+        }
       } else {  // the last 8 channels
         uint32_t f0, f1;
         ldsm2(f0, f1, a + (lane & 15) * pitch + k * 32);
 #pragma unroll
-        for (int p = 0; p < NP; ++p)
-          if (p < pairs) {
-            uint32_t g0, g1;
-            ldsm2(g0, g1, b + (p * 16 + (lane & 15)) * pitch + k * 32);
-            Mma<T>::k8(c[2 * p], f0, f1, g0);
-            Mma<T>::k8(c[2 * p + 1], f0, f1, g1);
-          }
+        for (int p = 0; p < NT / 4; ++p) {
+          uint32_t g[4];
+          ldsm4(g, b + (p * 32 + lane) * pitch + k * 32);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) Mma<T>::k8(c[4 * p + i], f0, f1, g[i]);
+        }
+        if (NT & 2) {
+          uint32_t g0, g1;
+          ldsm2(g0, g1, b + (NT / 4 * 32 + (lane & 15)) * pitch + k * 32);
+          Mma<T>::k8(c[NT / 4 * 4], f0, f1, g0);
+          Mma<T>::k8(c[NT / 4 * 4 + 1], f0, f1, g1);
+        }
+        if (NT & 1) Mma<T>::k8(c[NT - 1], f0, f1, ldsm1(b + ((NT - 1) * 8 + (lane & 7)) * pitch + k * 32));
       }
     }
   } else {
-    float s[2 * NP][4];  // hi lo + lo hi
+    float s[NT][4];  // hi lo + lo hi
 #pragma unroll
-    for (int t = 0; t < 2 * NP; ++t) s[t][0] = s[t][1] = s[t][2] = s[t][3] = 0.f;
+    for (int t = 0; t < NT; ++t) s[t][0] = s[t][1] = s[t][2] = s[t][3] = 0.f;
     const uint32_t ra = a + (lane >> 2) * pitch + (lane & 3) * 4, rb = b + (lane >> 2) * pitch + (lane & 3) * 4;
 #pragma unroll
     for (int k = 0; k < DT / 8; ++k) {
@@ -160,65 +170,83 @@ __device__ __forceinline__ void scores(float (&c)[2 * NP][4], uint32_t a, uint32
 #pragma unroll
       for (int i = 0; i < 4; ++i) f[i] = split(lds(ra + (i & 1) * 8 * pitch + k * 32 + (i >> 1) * 16));
 #pragma unroll
-      for (int t = 0; t < 2 * NP; ++t)
-        if (t / 2 < pairs) {
-          const Parts g0 = split(lds(rb + t * 8 * pitch + k * 32)), g1 = split(lds(rb + t * 8 * pitch + k * 32 + 16));
-          mma_tf32(s[t], f[0].lo, f[1].lo, f[2].lo, f[3].lo, g0.hi, g1.hi);
-          mma_tf32(s[t], f[0].hi, f[1].hi, f[2].hi, f[3].hi, g0.lo, g1.lo);
-          mma_tf32(c[t], f[0].hi, f[1].hi, f[2].hi, f[3].hi, g0.hi, g1.hi);
-        }
+      for (int t = 0; t < NT; ++t) {
+        const Parts g0 = split(lds(rb + t * 8 * pitch + k * 32)), g1 = split(lds(rb + t * 8 * pitch + k * 32 + 16));
+        mma_tf32(s[t], f[0].lo, f[1].lo, f[2].lo, f[3].lo, g0.hi, g1.hi);
+        mma_tf32(s[t], f[0].hi, f[1].hi, f[2].hi, f[3].hi, g0.lo, g1.lo);
+        mma_tf32(c[t], f[0].hi, f[1].hi, f[2].hi, f[3].hi, g0.hi, g1.hi);
+      }
     }
 #pragma unroll
-    for (int t = 0; t < 2 * NP; ++t)
+    for (int t = 0; t < NT; ++t)
 #pragma unroll
       for (int e = 0; e < 4; ++e) c[t][e] += s[t][e];
   }
 }
 
-// acc += W B: W[i][j] over the `pairs` times 16 rows j at b.  Bit j of `real` says whether row j counts: what lies in the others is
-// not looked at, finite or not.  WIDE: W in tf32 (float16's gradients).
-template <typename T, int DT, int NP, bool WIDE>
-__device__ __forceinline__ void weigh(float (&acc)[DT / 8][4], const float (&w)[2 * NP][4], uint32_t b, uint32_t pitch, int dim, int pairs,
-                                      uint64_t real) {
+// acc += W B: W[i][j] over the 8 NT rows j at b.  Bit j of `real` says whether row j counts: what lies in the others is not looked at,
+// finite or not.  WIDE: W in tf32 (float16's gradients).
+template <typename T, int DT, int NT, bool WIDE>
+__device__ __forceinline__ void weigh(float (&acc)[DT / 8][4], const float (&w)[NT][4], uint32_t b, uint32_t pitch, int dim, uint64_t real) {
   const int lane = threadIdx.x & 31, q2 = (lane & 3) * 2;
   if constexpr (sizeof(T) == 2) {
-    const uint32_t rb = b + (lane & 15) * pitch + (lane >> 4) * 16;
 #pragma unroll
-    for (int p = 0; p < NP; ++p)
-      if (p < pairs) {
-        const uint32_t bits = (uint32_t)(real >> (16 * p)) & 0xffffu;
-        uint32_t m0 = kAll, m1 = kAll;
-        if (bits != 0xffffu) {
-          const uint32_t mine = bits >> q2;
-          m0 = ((mine & 1) ? 0xffffu : 0u) | ((mine & 2) ? 0xffff0000u : 0u);
-          m1 = ((mine & 0x100) ? 0xffffu : 0u) | ((mine & 0x200) ? 0xffff0000u : 0u);
+    for (int p = 0; p < (NT + 1) / 2; ++p) {  // 16 rows at a time, and the last 8 of an odd number of tiles
+      const bool half = 2 * p + 1 == NT;
+      const uint32_t bits = (uint32_t)(real >> (16 * p)) & (half ? 0xffu : 0xffffu);
+      const bool ragged = bits != (half ? 0xffu : 0xffffu);
+      uint32_t m0 = kAll, m1 = kAll;
+      if (ragged) {
+        const uint32_t mine = bits >> q2;
+        m0 = ((mine & 1) ? 0xffffu : 0u) | ((mine & 2) ? 0xffff0000u : 0u);
+        m1 = ((mine & 0x100) ? 0xffffu : 0u) | ((mine & 0x200) ? 0xffff0000u : 0u);
+      }
+      uint32_t a[4] = {};
+      if (!WIDE) {
+        a[0] = Mma<T>::pack(w[2 * p][0], w[2 * p][1]);
+        a[1] = Mma<T>::pack(w[2 * p][2], w[2 * p][3]);
+        if (!half) {
+          a[2] = Mma<T>::pack(w[2 * p + 1 < NT ? 2 * p + 1 : 0][0], w[2 * p + 1 < NT ? 2 * p + 1 : 0][1]);
+          a[3] = Mma<T>::pack(w[2 * p + 1 < NT ? 2 * p + 1 : 0][2], w[2 * p + 1 < NT ? 2 * p + 1 : 0][3]);
         }
-        uint32_t a[4];
+      }
+      auto tile = [&](int n, uint32_t b0, uint32_t b1) {
+        b0 &= m0;
+        b1 &= m1;
         if (!WIDE) {
-          a[0] = Mma<T>::pack(w[2 * p][0], w[2 * p][1]);
-          a[1] = Mma<T>::pack(w[2 * p][2], w[2 * p][3]);
-          a[2] = Mma<T>::pack(w[2 * p + 1][0], w[2 * p + 1][1]);
-          a[3] = Mma<T>::pack(w[2 * p + 1][2], w[2 * p + 1][3]);
-        }
-        auto tile = [&](int n, uint32_t b0, uint32_t b1) {
-          b0 &= m0;
-          b1 &= m1;
-          if (!WIDE) {
-            Mma<T>::k16(acc[n], a[0], a[1], a[2], a[3], b0, b1);
-          } else {  // eight rows each; their order in the product is that of the accumulators: 0, 2, 4, 6, 1, 3, 5, 7
-            const float2 u = __half22float2(*reinterpret_cast<const __half2*>(&b0)), v = __half22float2(*reinterpret_cast<const __half2*>(&b1));
-            mma_tf32(acc[n], tf32(w[2 * p][0]), tf32(w[2 * p][2]), tf32(w[2 * p][1]), tf32(w[2 * p][3]), __float_as_uint(u.x), __float_as_uint(u.y));
-            mma_tf32(acc[n], tf32(w[2 * p + 1][0]), tf32(w[2 * p + 1][2]), tf32(w[2 * p + 1][1]), tf32(w[2 * p + 1][3]), __float_as_uint(v.x), __float_as_uint(v.y));
+          if (half) Mma<T>::k8(acc[n], a[0], a[1], b0);
+          else Mma<T>::k16(acc[n], a[0], a[1], a[2], a[3], b0, b1);
+        } else {  // eight rows each; their order in the product is that of the accumulators: 0, 2, 4, 6, 1, 3, 5, 7
+          const float2 u = __half22float2(*reinterpret_cast<const __half2*>(&b0));
+          mma_tf32(acc[n], tf32(w[2 * p][0]), tf32(w[2 * p][2]), tf32(w[2 * p][1]), tf32(w[2 * p][3]), __float_as_uint(u.x), __float_as_uint(u.y));
+          if (!half) {
+            constexpr int last = NT - 1;
+            const int o = 2 * p + 1 < NT ? 2 * p + 1 : last;
+            const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&b1));
+            mma_tf32(acc[n], tf32(w[o][0]), tf32(w[o][2]), tf32(w[o][1]), tf32(w[o][3]), __float_as_uint(v.x), __float_as_uint(v.y));
           }
-        };
+        }
+      };
+      if (half) {
+        const uint32_t rb = b + (p * 16 + (lane & 7)) * pitch + ((lane >> 3) & 1) * 16;
+#pragma unroll
+        for (int n = 0; n < DT / 8; n += 2) {
+          if (!kExact<DT> && n * 8 >= dim) break;
+          uint32_t g0, g1;  // (behind the last channel: the next head's, or the end of the row, not used)
+          ldsm2_t(g0, g1, rb + n * 16);
+          tile(n, g0, 0u);
+          if (kExact<DT> ? n + 2 <= DT / 8 : n * 8 + 16 <= dim) tile(n + 1 < DT / 8 ? n + 1 : n, g1, 0u);
+        }
+      } else {
+        const uint32_t rb = b + (p * 16 + (lane & 15)) * pitch + (lane >> 4) * 16;
 #pragma unroll
         for (int n = 0; n < DT / 8; n += 2) {
           if (!kExact<DT> && n * 8 >= dim) break;
           if (kExact<DT> ? n + 2 <= DT / 8 : n * 8 + 16 <= dim) {
             uint32_t g[4];
-            ldsm4_t(g, rb + p * 16 * pitch + n * 16);
+            ldsm4_t(g, rb + n * 16);
             tile(n, g[0], g[1]);
-            tile(n + 1, g[2], g[3]);
+            tile(n + 1 < DT / 8 ? n + 1 : n, g[2], g[3]);
           } else {
             uint32_t g0, g1;
             ldsm2_t(g0, g1, b + (p * 16 + (lane & 15)) * pitch + n * 16);
@@ -226,11 +254,12 @@ __device__ __forceinline__ void weigh(float (&acc)[DT / 8][4], const float (&w)[
           }
         }
       }
+    }
   } else {
     const uint32_t rb = b + q2 * pitch + (lane >> 2) * 4;
-    Parts a[2 * NP][4];
+    Parts a[NT][4];
 #pragma unroll
-    for (int t = 0; t < 2 * NP; ++t) {
+    for (int t = 0; t < NT; ++t) {
       a[t][0] = split(w[t][0]);
       a[t][1] = split(w[t][2]);
       a[t][2] = split(w[t][1]);
@@ -241,15 +270,14 @@ __device__ __forceinline__ void weigh(float (&acc)[DT / 8][4], const float (&w)[
       if (!kExact<DT> && n * 8 >= dim) break;
       float c[4] = {}, s[4] = {};
 #pragma unroll
-      for (int t = 0; t < 2 * NP; ++t)
-        if (t / 2 < pairs) {
-          const uint32_t mine = (uint32_t)(real >> (8 * t)) >> q2;
-          const Parts g0 = split((mine & 1) ? lds(rb + t * 8 * pitch + n * 32) : 0.f);
-          const Parts g1 = split((mine & 2) ? lds(rb + (t * 8 + 1) * pitch + n * 32) : 0.f);
-          mma_tf32(s, a[t][0].lo, a[t][1].lo, a[t][2].lo, a[t][3].lo, g0.hi, g1.hi);
-          mma_tf32(s, a[t][0].hi, a[t][1].hi, a[t][2].hi, a[t][3].hi, g0.lo, g1.lo);
-          mma_tf32(c, a[t][0].hi, a[t][1].hi, a[t][2].hi, a[t][3].hi, g0.hi, g1.hi);
-        }
+      for (int t = 0; t < NT; ++t) {
+        const uint32_t mine = (uint32_t)(real >> (8 * t)) >> q2;
+        const float x0 = lds(rb + t * 8 * pitch + n * 32), x1 = lds(rb + (t * 8 + 1) * pitch + n * 32);
+        const Parts g0 = split((mine & 1) ? x0 : 0.f), g1 = split((mine & 2) ? x1 : 0.f);
+        mma_tf32(s, a[t][0].lo, a[t][1].lo, a[t][2].lo, a[t][3].lo, g0.hi, g1.hi);
+        mma_tf32(s, a[t][0].hi, a[t][1].hi, a[t][2].hi, a[t][3].hi, g0.lo, g1.lo);
+        mma_tf32(c, a[t][0].hi, a[t][1].hi, a[t][2].hi, a[t][3].hi, g0.hi, g1.hi);
+      }
 #pragma unroll
       for (int e = 0; e < 4; ++e) acc[n][e] += c[e] + s[e];
     }
