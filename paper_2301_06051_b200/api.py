@@ -264,6 +264,7 @@ class BucketBias:
             raise ValueError("index has 2 e - 1 entries for each extent e")
         if table.dim() != 2 or table.dtype != torch.float32:
             raise ValueError("a bias table is float32 [heads, buckets]")
+        self._index_at, self._extent = self.index.ctypes.data, (C.c_int32 * 3)(*self.extent)
 
 
 def log_buckets(extent: Sequence[int], near: Sequence[int], sides: Sequence[int]):
@@ -502,7 +503,7 @@ class Context:
             if seg.coords is None:
                 raise ValueError("a relative position bias needs the segments' coords")
             p.bias, p.buckets = _ptr(bias.table), bias.table.shape[1]
-            p.coords, p.bucket_of, p.extent = _int32(seg.coords, (n, 4)), bias.index.ctypes.data, bias.extent
+            p.coords, p.bucket_of, p.extent = _int32(seg.coords, (n, 4)), bias._index_at, bias._extent
         return p
 
     def segment_attention(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, seg: Segments,

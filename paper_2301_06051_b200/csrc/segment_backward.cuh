@@ -65,21 +65,6 @@ __device__ __forceinline__ float tally_value(long long hi, long long lo, float l
   return (float)(((double)hi + (double)lo * (1.0 / (1 << kLoBits))) * (1.0 / (1 << kHiBits)) * (double)limit);
 }
 
-template <int NT>
-__device__ __forceinline__ bool all_real(uint64_t real) { return real == (NT == 8 ? ~(uint64_t)0 : ((uint64_t)1 << (8 * NT & 63)) - 1); }
-
-// Columns that hold no row: products of whatever lies there do not count.
-template <int NT>
-__device__ __forceinline__ void clear_columns(float (&c)[NT][4], uint64_t real) {
-  if (all_real<NT>(real)) return;
-  const uint64_t mine = real >> ((threadIdx.x & 3) * 2);
-#pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    if (!(mine >> (8 * t) & 1)) c[t][0] = c[t][2] = 0.f;
-    if (!(mine >> (8 * t + 1) & 1)) c[t][1] = c[t][3] = 0.f;
-  }
-}
-
 // A tile's two rows of the first pass: maximum and sum as in Flow, D and the largest |p dp| before they are divided by the sum.
 struct RowSums {
   float m[2], l[2], d[2], most[2];
@@ -158,7 +143,7 @@ __device__ __forceinline__ void differ_columns(float (&s)[NT][4], float (&dp)[NT
         buckets_of(bk, index + t * 8, pitch);
       } else {
         const uint16_t* at = index + (t * 8 + q2) * pitch + g;
-        bk[0] = at[0]; bk[1] = at[pitch]; bk[2] = at[8]; bk[3] = at[pitch + 8];
+        bk[0] = at[0] & kBucketMask; bk[1] = at[pitch] & kBucketMask; bk[2] = at[8] & kBucketMask; bk[3] = at[pitch + 8] & kBucketMask;
       }
 #pragma unroll
       for (int e = 0; e < 4; ++e) b[e] = bias_at(bias, bk[e]);
@@ -174,7 +159,10 @@ __device__ __forceinline__ void differ_columns(float (&s)[NT][4], float (&dp)[NT
       const uint32_t mine = (uint32_t)(real >> (8 * t)) >> q2;
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        if (!((mine >> (e & 1)) & 1)) s[t][e] = dp[t][e] = slope[e] = 0.f;
+        if (!((mine >> (e & 1)) & 1)) {
+          s[t][e] = dp[t][e] = slope[e] = 0.f;
+          bk[e] = 0;  // (an unwritten bucket may lie outside of the table)
+        }
     }
     if (tally.on)
 #pragma unroll
@@ -226,7 +214,7 @@ template <typename T, int DT, int NT>
 __device__ __forceinline__ void products(float (&s)[NT][4], float (&dp)[NT][4], const Operands& x, uint64_t keys) {
   scores<T, DT, NT>(s, x.q, x.ck, x.pitch, x.dim);
   scores<T, DT, NT>(dp, x.o, x.cv, x.pitch, x.dim);
-  clear_columns<NT>(dp, keys);
+  set_columns<NT>(dp, keys, 0.f);  // (whatever lies there)
 }
 // A segment whose keys are one chunk: everything of the tile's rows at once.
 template <typename T, int DT, int NT>
@@ -284,7 +272,7 @@ static BackLayout back_layout(const SegArgs& a, int limit) {
   BackLayout l = {};
   l.s = short_layout<T>(a, kBackHeads<T, DT>, limit, 4);
   uint32_t at = l.s.bytes;
-  l.stats = at; at += l.s.heads * (kRowBlock + limit + 15) * 16;
+  l.stats = at; at += l.s.heads * (l.s.batch + 16) * 16;
   if (a.dbias) {
     l.hist = at; at += l.s.heads * 2 * a.buckets * 4;
     l.spoilt = at; at += (l.s.heads * a.buckets + 31) / 32 * 4;
@@ -306,7 +294,7 @@ __global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) short_backward_ker
   int4* cells = reinterpret_cast<int4*>(smem + L.s.cells);
   uint16_t* index = reinterpret_cast<uint16_t*>(smem + L.s.index);
   float4* stats = reinterpret_cast<float4*>(smem + L.stats);
-  const int stat_rows = kRowBlock + L.s.limit + 15;
+  const int stat_rows = L.s.batch + 16;
   const int head0 = blockIdx.y * HG, heads = min(HG, a.heads - head0);
   const uint32_t pitch = kExact<DT> ? HG * DT * sizeof(T) + 16 : L.s.pitch;
   const uint32_t q0 = smem_u32(smem + L.s.rows), k0 = q0 + L.s.array, v0 = k0 + L.s.array, o0 = v0 + L.s.array;
@@ -317,8 +305,6 @@ __global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) short_backward_ker
   tally.on = a.dbias != nullptr;
   tally.bound(0.f);
   stage_tables(a, maps, bias, head0, HG);
-  if (a.bias)
-    for (int i = threadIdx.x; i < L.s.index_words; i += kThreads) reinterpret_cast<uint32_t*>(index)[i] = 0;
   float* mine = work.partial + (int64_t)blockIdx.x * work.table + head0 * a.buckets;
   if (tally.on) {
     for (int i = threadIdx.x; i < HG * 2 * a.buckets; i += kThreads) tally.hist[i] = 0;
@@ -354,9 +340,9 @@ __global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) short_backward_ker
   x.pitch_idx = L.s.pitch_idx; x.pitch = pitch; x.dim = dim;
   for (int block = blockIdx.x; block < blocks; block += gridDim.x) {
     __syncthreads();
+    make_plan(a, plan, block, blocks, L.s.limit);
+    while (next_batch(a, plan, cells, block, L.s.batch)) {
     if (threadIdx.x == 0) block_bound = 0;
-    make_plan(a, plan, cells, block, blocks, L.s.limit);
-    if (plan.items == 0) continue;
     load_rows<T, 4>(q0, L.s.array, pitch, src, plan.ids, plan.rows, chunks, real);
     cp_commit();
     if (a.bias) fill_index(a, plan, cells, maps, index, L.s.pitch_idx);
@@ -452,6 +438,9 @@ __global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) short_backward_ker
         store_rows<T, DT>(dk, a.scale, a.dk, a.ld_dk, col + h * dim, dim, id0, id1);
         store_rows<T, DT>(dv, 1.f, a.dv, a.ld_dv, col + h * dim, dim, id0, id1);
       }
+    }
+    if (plan.next == kRowBlock) break;
+    __syncthreads();
     }
   }
   if (tally.on) {
@@ -744,8 +733,8 @@ int backward_of(dsvt_ctx* ctx, const SegArgs& a) {
   if (w.table > 0 && stay > (int64_t)kPartialWords / w.table) stay = kPartialWords / w.table;
   if (stay > blocks) stay = blocks;
   w.blocks = (int)stay;
-  auto kernel = short_backward_kernel<T, DT>;
-  int rc = allow_smem(ctx, kernel, l.bytes);
+  constexpr auto kernel = short_backward_kernel<T, DT>;
+  int rc = allow_smem<kernel>(ctx);
   if (rc != DSVT_OK) return rc;
   launch_pdl(kernel, dim3((unsigned)stay, groups), dim3(kThreads), l.bytes, ctx->stream, a, l, sc, w, blocks);
   DSVT_LAUNCHED(ctx);
@@ -753,9 +742,9 @@ int backward_of(dsvt_ctx* ctx, const SegArgs& a) {
   if (longer) {
     using S = BackShape<T, DT>;
     const BackLongLayout lq = back_long_layout<T, DT>(a, false), lk = back_long_layout<T, DT>(a, true);
-    auto by_queries = long_backward_kernel<T, DT, false>;
-    auto by_keys = long_backward_kernel<T, DT, true>;
-    if ((rc = allow_smem(ctx, by_queries, lq.bytes)) != DSVT_OK || (rc = allow_smem(ctx, by_keys, lk.bytes)) != DSVT_OK) return rc;
+    constexpr auto by_queries = long_backward_kernel<T, DT, false>;
+    constexpr auto by_keys = long_backward_kernel<T, DT, true>;
+    if ((rc = allow_smem<by_queries>(ctx)) != DSVT_OK || (rc = allow_smem<by_keys>(ctx)) != DSVT_OK) return rc;
     // as many heads to a launch as the workspace has room for the statistics of, whole blocks' if it can be
     int64_t at_once = stat_words / ((int64_t)3 * a.n);
     if (at_once < 1) return DSVT_ERR_CAPACITY;

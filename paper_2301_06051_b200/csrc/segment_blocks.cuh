@@ -8,18 +8,20 @@ namespace dsvt_train {
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kRowBlock = 32;
 constexpr int kShort = 128;                         // most rows of a segment that is held whole
-constexpr int kMaxRows = kRowBlock - 1 + kShort;    // rows of a block
+constexpr int kBatch = 48;                          // rows in shared memory at a time, or the longest segment's if that is more
 constexpr int kMaxItems = kRowBlock * (kShort / 16);
 
-// 16 rows of a segment: its first row's place in the block, its length, the tile.
+// 16 rows of a segment: its first row's place in the batch, its length, the tile.
 struct Item { uint8_t at, len, tile, pad; };
 
+// A block's segments, and the batch of them in shared memory: mostly all of them, else as many as fit.
 struct Plan {
-  int rows, items, pairs;  // (pairs: of queries and keys)
-  uint32_t starts;                        // bit i: a segment starts at place i
-  uint8_t len_at[kRowBlock];
-  uint32_t real[(kMaxRows + 31) / 32 + 3];  // bit i: place i holds a voxel
-  int32_t ids[kMaxRows + 17];
+  int rows, items, pairs, next;        // of the batch (pairs: of queries and keys); where the next batch starts
+  int first;                           // the batch's first row, from the block's
+  uint32_t starts;                     // bit i: a segment starts at place i
+  uint8_t len_at[kRowBlock];           // by row of the block: length of the segment that starts there
+  uint32_t real[kShort / 32 + 3];      // bit i: place i holds a voxel
+  int32_t ids[kShort];
   Item item[kMaxItems];
 };
 
@@ -59,47 +61,63 @@ __device__ __forceinline__ int bucket_at(const BucketMaps& m, const uint16_t* ma
   return maps[dx] + maps[dy] + maps[dz];  // (the maps in shared memory hold four times the index: a bias's offset)
 }
 
-// The block's segments (of at most `limit` rows), their rows' voxels and the list of their tiles.
-__device__ __forceinline__ void make_plan(const SegArgs& a, Plan& p, int4* cells, int block, int blocks, int limit) {
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, base = block * kRowBlock;
+// Finds the block's segments, of at most `limit` rows.
+__device__ __forceinline__ void make_plan(const SegArgs& a, Plan& p, int block, int blocks, int limit) {
+  const int tid = threadIdx.x, base = block * kRowBlock;
   if (tid < kRowBlock) p.len_at[tid] = 0;
+  if (tid == 0) p.next = 0;
   const int2 near = segments_near(a, base, base + kRowBlock, block == 0, block == blocks - 1);
-  __syncthreads();
   for (int s = near.x + tid; s < near.y; s += kThreads) {
     const int lo = a.seg_start[s], hi = a.seg_start[s + 1];
     if (segment_sound(a, lo, hi) && hi - lo <= limit && lo >= base && lo < base + kRowBlock) p.len_at[lo - base] = (uint8_t)(hi - lo);
   }
   __syncthreads();
+}
+
+// The next batch of the block's segments, of at most `most` rows together: their rows' voxels and cells and the list of their tiles.
+// False if there are no more.  A barrier comes before.
+__device__ __forceinline__ bool next_batch(const SegArgs& a, Plan& p, int4* cells, int block, int most) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   if (warp == 0) {
-    const int len = p.len_at[lane], tiles = (len + 15) >> 4;
-    const uint32_t starts = __ballot_sync(kAll, len > 0);
-    int rows = len > 0 ? lane + len : 0, upto = tiles, pairs = len * len;
+    const int len = p.len_at[lane];
+    const uint32_t left = __ballot_sync(kAll, len > 0 && lane >= p.next);
+    const int first = __ffs(left) - 1, at = lane - first;
+    const bool in = (left >> lane & 1) && at + len <= most;
+    const uint32_t taken = __ballot_sync(kAll, in), rest = left & ~taken;
+    const int tiles = in ? (len + 15) >> 4 : 0;
+    int rows = in ? at + len : 0, upto = tiles, pairs = in ? len * len : 0;
     for (int m = 1; m < 32; m <<= 1) {
       rows = max(rows, __shfl_xor_sync(kAll, rows, m));
       pairs += __shfl_xor_sync(kAll, pairs, m);
       const int before = __shfl_up_sync(kAll, upto, m);
       if (lane >= m) upto += before;
     }
-    for (int t = 0; t < tiles; ++t) p.item[upto - tiles + t] = Item{(uint8_t)lane, (uint8_t)len, (uint8_t)t, 0};
+    for (int t = 0; t < tiles; ++t) p.item[upto - tiles + t] = Item{(uint8_t)at, (uint8_t)len, (uint8_t)t, 0};
     if (lane == 31) p.items = upto;
-    if (lane == 0) { p.rows = rows; p.pairs = pairs; p.starts = starts; }
+    if (lane == 0) {
+      p.rows = rows;
+      p.pairs = pairs;
+      p.first = first;
+      p.starts = left ? taken >> first : 0u;
+      p.next = rest ? __ffs(rest) - 1 : kRowBlock;
+    }
   }
   __syncthreads();
-  const int rows = p.rows;
-  const uint32_t starts = p.starts;
+  if (p.items == 0) return false;
   if (tid < (int)(sizeof(p.real) / 4) * 32) {
     int id = -1;
-    const uint32_t upto = starts & (tid >= 31 ? kAll : (2u << tid) - 1u);
-    if (tid < rows && upto) {
+    const uint32_t upto = p.starts & (tid >= 31 ? kAll : (2u << tid) - 1u);
+    if (tid < p.rows && upto) {
       const int at = 31 - __clz(upto);
-      if (tid < at + p.len_at[at]) id = voxel_at(a, base + tid);
+      if (tid < at + p.len_at[p.first + at]) id = voxel_at(a, block * kRowBlock + p.first + tid);
     }
     const uint32_t real = __ballot_sync(kAll, id >= 0);
     if (lane == 0) p.real[warp] = real;
-    if (tid < kMaxRows + 17) p.ids[tid] = id;
+    if (tid < kShort) p.ids[tid] = id;
     if (a.bias && id >= 0) cells[tid] = a.coords[id];
   }
   __syncthreads();
+  return true;
 }
 
 // Bit j: place at + j (j < count <= 64) holds a voxel.
@@ -113,19 +131,18 @@ __device__ __forceinline__ uint64_t real_rows(const Plan& p, int at, int count) 
 
 // Entries to a row of the bucket tile, for segments of at most `cols` rows: rows of an odd multiple of 16 bytes, so that the eight
 // rows of a score tile's fragment lie in different banks.
-__host__ __device__ constexpr int index_pitch(int cols) { return 8 * (((cols + 15) / 16 * 2) | 1); }
+__host__ __device__ constexpr int index_pitch(int cols) { return 8 * (((cols + 7) / 8) | 1); }
 
-// The buckets of all pairs of the block: index[i][j - first of i's segment].  Columns behind a segment's end stay at 0 or
-// whatever bucket an earlier one left there.
+// The buckets (times 4) of all pairs of the batch: index[i][j - first of i's segment].  The rest of the tile is never written.
 __device__ __forceinline__ void fill_index(const SegArgs& a, const Plan& p, const int4* cells, const uint16_t* maps, uint16_t* index, int pitch) {
-  const int lane = threadIdx.x & 31;
-  for (int i = threadIdx.x >> 5; i < p.rows; i += kWarps) {
+  const int part = threadIdx.x & 15;
+  for (int i = threadIdx.x >> 4; i < p.rows; i += kThreads / 16) {
     const uint32_t upto = p.starts & (i >= 31 ? kAll : (2u << i) - 1u);
-    const int at = upto ? 31 - __clz(upto) : 0, len = p.len_at[at];
+    const int at = upto ? 31 - __clz(upto) : 0, len = p.len_at[p.first + at];
     if (i >= at + len || p.ids[i] < 0) continue;
     const int4 mine = cells[i];
-    for (int j = lane; j < len; j += 32)
-      if (p.ids[at + j] >= 0) index[i * pitch + j] = (uint16_t)bucket_at(a.maps, maps, mine, cells[at + j]);
+#pragma unroll 3
+    for (int j = part; j < len; j += 16) index[i * pitch + j] = (uint16_t)bucket_at(a.maps, maps, mine, cells[at + j]);
   }
 }
 
@@ -163,12 +180,14 @@ __device__ __forceinline__ void store2(T* to, float x, float y) {
   else *reinterpret_cast<uint32_t*>(to) = Mma<T>::pack(x, y);
 }
 
+constexpr uint32_t kBucketMask = 4 * (kMaxBuckets - 1);
 // The buckets of a tile's four pairs, times 4; `index`: at its first row and column.
 __device__ __forceinline__ void buckets_of(int (&bk)[4], const uint16_t* index, int pitch) {
   const int lane = threadIdx.x & 31;
   const uint16_t* at = index + (lane >> 2) * pitch + (lane & 3) * 2;
   const uint32_t i0 = *reinterpret_cast<const uint32_t*>(at), i1 = *reinterpret_cast<const uint32_t*>(at + 8 * pitch);
-  bk[0] = i0 & 0xffff; bk[1] = i0 >> 16; bk[2] = i1 & 0xffff; bk[3] = i1 >> 16;
+  // (kept in range: where a row or column of the tile lies beyond the segment, nothing may have been written)
+  bk[0] = i0 & kBucketMask; bk[1] = i0 >> 16 & kBucketMask; bk[2] = i1 & kBucketMask; bk[3] = i1 >> 16 & kBucketMask;
 }
 __device__ __forceinline__ float bias_at(const float* bias, int bk) { return *reinterpret_cast<const float*>(reinterpret_cast<const char*>(bias) + bk); }
 
@@ -196,6 +215,24 @@ __device__ __forceinline__ void score_tile(float (&s)[4], float (&slope)[4], con
   }
 }
 
+// Sets the columns that hold no row.  Without gaps only the last tile has some.
+template <int NT>
+__device__ __forceinline__ void set_columns(float (&c)[NT][4], uint64_t real, float to) {
+  constexpr uint64_t before = ((uint64_t)1 << (8 * (NT - 1))) - 1;
+  const int q2 = (threadIdx.x & 3) * 2;
+  if ((real & before) != before) {
+    const uint64_t mine = real >> q2;
+#pragma unroll
+    for (int t = 0; t < NT - 1; ++t) {
+      if (!(mine >> (8 * t) & 1)) c[t][0] = c[t][2] = to;
+      if (!(mine >> (8 * t + 1) & 1)) c[t][1] = c[t][3] = to;
+    }
+  }
+  const uint32_t last = (uint32_t)(real >> (8 * (NT - 1))) >> q2;
+  if (!(last & 1)) c[NT - 1][0] = c[NT - 1][2] = to;
+  if (!(last & 2)) c[NT - 1][1] = c[NT - 1][3] = to;
+}
+
 // `index`: the fragment's first row's buckets at the chunk's first column (rows g and g + 8 of the tile).
 template <int NT>
 __device__ __forceinline__ void transform(float (&s)[NT][4], const Scoring& sc, const float* bias, const uint16_t* index, int pitch, uint64_t real) {
@@ -213,14 +250,7 @@ __device__ __forceinline__ void transform(float (&s)[NT][4], const Scoring& sc, 
   float none[4];
 #pragma unroll
   for (int t = 0; t < NT; ++t) score_of<false>(sc, s[t], b[t], none);
-  if (real != (NT == 8 ? ~(uint64_t)0 : ((uint64_t)1 << (8 * NT & 63)) - 1)) {
-    const uint64_t mine = real >> ((threadIdx.x & 3) * 2);
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      if (!(mine >> (8 * t) & 1)) s[t][0] = s[t][2] = -INFINITY;
-      if (!(mine >> (8 * t + 1) & 1)) s[t][1] = s[t][3] = -INFINITY;
-    }
-  }
+  set_columns<NT>(s, real, -INFINITY);
 }
 
 __device__ __forceinline__ float quad_max(float v) {

@@ -1,16 +1,18 @@
 // Segment attention, forward: softmax(q k^T + bias) v inside each segment.
 #pragma once
+#include <atomic>
+
 #include "segment_blocks.cuh"
 
 namespace dsvt_train {
 
-// Heads of a block that holds its segments whole: rows of at most 400 bytes, which leaves room for two blocks of 36-voxel sets.
+// Heads of a block that holds its segments whole: rows of at most 400 bytes, which leaves room for three blocks of 36-voxel sets.
 template <typename T, int DT>
 constexpr int kHeads = DT * sizeof(T) <= 48 ? 8 : DT * sizeof(T) <= 96 ? 4 : DT * sizeof(T) <= 128 ? 2 : 1;
 
 struct ShortLayout {
-  int heads;                                   // of a block
-  int pitch_idx, limit, index_words;           // entries to a row of the bucket tile; longest segment; the bucket tile's size
+  int heads, batch;                            // of a block; rows at a time
+  int pitch_idx, limit;                        // entries to a row of the bucket tile; longest segment
   uint32_t pitch, array;                       // bytes of a row and of an array of rows
   uint32_t maps, bias, cells, index, rows, bytes;
 };
@@ -20,22 +22,22 @@ static ShortLayout short_layout(const SegArgs& a, int heads, int limit, int arra
   ShortLayout l = {};
   l.heads = heads;
   l.limit = limit;
-  const int rows = kRowBlock - 1 + limit;
+  l.batch = limit > kBatch ? limit : kBatch;
   l.pitch = (uint32_t)(heads * a.dim * sizeof(T) + 16);
-  l.array = rows * l.pitch;
+  l.array = l.batch * l.pitch;
   uint32_t at = (sizeof(Plan) + 15) / 16 * 16;
   auto take = [&](size_t bytes) { const uint32_t was = at; at += (uint32_t)((bytes + 15) / 16 * 16); return was; };
   if (a.bias) {
-    l.maps = take(sizeof(a.maps.of));
-    l.bias = take((size_t)heads * a.buckets * 4);
-    l.cells = take((size_t)rows * 16);
+    l.maps = take((size_t)(a.maps.at_z + 2 * a.maps.extent[2] - 1) * 2);
+    l.cells = take((size_t)l.batch * 16);
     l.pitch_idx = index_pitch(limit);
-    l.index_words = (rows + 16) * l.pitch_idx / 2 + 32;
-    l.index = take((size_t)l.index_words * 4);
+    l.index = take(((size_t)(l.batch + 16) * l.pitch_idx + 64) * 2);
+    l.bias = take((size_t)heads * a.buckets * 4);  // (a look-up of an unwritten bucket ends within 4 KB of a head's first: the rows follow)
   }
-  // A tile of 16 rows may begin at an array's last row, and segments of more than 40 rows go in chunks of up to 40: what follows the
-  // rows is read, and not used.
+  // A tile of 16 rows may begin at an array's last row, and longer segments go in chunks of up to 40: what follows the rows is read,
+  // and not used.
   l.rows = take((size_t)arrays * l.array + (limit <= 40 ? 16 : 40) * l.pitch);
+  if (at - l.rows < 4096) at = l.rows + 4096;
   l.bytes = at;
   return l;
 }
@@ -52,7 +54,7 @@ __device__ __forceinline__ void attend_tile(Flow<DT>& f, uint32_t q, uint32_t k,
 }
 
 template <typename T, int DT>
-__global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) short_forward_kernel(const __grid_constant__ SegArgs a, const ShortLayout L, const Scoring sc) {
+__global__ void __launch_bounds__(kThreads, DT <= 24 && sizeof(T) == 2 ? 3 : DT <= 32 ? 2 : 1) short_forward_kernel(const __grid_constant__ SegArgs a, const ShortLayout L, const Scoring sc) {
   extern __shared__ __align__(16) unsigned char smem[];
   constexpr int HG = kHeads<T, DT>;
   const int dim = kExact<DT> ? DT : a.dim;
@@ -65,20 +67,26 @@ __global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) short_forward_kern
   const int head0 = blockIdx.y * HG, heads = min(HG, a.heads - head0);
   const uint32_t pitch = kExact<DT> ? HG * DT * sizeof(T) + 16 : L.pitch;
   const uint32_t q0 = smem_u32(smem + L.rows), k0 = q0 + L.array, v0 = k0 + L.array;
-  stage_tables(a, maps, bias, head0, HG);
-  if (a.bias)
-    for (int i = threadIdx.x; i < L.index_words; i += kThreads) reinterpret_cast<uint32_t*>(index)[i] = 0;
-  make_plan(a, plan, cells, blockIdx.x, gridDim.x, L.limit);
+  make_plan(a, plan, blockIdx.x, gridDim.x, L.limit);
   const int chunks = HG * dim * (int)sizeof(T) / 16, real = heads * dim * (int)sizeof(T) / 16;
   const int64_t col = (int64_t)head0 * dim;
   const Rows<3> src = {{first_head<T>(a.q, col), first_head<T>(a.k, col), first_head<T>(a.v, col)},
                        {a.ld_q * (int64_t)sizeof(T), a.ld_k * (int64_t)sizeof(T), a.ld_v * (int64_t)sizeof(T)}};
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, h = warp % HG;
+  bool staged = false;
+  while (next_batch(a, plan, cells, blockIdx.x, L.batch)) {
   load_rows<T, 3>(q0, L.array, pitch, src, plan.ids, plan.rows, chunks, real);
   cp_commit();
-  if (a.bias) fill_index(a, plan, cells, maps, index, L.pitch_idx);
+  if (a.bias) {
+    if (!staged) {  // (while the rows are on their way)
+      stage_tables(a, maps, bias, head0, HG);
+      __syncthreads();
+      staged = true;
+    }
+    fill_index(a, plan, cells, maps, index, L.pitch_idx);
+  }
   cp_wait<0>();
   __syncthreads();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, h = warp % HG;
   if (h < heads) {
     const uint32_t at_head = h * dim * sizeof(T);
     const float* mine = bias + h * a.buckets;
@@ -123,6 +131,9 @@ __global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) short_forward_kern
     char* to = (char*)a.out + (id * a.ld_out + col) * (int64_t)sizeof(T);
 #pragma unroll 4
     for (int c = part; c < real; c += 8) *reinterpret_cast<uint4*>(to + c * 16) = *reinterpret_cast<const uint4*>(smem + L.rows + r * pitch + c * 16);
+  }
+  if (plan.next == kRowBlock) break;
+  __syncthreads();
   }
 }
 
@@ -288,11 +299,16 @@ __global__ void __launch_bounds__(kThreads) long_forward_kernel(const __grid_con
 
 // Up to kShort rows a segment is held whole where that leaves room for two blocks on an SM, or at least for one; in calls with longer
 // ones up to 64 rows, and the longer ones go through in tiles.
-constexpr uint32_t kSmemMost = 227 * 1024;
+constexpr uint32_t kSmemMost = 226 * 1024;  // (of 227 KB; the rest for what kernels declare themselves)
 
-template <typename K>
-static int allow_smem(dsvt_ctx* ctx, K kernel, uint32_t bytes) {
-  if (bytes > 48 * 1024) DSVT_CUDA_TRY(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+// (once per kernel and device: the call costs more than a launch's share of it)
+template <auto kernel>
+static int allow_smem(dsvt_ctx* ctx) {
+  static std::atomic<uint64_t> done{0};
+  const uint64_t bit = (uint64_t)1 << (ctx->device & 63);
+  if (ctx->device < 64 && (done.load(std::memory_order_relaxed) & bit)) return DSVT_OK;
+  DSVT_CUDA_TRY(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemMost));
+  done.fetch_or(bit, std::memory_order_relaxed);
   return DSVT_OK;
 }
 
@@ -302,16 +318,16 @@ int forward_of(dsvt_ctx* ctx, const SegArgs& a) {
   ShortLayout l = short_layout<T>(a, kHeads<T, DT>, limit, 3);
   if (l.bytes > kSmemMost) l = short_layout<T>(a, kHeads<T, DT>, limit = 64, 3);
   const Scoring sc = scoring_of(a);
-  auto kernel = short_forward_kernel<T, DT>;
-  int rc = allow_smem(ctx, kernel, l.bytes);
+  constexpr auto kernel = short_forward_kernel<T, DT>;
+  int rc = allow_smem<kernel>(ctx);
   if (rc != DSVT_OK) return rc;
   launch_pdl(kernel, dim3((unsigned)dsvt_ceil_div(a.n, kRowBlock), (unsigned)dsvt_ceil_div(a.heads, kHeads<T, DT>)), dim3(kThreads), l.bytes, ctx->stream, a, l, sc);
   DSVT_LAUNCHED(ctx);
   if (limit >= a.max_len) return DSVT_OK;
   using S = LongShape<T, DT>;
   const LongLayout g = long_layout<T, DT>(a, 1, 2, 0);
-  auto longer = long_forward_kernel<T, DT>;
-  rc = allow_smem(ctx, longer, g.bytes);
+  constexpr auto longer = long_forward_kernel<T, DT>;
+  rc = allow_smem<longer>(ctx);
   if (rc != DSVT_OK) return rc;
   launch_pdl(longer, dim3((unsigned)dsvt_ceil_div(a.n, S::rows), (unsigned)dsvt_ceil_div(a.heads, S::HG)), dim3(kThreads), g.bytes, ctx->stream, a, g, sc, limit);
   DSVT_LAUNCHED(ctx);
