@@ -32,10 +32,16 @@ struct BackWork {
   int32_t table, blocks, head0, head_end, n;  // (heads of a launch of the long ones)
 };
 
-// A value beyond the limit (which the two passes' roundings of large scores may leave there), or not finite.
-static __device__ __noinline__ void odd_value(int* at, uint32_t* spoilt, int entry, float v) {
-  if (isfinite(v)) atomicAdd(at, v > 0.f ? 1 << kHiBits : -(1 << kHiBits));
-  else atomicOr(spoilt + (entry >> 5), 1u << (entry & 31));
+// A value that need not be within the limit (the two passes' roundings of large scores may leave one beyond it), nor finite.
+static __device__ __noinline__ void odd_value(int* at, uint32_t* spoilt, int entry, float v, float limit, float to_hi, int buckets) {
+  if (!isfinite(v)) {
+    atomicOr(spoilt + (entry >> 5), 1u << (entry & 31));
+    return;
+  }
+  v = fminf(fmaxf(v, -limit), limit);
+  const float t = fmaf(v, to_hi, kMagic), r = fmaf(v, to_hi, -(t - kMagic)), u = fmaf(r, (float)(1 << kLoBits), kMagic);
+  atomicAdd(at, __float_as_int(t) - __float_as_int(kMagic));
+  atomicAdd(at + buckets, __float_as_int(u) - __float_as_int(kMagic));
 }
 
 struct Tally {
@@ -50,13 +56,24 @@ struct Tally {
     limit = __int_as_float((e + 127) << 23);
     to_hi = __int_as_float((kHiBits - e + 127) << 23);
   }
-  // (bk: the bucket times 4)
-  __device__ __forceinline__ void add(int h, int bk, float v) const {
-    int* at = reinterpret_cast<int*>(reinterpret_cast<char*>(hist + 2 * h * buckets) + bk);
-    if (!(fabsf(v) <= limit)) { odd_value(at, spoilt, h * buckets + (bk >> 2), v); return; }
-    const float t = fmaf(v, to_hi, kMagic), r = fmaf(v, to_hi, -(t - kMagic)), u = fmaf(r, (float)(1 << kLoBits), kMagic);
-    atomicAdd(at, __float_as_int(t) - __float_as_int(kMagic));
-    atomicAdd(at + buckets, __float_as_int(u) - __float_as_int(kMagic));
+  // Two values; x, y: their buckets times 4.
+  __device__ __forceinline__ void add2(int h, int x, int y, float v, float w) const {
+    char* base = reinterpret_cast<char*>(hist + 2 * h * buckets);
+    int *to = reinterpret_cast<int*>(base + x), *tu = reinterpret_cast<int*>(base + y);
+    if (!(fmaxf(fabsf(v), fabsf(w)) <= limit) || v != v || w != w) {  // (a maximum passes over a NaN)
+      odd_value(to, spoilt, h * buckets + (x >> 2), v, limit, to_hi, buckets);
+      odd_value(tu, spoilt, h * buckets + (y >> 2), w, limit, to_hi, buckets);
+      return;
+    }
+    const F2 z = pair(v, w), scale = pair(to_hi, to_hi), magic = pair(kMagic, kMagic);
+    const F2 t = fma2(z, scale, magic), minus = pair(-1.f, -1.f);
+    const F2 r = fma2(z, scale, mul(add(t, pair(-kMagic, -kMagic)), minus));
+    const F2 u = fma2(r, pair((float)(1 << kLoBits), (float)(1 << kLoBits)), magic);
+    const int zero = __float_as_int(kMagic);
+    atomicAdd(to, __float_as_int(parts(t).x) - zero);
+    atomicAdd(to + buckets, __float_as_int(parts(u).x) - zero);
+    atomicAdd(tu, __float_as_int(parts(t).y) - zero);
+    atomicAdd(tu + buckets, __float_as_int(parts(u).y) - zero);
   }
 };
 
@@ -84,18 +101,20 @@ __device__ __forceinline__ void sum_rows(RowSums& f, float (&s)[NT][4], const fl
     m = quad_max(m);
     const float base = m == -INFINITY ? 0.f : m, fade = ex2_approx(f.m[r] - base);
     f.m[r] = m;
-    float l = f.l[r] * fade, d = f.d[r] * fade, most = f.most[r] * fade;
+    const F2 down = pair(-base, -base);
+    F2 l = pair(f.l[r] * fade, 0.f), d = pair(f.d[r] * fade, 0.f);
+    float most = f.most[r] * fade;
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-      for (int e = 2 * r; e < 2 * r + 2; ++e) {
-        s[t][e] = ex2_approx(s[t][e] - base);
-        l += s[t][e];
-        const float x = s[t][e] * dp[t][e];
-        d += x;
-        most = fmaxf(most, fabsf(x));
-      }
-    f.l[r] = l; f.d[r] = d; f.most[r] = most;
+    for (int t = 0; t < NT; ++t) {
+      const float2 x = parts(add(two(s[t], 2 * r), down));
+      s[t][2 * r] = ex2_approx(x.x);
+      s[t][2 * r + 1] = ex2_approx(x.y);
+      const F2 p = two(s[t], 2 * r), y = mul(p, two(dp[t], 2 * r));
+      l = add(l, p);
+      d = add(d, y);
+      most = fmaxf(most, fmaxf(fabsf(parts(y).x), fabsf(parts(y).y)));
+    }
+    f.l[r] = sum_of(l); f.d[r] = sum_of(d); f.most[r] = most;
   }
 }
 // Row r's maximum, 1 / sum and D, and the bound of its |ds| (0 where it is not finite: such values are counted apart).
@@ -110,9 +129,11 @@ __device__ __forceinline__ float3 row_stats(const RowSums& f, int r, float* boun
 template <int NT>
 __device__ __forceinline__ void differ_weights(const float (&s)[NT][4], float (&dp)[NT][4], const float3 (&st)[2]) {
 #pragma unroll
-  for (int t = 0; t < NT; ++t)
+  for (int r = 0; r < 2; ++r) {
+    const F2 inv = pair(st[r].y, st[r].y), D = pair(-st[r].z, -st[r].z);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) dp[t][e] = s[t][e] * st[e >> 1].y * (dp[t][e] - st[e >> 1].z);
+    for (int t = 0; t < NT; ++t) put(dp[t], 2 * r, mul(mul(two(s[t], 2 * r), inv), add(two(dp[t], 2 * r), D)));
+  }
 }
 
 // The same from products, s = q k.
@@ -124,15 +145,33 @@ __device__ __forceinline__ void differ_rows(float (&s)[NT][4], float (&dp)[NT][4
     float slope[4];
     score_tile<true>(s[t], slope, sc, bias, index + t * 8, pitch, (uint32_t)(real >> (8 * t)));
 #pragma unroll
-    for (int e = 0; e < 4; ++e) dp[t][e] = ex2_approx(s[t][e] - st[e >> 1].x) * st[e >> 1].y * (dp[t][e] - st[e >> 1].z) * slope[e];
+    for (int r = 0; r < 2; ++r) {
+      const float2 x = parts(add(two(s[t], 2 * r), pair(-st[r].x, -st[r].x)));
+      const F2 p = mul(pair(ex2_approx(x.x), ex2_approx(x.y)), pair(st[r].y, st[r].y));
+      F2 dz = mul(p, add(two(dp[t], 2 * r), pair(-st[r].z, -st[r].z)));
+      if (sc.cap != 0.f) dz = mul(dz, two(slope, 2 * r));
+      put(dp[t], 2 * r, dz);
+    }
+    // (a column without a key: its weight is zero, but a product of what lies there need not be a number)
+    if (((uint32_t)(real >> (8 * t)) & 0xffu) != 0xffu) {
+      const uint32_t mine = (uint32_t)(real >> (8 * t)) >> ((threadIdx.x & 3) * 2);
+      if (!(mine & 1)) dp[t][0] = dp[t][2] = 0.f;
+      if (!(mine & 2)) dp[t][1] = dp[t][3] = 0.f;
+    }
   }
 }
 
+// The second pass's columns' maximum, 1 / sum and D: three arrays, `step` floats apart.
+struct ColumnStats {
+  const float* at;
+  int step;
+};
+
 // The second pass's chunk: rows are keys, columns queries.  s: products k q -> p; dp: products v do -> dz.  `index`: buckets, at the first
-// row and column of the fragment (ROWS: [key][query], else [query][key]); `stats`: the columns' maximum, 1 / sum and D.
+// row and column of the fragment (ROWS: [key][query], else [query][key]); `stats`: at the first column.
 template <int NT, bool ROWS>
 __device__ __forceinline__ void differ_columns(float (&s)[NT][4], float (&dp)[NT][4], const Scoring& sc, const float* bias, const uint16_t* index, int pitch,
-                                               const float4* stats, uint64_t real, const Tally& tally, int h, bool count0, bool count1) {
+                                               const ColumnStats& stats, uint64_t real, const Tally& tally, int h, bool count0, bool count1) {
   const int g = (threadIdx.x & 31) >> 2, q2 = (threadIdx.x & 3) * 2;
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
@@ -149,11 +188,15 @@ __device__ __forceinline__ void differ_columns(float (&s)[NT][4], float (&dp)[NT
       for (int e = 0; e < 4; ++e) b[e] = bias_at(bias, bk[e]);
     }
     score_of<true>(sc, s[t], b, slope);
-    const float4 st[2] = {stats[t * 8 + q2], stats[t * 8 + q2 + 1]};
+    const float* st = stats.at + t * 8 + q2;
+    const float2 m = *reinterpret_cast<const float2*>(st), i = *reinterpret_cast<const float2*>(st + stats.step), D = *reinterpret_cast<const float2*>(st + 2 * stats.step);
+    const F2 down = pair(-m.x, -m.y), inv = pair(i.x, i.y), less = pair(-D.x, -D.y);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      s[t][e] = ex2_approx(s[t][e] - st[e & 1].x) * st[e & 1].y;
-      dp[t][e] = s[t][e] * (dp[t][e] - st[e & 1].z);
+    for (int e = 0; e < 4; e += 2) {
+      const float2 x = parts(add(two(s[t], e), down));
+      const F2 p = mul(pair(ex2_approx(x.x), ex2_approx(x.y)), inv);
+      put(s[t], e, p);
+      put(dp[t], e, mul(p, add(two(dp[t], e), less)));
     }
     if (((uint32_t)(real >> (8 * t)) & 0xffu) != 0xffu) {  // columns without a query: whatever lies there
       const uint32_t mine = (uint32_t)(real >> (8 * t)) >> q2;
@@ -164,12 +207,13 @@ __device__ __forceinline__ void differ_columns(float (&s)[NT][4], float (&dp)[NT
           bk[e] = 0;  // (an unwritten bucket may lie outside of the table)
         }
     }
-    if (tally.on)
+    if (tally.on) {
+      if (count0) tally.add2(h, bk[0], bk[1], dp[t][0], dp[t][1]);
+      if (count1) tally.add2(h, bk[2], bk[3], dp[t][2], dp[t][3]);
+    }
+    if (sc.cap != 0.f)
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (e < 2 ? count0 : count1) tally.add(h, bk[e], dp[t][e]);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) dp[t][e] *= slope[e];
+      for (int e = 0; e < 4; ++e) dp[t][e] *= slope[e];
   }
 }
 
@@ -219,9 +263,10 @@ __device__ __forceinline__ void products(float (&s)[NT][4], float (&dp)[NT][4], 
 // A segment whose keys are one chunk: everything of the tile's rows at once.
 template <typename T, int DT, int NT>
 __device__ __forceinline__ void rows_at_once(float (&acc)[DT / 8][4], float3 (&st)[2], float (&bound)[2], const Operands& x, const Scoring& sc, uint64_t keys) {
-  float s[NT][4], dp[NT][4];
+  float s1[1][NT][4], dp[NT][4];
+  float(&s)[NT][4] = s1[0];
   products<T, DT, NT>(s, dp, x, keys);
-  transform<NT>(s, sc, x.bias, x.index, x.pitch_idx, keys);
+  transform<1, NT>(s1, sc, x.bias, 0, x.index, x.pitch_idx, keys);
   RowSums f;
   f.start();
   sum_rows<NT>(f, s, dp);
@@ -233,13 +278,14 @@ __device__ __forceinline__ void rows_at_once(float (&acc)[DT / 8][4], float3 (&s
     scores<T, DT, NT>(s, x.q, x.ck, x.pitch, x.dim);
     differ_rows<NT>(s, dp, sc, x.bias, x.index, x.pitch_idx, st, keys);
   }
-  weigh<T, DT, NT, kWide<T>>(acc, dp, x.ck, x.pitch, x.dim, keys);
+  weigh<T, DT, NT, kWide<T>>(acc, dp, x.ck, x.pitch, x.dim);
 }
 template <typename T, int DT, int NT>
 __device__ __forceinline__ void rows_first(RowSums& f, const Operands& x, const Scoring& sc, uint64_t keys) {
-  float s[NT][4], dp[NT][4];
+  float s1[1][NT][4], dp[NT][4];
+  float(&s)[NT][4] = s1[0];
   products<T, DT, NT>(s, dp, x, keys);
-  transform<NT>(s, sc, x.bias, x.index, x.pitch_idx, keys);
+  transform<1, NT>(s1, sc, x.bias, 0, x.index, x.pitch_idx, keys);
   sum_rows<NT>(f, s, dp);
 }
 template <typename T, int DT, int NT>
@@ -247,18 +293,18 @@ __device__ __forceinline__ void rows_second(float (&acc)[DT / 8][4], const float
   float s[NT][4], dp[NT][4];
   products<T, DT, NT>(s, dp, x, keys);
   differ_rows<NT>(s, dp, sc, x.bias, x.index, x.pitch_idx, st, keys);
-  weigh<T, DT, NT, kWide<T>>(acc, dp, x.ck, x.pitch, x.dim, keys);
+  weigh<T, DT, NT, kWide<T>>(acc, dp, x.ck, x.pitch, x.dim);
 }
 // By keys.
 template <typename T, int DT, int NT, bool ROWS>
-__device__ __forceinline__ void columns(float (&dk)[DT / 8][4], float (&dv)[DT / 8][4], const Operands& x, const Scoring& sc, const float4* stats, uint64_t queries,
+__device__ __forceinline__ void columns(float (&dk)[DT / 8][4], float (&dv)[DT / 8][4], const Operands& x, const Scoring& sc, const ColumnStats& stats, uint64_t queries,
                                         const Tally& tally, int h, bool count0, bool count1) {
   float s[NT][4], dp[NT][4];
   scores<T, DT, NT>(s, x.k, x.cq, x.pitch, x.dim);
   scores<T, DT, NT>(dp, x.v, x.co, x.pitch, x.dim);
   differ_columns<NT, ROWS>(s, dp, sc, x.bias, x.index, x.pitch_idx, stats, queries, tally, h, count0, count1);
-  weigh<T, DT, NT, kWide<T>>(dk, dp, x.cq, x.pitch, x.dim, queries);
-  weigh<T, DT, NT, false>(dv, s, x.co, x.pitch, x.dim, queries);
+  weigh<T, DT, NT, kWide<T>>(dk, dp, x.cq, x.pitch, x.dim);
+  weigh<T, DT, NT, false>(dv, s, x.co, x.pitch, x.dim);
 }
 
 // ---- short segments ------------------------------------------------------------------------------------------------
@@ -270,9 +316,9 @@ struct BackLayout {
 template <typename T, int DT>
 static BackLayout back_layout(const SegArgs& a, int limit) {
   BackLayout l = {};
-  l.s = short_layout<T>(a, kBackHeads<T, DT>, limit, 4);
+  l.s = short_layout<T>(a, kBackHeads<T, DT>, limit, 4, 64);
   uint32_t at = l.s.bytes;
-  l.stats = at; at += l.s.heads * (l.s.batch + 16) * 16;
+  l.stats = at; at += l.s.heads * 3 * (l.s.batch + 16) * 4;
   if (a.dbias) {
     l.hist = at; at += l.s.heads * 2 * a.buckets * 4;
     l.spoilt = at; at += (l.s.heads * a.buckets + 31) / 32 * 4;
@@ -282,7 +328,7 @@ static BackLayout back_layout(const SegArgs& a, int limit) {
 }
 
 template <typename T, int DT>
-__global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) short_backward_kernel(const __grid_constant__ SegArgs a, const BackLayout L, const Scoring sc, const BackWork work, int blocks) {
+__global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) short_backward_kernel(const __grid_constant__ SegArgs a, const BackLayout L, const Scoring sc, const BackWork work) {
   extern __shared__ __align__(16) unsigned char smem[];
   constexpr int HG = kBackHeads<T, DT>;
   const int dim = kExact<DT> ? DT : a.dim;
@@ -293,7 +339,7 @@ __global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) short_backward_ker
   float* bias = reinterpret_cast<float*>(smem + L.s.bias);
   int4* cells = reinterpret_cast<int4*>(smem + L.s.cells);
   uint16_t* index = reinterpret_cast<uint16_t*>(smem + L.s.index);
-  float4* stats = reinterpret_cast<float4*>(smem + L.stats);
+  float* stats = reinterpret_cast<float*>(smem + L.stats);  // [heads][3][stat_rows]
   const int stat_rows = L.s.batch + 16;
   const int head0 = blockIdx.y * HG, heads = min(HG, a.heads - head0);
   const uint32_t pitch = kExact<DT> ? HG * DT * sizeof(T) + 16 : L.s.pitch;
@@ -304,7 +350,7 @@ __global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) short_backward_ker
   tally.buckets = a.buckets;
   tally.on = a.dbias != nullptr;
   tally.bound(0.f);
-  stage_tables(a, maps, bias, head0, HG);
+  stage_tables<kThreads>(a, maps, bias, head0, HG);
   float* mine = work.partial + (int64_t)blockIdx.x * work.table + head0 * a.buckets;
   if (tally.on) {
     for (int i = threadIdx.x; i < HG * 2 * a.buckets; i += kThreads) tally.hist[i] = 0;
@@ -338,14 +384,22 @@ __global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) short_backward_ker
   Operands x = {};
   x.bias = bias + h * a.buckets;
   x.pitch_idx = L.s.pitch_idx; x.pitch = pitch; x.dim = dim;
-  for (int block = blockIdx.x; block < blocks; block += gridDim.x) {
+  for (int r = blockIdx.x; r < L.s.ranges; r += gridDim.x) {
     __syncthreads();
-    make_plan(a, plan, block, blocks, L.s.limit);
-    while (next_batch(a, plan, cells, block, L.s.batch)) {
+    const Range range = start_range<kThreads>(a, plan, r, L.s.ranges, L.s.per);
+    while (next_batch<kThreads>(a, plan, range, L.s.limit, L.s.batch)) {
     if (threadIdx.x == 0) block_bound = 0;
-    load_rows<T, 4>(q0, L.s.array, pitch, src, plan.ids, plan.rows, chunks, real);
+    if (a.bias) {
+      load_cells<kThreads>(a, smem_u32(cells), plan.ids, plan.rows);
+      cp_commit();
+    }
+    load_rows<T, kThreads, 4>(q0, L.s.array, pitch, src, plan.ids, plan.rows, chunks, real);
     cp_commit();
-    if (a.bias) fill_index(a, plan, cells, maps, index, L.s.pitch_idx);
+    if (a.bias) {
+      cp_wait<1>();
+      __syncthreads();
+      fill_index<kThreads>(a, plan, cells, maps, index, L.s.pitch_idx);
+    }
     cp_wait<0>();
     __syncthreads();
     if (h < heads) {
@@ -375,24 +429,36 @@ __global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) short_backward_ker
         } else {
           RowSums f;
           f.start();
-          for (int j = 0; j < item.len; j += 32) {
-            to_chunk(j);
-            rows_first<T, DT, 4>(f, x, sc, real_rows(plan, item.at + j, min(32, item.len - j)));
-          }
-          st[0] = row_stats(f, 0, &bound[0]);
-          st[1] = row_stats(f, 1, &bound[1]);
-          for (int j = 0; j < item.len; j += 32) {
-            to_chunk(j);
-            rows_second<T, DT, 4>(acc, st, x, sc, real_rows(plan, item.at + j, min(32, item.len - j)));
+          const int tiles = (item.len + 7) >> 3;
+          for (int pass = 0; pass < 2; ++pass) {  // in parts of 3 and 4 tiles
+            int parts = (tiles + 3) / 4, left = tiles;
+            for (int j = 0; left > 0; --parts) {
+              const int now = (left + parts - 1) / parts;
+              const uint64_t keys = real_rows(plan, item.at + j, min(8 * now, item.len - j));
+              to_chunk(j);
+              if (pass == 0) {
+                if (now == 4) rows_first<T, DT, 4>(f, x, sc, keys);
+                else rows_first<T, DT, 3>(f, x, sc, keys);
+              } else {
+                if (now == 4) rows_second<T, DT, 4>(acc, st, x, sc, keys);
+                else rows_second<T, DT, 3>(acc, st, x, sc, keys);
+              }
+              j += 8 * now;
+              left -= now;
+            }
+            if (pass == 0) {
+              st[0] = row_stats(f, 0, &bound[0]);
+              st[1] = row_stats(f, 1, &bound[1]);
+            }
           }
         }
         const int id0 = r0 < item.len ? plan.ids[item.at + r0] : -1, id1 = r0 + 8 < item.len ? plan.ids[item.at + r0 + 8] : -1;
         if (id0 >= 0) most = fmaxf(most, bound[0]);
         if (id1 >= 0) most = fmaxf(most, bound[1]);
         if ((lane & 3) == 0) {
-          float4* to = stats + h * stat_rows + row + g;
-          if (r0 < item.len) to[0] = make_float4(st[0].x, st[0].y, st[0].z, 0.f);
-          if (r0 + 8 < item.len) to[8] = make_float4(st[1].x, st[1].y, st[1].z, 0.f);
+          float* to = stats + 3 * h * stat_rows + row + g;
+          if (r0 < item.len) { to[0] = st[0].x; to[stat_rows] = st[0].y; to[2 * stat_rows] = st[0].z; }
+          if (r0 + 8 < item.len) { to[8] = st[1].x; to[stat_rows + 8] = st[1].y; to[2 * stat_rows + 8] = st[1].z; }
         }
         store_rows<T, DT>(acc, a.scale, a.dq, a.ld_dq, col + h * dim, dim, id0, id1);
       }
@@ -425,7 +491,7 @@ __global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) short_backward_ker
           const int cols = min(32, item.len - j);
           const uint64_t queries = real_rows(plan, item.at + j, cols);
           const uint32_t at = (item.at + j) * pitch + at_head;
-          const float4* from = stats + h * stat_rows + item.at + j;
+          const ColumnStats from = {stats + 3 * h * stat_rows + item.at + j, stat_rows};
           x.cq = q0 + at; x.co = o0 + at;
           x.index = index + (item.at + j) * L.s.pitch_idx + 16 * item.tile;
           switch ((cols + 7) >> 3) {
@@ -439,7 +505,7 @@ __global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) short_backward_ker
         store_rows<T, DT>(dv, 1.f, a.dv, a.ld_dv, col + h * dim, dim, id0, id1);
       }
     }
-    if (plan.next == kRowBlock) break;
+    if (plan.cursor >= range.end) break;
     __syncthreads();
     }
   }
@@ -453,7 +519,7 @@ __global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) short_backward_ker
 template <typename T, int DT>
 struct BackShape {
   static constexpr int HG = DT * sizeof(T) <= 64 ? 4 : DT * sizeof(T) <= 128 ? 2 : 1, WH = HG < 2 ? HG : 2, HPW = HG / WH, rows = 16 * kWarps / WH;
-  static constexpr int chunk = sizeof(T) == 2 ? 64 : DT <= 64 ? 32 : 16, NT = chunk < 32 ? 2 : 4;  // rows that pass at a time; tiles of 8 of them in registers
+  static constexpr int chunk = sizeof(T) == 2 || DT <= 64 ? 32 : 16, NT = chunk < 32 ? 2 : 4;  // rows that pass at a time; tiles of 8 of them in registers
 };
 
 struct BackLongLayout {
@@ -481,7 +547,7 @@ static BackLongLayout back_long_layout(const SegArgs& a, bool by_keys) {
     l.index = take((size_t)S::rows * l.pitch_idx * 2);
   }
   if (by_keys) {
-    l.stats = take((size_t)3 * S::HG * S::chunk * 16);
+    l.stats = take((size_t)3 * S::HG * 3 * S::chunk * 4);
     if (a.dbias) {
       l.hist = take((size_t)S::HG * 2 * a.buckets * 4);
       l.spoilt = take((size_t)(S::HG * a.buckets + 31) / 32 * 4);
@@ -534,7 +600,7 @@ __global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) long_backward_kern
       tally.hist[at] = tally.hist[at + a.buckets] = 0;
     }
   };
-  stage_tables(a, maps, bias, head0, S::HG);
+  stage_tables<kThreads>(a, maps, bias, head0, S::HG);
   const int chunks = S::HG * dim * (int)sizeof(T) / 16, real = heads * dim * (int)sizeof(T) / 16;
   const int64_t col = (int64_t)head0 * dim;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2;
@@ -549,7 +615,7 @@ __global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) long_backward_kern
     const int parts = (tile.hi - tile.lo + S::chunk - 1) / S::chunk;
     auto ids_of = [&](int c) { return ids + S::rows + c % 3 * S::chunk; };
     auto cells_of = [&](int c) { return reinterpret_cast<int4*>(smem + L.passing_cells) + c % 3 * S::chunk; };
-    auto stats_of = [&](int c) { return reinterpret_cast<float4*>(smem + L.stats) + c % 3 * S::HG * S::chunk; };
+    auto stats_of = [&](int c) { return reinterpret_cast<float*>(smem + L.stats) + c % 3 * (S::HG * 3 * S::chunk); };  // [heads][3][chunk]
     auto array = [&](int c, int which) { return smem_u32(smem + L.passing) + ((c & 1) * 2 + which) * L.chunk; };
     __syncthreads();  // (the tile before is done with the shared memory)
     if (threadIdx.x < S::rows) {
@@ -570,16 +636,13 @@ __global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) long_backward_kern
       if (BY_KEYS)
         for (int i = threadIdx.x; i < heads * S::chunk; i += kThreads) {
           const int h = i / S::chunk, j = i % S::chunk, at = tile.lo + c * S::chunk + j;
-          float4 st = make_float4(0.f, 0.f, 0.f, 0.f);
-          if (at < tile.hi) {
-            const float* from = work.stats + ((int64_t)(head0 - work.head0 + h) * work.n + at) * 3;
-            st = make_float4(from[0], from[1], from[2], 0.f);
-          }
-          stats_of(c)[h * S::chunk + j] = st;
+          const float* from = work.stats + ((int64_t)(head0 - work.head0 + h) * work.n + at) * 3;
+#pragma unroll
+          for (int k = 0; k < 3; ++k) stats_of(c)[(3 * h + k) * S::chunk + j] = at < tile.hi ? from[k] : 0.f;
         }
     };
     auto load = [&](int c) {
-      load_rows<T, 2>(array(c, 0), L.chunk, pitch, passing, ids_of(c), S::chunk, chunks, real);
+      load_rows<T, kThreads, 2>(array(c, 0), L.chunk, pitch, passing, ids_of(c), S::chunk, chunks, real);
       cp_commit();
     };
     RowSums f[BY_KEYS ? 1 : HPW];
@@ -599,7 +662,7 @@ __global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) long_backward_kern
       fetch_id(1);
       __syncthreads();
       if (BY_KEYS || sweep == 0) {
-        load_rows<T, 2>(own0, L.tile, pitch, own, ids, S::rows, chunks, real);
+        load_rows<T, kThreads, 2>(own0, L.tile, pitch, own, ids, S::rows, chunks, real);
       }
       load(0);
       for (int c = 0; c < parts; ++c) {
@@ -624,7 +687,6 @@ __global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) long_backward_kern
           __syncthreads();
         }
         uint64_t there = __ballot_sync(kAll, lane < S::chunk && ids_of(c)[lane] >= 0);
-        if (S::chunk > 32) there |= (uint64_t)__ballot_sync(kAll, ids_of(c)[32 + lane] >= 0) << 32;
 #pragma unroll
         for (int i = 0; i < HPW; ++i) {
           const int h = (warp % S::WH) * HPW + i;
@@ -641,7 +703,7 @@ __global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) long_backward_kern
             x.co = x.cv = array(c, 1) + j * pitch + at_head;
             x.index = index + row * L.pitch_idx + j;
             if constexpr (BY_KEYS) {
-              columns<T, DT, NT, true>(acc[i], dv[i], x, sc, stats_of(c) + h * S::chunk + j, bits, tally, h, ids[row + g] >= 0, ids[row + g + 8] >= 0);
+              columns<T, DT, NT, true>(acc[i], dv[i], x, sc, ColumnStats{stats_of(c) + 3 * h * S::chunk + j, S::chunk}, bits, tally, h, ids[row + g] >= 0, ids[row + g + 8] >= 0);
             } else {
               if (sweep == 0) rows_first<T, DT, NT>(f[i], x, sc, bits);
               else rows_second<T, DT, NT>(acc[i], st[i], x, sc, bits);
@@ -716,7 +778,7 @@ int backward_of(dsvt_ctx* ctx, const SegArgs& a) {
   BackLayout l = back_layout<T, DT>(a, limit);
   while (l.bytes > kSmemMost) l = back_layout<T, DT>(a, limit = limit > 64 ? 64 : limit / 2);
   const Scoring sc = scoring_of(a);
-  const int groups = (int)dsvt_ceil_div(a.heads, kBackHeads<T, DT>), blocks = (int)dsvt_ceil_div(a.n, kRowBlock);
+  const int groups = (int)dsvt_ceil_div(a.heads, kBackHeads<T, DT>);
   BackWork w = {};
   uint32_t* base = reinterpret_cast<uint32_t*>(ctx->bm_zero);
   w.partial = reinterpret_cast<float*>(base);
@@ -731,12 +793,13 @@ int backward_of(dsvt_ctx* ctx, const SegArgs& a) {
   const int per_sm = DT <= 32 && l.bytes <= kSmemMost / 2 ? 2 : 1;
   int64_t stay = dsvt_ceil_div(per_sm * ctx->sm_count, groups);
   if (w.table > 0 && stay > (int64_t)kPartialWords / w.table) stay = kPartialWords / w.table;
-  if (stay > blocks) stay = blocks;
+  set_ranges(l.s, a.n, (int)stay, 128);
+  if (stay > l.s.ranges) stay = l.s.ranges;
   w.blocks = (int)stay;
   constexpr auto kernel = short_backward_kernel<T, DT>;
   int rc = allow_smem<kernel>(ctx);
   if (rc != DSVT_OK) return rc;
-  launch_pdl(kernel, dim3((unsigned)stay, groups), dim3(kThreads), l.bytes, ctx->stream, a, l, sc, w, blocks);
+  launch_pdl(kernel, dim3((unsigned)stay, groups), dim3(kThreads), l.bytes, ctx->stream, a, l, sc, w);
   DSVT_LAUNCHED(ctx);
   const bool longer = limit < a.max_len;
   if (longer) {

@@ -1,38 +1,41 @@
-// Segment attention: what a block works on.  Short segments: all those that start in a block's kRowBlock rows, whole, in shared
-// memory.  Long ones: a tile of the rows of one segment, the segment's other rows passing by in chunks.
+// Segment attention: what a block works on.  Short segments: those that start in a range of rows, whole, as many at a time as fit in
+// shared memory.  Long ones: a tile of the rows of one segment, the segment's other rows passing by in chunks.
 #pragma once
+#include <limits.h>
+
 #include "segment_mma.cuh"
 
 namespace dsvt_train {
 
-constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kRowBlock = 32;
+constexpr int kThreads = 256, kWarps = kThreads / 32;  // of the long ones' blocks
 constexpr int kShort = 128;                         // most rows of a segment that is held whole
 constexpr int kBatch = 48;                          // rows in shared memory at a time, or the longest segment's if that is more
-constexpr int kMaxItems = kRowBlock * (kShort / 16);
 
 // 16 rows of a segment: its first row's place in the batch, its length, the tile.
 struct Item { uint8_t at, len, tile, pad; };
 
-// A block's segments, and the batch of them in shared memory: mostly all of them, else as many as fit.
+// A batch of segments in shared memory.  A segment's place is a multiple of 8 rows, so that tiles of 8 rows are its own; the places
+// behind its end are zeros.
 struct Plan {
-  int rows, items, pairs, next;        // of the batch (pairs: of queries and keys); where the next batch starts
-  int first;                           // the batch's first row, from the block's
-  uint32_t starts;                     // bit i: a segment starts at place i
-  uint8_t len_at[kRowBlock];           // by row of the block: length of the segment that starts there
+  int rows, items, pairs;              // (pairs: of queries and keys)
+  int cursor;                          // the first segment that has not been looked at
+  int lo[kShort / 8];                  // by segment: first row, length, place
+  uint8_t len[kShort / 8], place[kShort / 8];
+  uint8_t owner[kShort / 8];           // by 8 places: the segment
   uint32_t real[kShort / 32 + 3];      // bit i: place i holds a voxel
   int32_t ids[kShort];
-  Item item[kMaxItems];
+  Item item[kShort / 8];
 };
 
-// Which entries of seg_start can be of segments that start in rows [from, to): found by 256 probes a round (one for most calls).
+// Which entries of seg_start can be of segments that start in rows [from, to): found by a probe per thread and round (one or two for most calls); N: threads of the block.
 // `first`, `last`: nothing lies before or behind the rows.
+template <int N>
 __device__ __forceinline__ int2 segments_near(const SegArgs& a, int from, int to, bool first, bool last) {
   const int tid = threadIdx.x;
   int lo = 0, hi = a.cap_segments, end = hi;
   if (a.num_segments) { const int m = *a.num_segments; end = m < 0 ? 0 : m < end ? m : end; }
   while (true) {
-    const int span = hi - lo, step = (span + kThreads - 1) / kThreads;
+    const int span = hi - lo, step = (span + N - 1) / N;
     const int64_t i = lo + (int64_t)tid * step;
     const int v = i < hi ? a.seg_start[i] : 0;
     const bool in = i < hi && i < end;
@@ -41,18 +44,19 @@ __device__ __forceinline__ int2 segments_near(const SegArgs& a, int from, int to
     if (!last && next_hi < hi) hi = (int)next_hi;
     if (!first && below > 0) lo += (below - 1) * step;
     if (hi > end) hi = end;
-    if (hi - lo <= 8 * kThreads || hi - lo >= span) break;
+    if (hi - lo <= 8 * N || hi - lo >= span) break;
   }
   return make_int2(lo, hi);
 }
 
 // Copies what every block reads: the index tables of the displacements and its heads' bias, in units of log 2.
+template <int N>
 __device__ __forceinline__ void stage_tables(const SegArgs& a, uint16_t* maps, float* bias, int head0, int heads) {
   if (!a.bias) return;
-  for (int i = threadIdx.x; i < a.maps.at_z + 2 * a.maps.extent[2] - 1; i += kThreads) maps[i] = (uint16_t)(4 * a.maps.of[i]);
+  for (int i = threadIdx.x; i < a.maps.at_z + 2 * a.maps.extent[2] - 1; i += N) maps[i] = (uint16_t)(4 * a.maps.of[i]);
   const int count = min(heads, a.heads - head0) * a.buckets;
   const float* from = a.bias + (int64_t)head0 * a.buckets;
-  for (int i = threadIdx.x; i < count; i += kThreads) bias[i] = bias_log2(from[i]);
+  for (int i = threadIdx.x; i < count; i += N) bias[i] = bias_log2(from[i]);
 }
 
 __device__ __forceinline__ int bucket_at(const BucketMaps& m, const uint16_t* maps, int4 i, int4 j) {
@@ -61,60 +65,85 @@ __device__ __forceinline__ int bucket_at(const BucketMaps& m, const uint16_t* ma
   return maps[dx] + maps[dy] + maps[dz];  // (the maps in shared memory hold four times the index: a bias's offset)
 }
 
-// Finds the block's segments, of at most `limit` rows.
-__device__ __forceinline__ void make_plan(const SegArgs& a, Plan& p, int block, int blocks, int limit) {
-  const int tid = threadIdx.x, base = block * kRowBlock;
-  if (tid < kRowBlock) p.len_at[tid] = 0;
-  if (tid == 0) p.next = 0;
-  const int2 near = segments_near(a, base, base + kRowBlock, block == 0, block == blocks - 1);
-  for (int s = near.x + tid; s < near.y; s += kThreads) {
-    const int lo = a.seg_start[s], hi = a.seg_start[s + 1];
-    if (segment_sound(a, lo, hi) && hi - lo <= limit && lo >= base && lo < base + kRowBlock) p.len_at[lo - base] = (uint8_t)(hi - lo);
-  }
+// The segments that start in rows [from, to) of a call, the first range and the last open to their side.
+struct Range { int from, to, end; };
+template <int N>
+__device__ __forceinline__ Range start_range(const SegArgs& a, Plan& p, int range, int ranges, int per) {
+  const int2 near = segments_near<N>(a, range * per, (range + 1) * per, range == 0, range == ranges - 1);
+  if (threadIdx.x == 0) p.cursor = near.x;
   __syncthreads();
+  return Range{range == 0 ? INT_MIN : range * per, range == ranges - 1 ? INT_MAX : (range + 1) * per, near.y};
 }
 
-// The next batch of the block's segments, of at most `most` rows together: their rows' voxels and cells and the list of their tiles.
-// False if there are no more.  A barrier comes before.
-__device__ __forceinline__ bool next_batch(const SegArgs& a, Plan& p, int4* cells, int block, int most) {
+// The next batch of a range's segments of up to `limit` rows, at most `most` places together: their rows' voxels and the list of their
+// tiles.  False if there are no more.  A barrier comes before.
+template <int N>
+__device__ __forceinline__ bool next_batch(const SegArgs& a, Plan& p, const Range& range, int limit, int most) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   if (warp == 0) {
-    const int len = p.len_at[lane];
-    const uint32_t left = __ballot_sync(kAll, len > 0 && lane >= p.next);
-    const int first = __ffs(left) - 1, at = lane - first;
-    const bool in = (left >> lane & 1) && at + len <= most;
-    const uint32_t taken = __ballot_sync(kAll, in), rest = left & ~taken;
-    const int tiles = in ? (len + 15) >> 4 : 0;
-    int rows = in ? at + len : 0, upto = tiles, pairs = in ? len * len : 0;
-    for (int m = 1; m < 32; m <<= 1) {
-      rows = max(rows, __shfl_xor_sync(kAll, rows, m));
-      pairs += __shfl_xor_sync(kAll, pairs, m);
-      const int before = __shfl_up_sync(kAll, upto, m);
-      if (lane >= m) upto += before;
+    int at = 0, segments = 0, items = 0, pairs = 0, cursor = p.cursor;
+    bool open = true;
+    while (open && cursor < range.end) {  // 32 segments at a time
+      const int s = cursor + lane;
+      int lo = 0, hi = 0;
+      if (s < range.end) { lo = a.seg_start[s]; hi = a.seg_start[s + 1]; }
+      const bool here = s < range.end && lo >= range.from && lo < range.to;
+      const bool mine = here && segment_sound(a, lo, hi) && hi - lo <= limit;
+      const int len = mine ? hi - lo : 0, tiles = (len + 15) >> 4, size = (len + 7) & ~7;
+      int end = size, upto = tiles;  // sums up to and with this lane's segment
+      for (int m = 1; m < 32; m <<= 1) {
+        const int e = __shfl_up_sync(kAll, end, m), u = __shfl_up_sync(kAll, upto, m);
+        if (lane >= m) {
+          end += e;
+          upto += u;
+        }
+      }
+      const bool in = mine && at + end <= most;
+      const uint32_t taken = __ballot_sync(kAll, in), rest = __ballot_sync(kAll, mine) & ~taken;
+      if (in) {
+        const int place = at + end - size, slot = segments + __popc(taken & ((1u << lane) - 1u));
+        p.lo[slot] = lo;
+        p.len[slot] = (uint8_t)len;
+        p.place[slot] = (uint8_t)place;
+        for (int t = 0; t < tiles; ++t) p.item[items + upto - tiles + t] = Item{(uint8_t)place, (uint8_t)len, (uint8_t)t, 0};
+        for (int t = 0; t < size; t += 8) p.owner[(place + t) >> 3] = (uint8_t)slot;
+        pairs += len * len;
+      }
+      if (taken) {
+        const int last = 31 - __clz(taken);
+        at += __shfl_sync(kAll, end, last);
+        items += __shfl_sync(kAll, upto, last);
+        segments += __popc(taken);
+      }
+      const uint32_t behind = __ballot_sync(kAll, s < range.end && lo >= range.to);
+      if (rest) {
+        cursor += __ffs(rest) - 1;
+        open = false;
+      } else {
+        cursor = behind ? range.end : cursor + 32;
+        open = at + 8 <= most;
+      }
     }
-    for (int t = 0; t < tiles; ++t) p.item[upto - tiles + t] = Item{(uint8_t)at, (uint8_t)len, (uint8_t)t, 0};
-    if (lane == 31) p.items = upto;
+    for (int m = 16; m > 0; m >>= 1) pairs += __shfl_xor_sync(kAll, pairs, m);
     if (lane == 0) {
-      p.rows = rows;
+      p.rows = at;
+      p.items = items;
       p.pairs = pairs;
-      p.first = first;
-      p.starts = left ? taken >> first : 0u;
-      p.next = rest ? __ffs(rest) - 1 : kRowBlock;
+      p.cursor = cursor;
     }
   }
   __syncthreads();
   if (p.items == 0) return false;
-  if (tid < (int)(sizeof(p.real) / 4) * 32) {
+  if (tid < 3) p.real[kShort / 32 + tid] = 0;
+  for (int i = tid; i < kShort; i += N) {
     int id = -1;
-    const uint32_t upto = p.starts & (tid >= 31 ? kAll : (2u << tid) - 1u);
-    if (tid < p.rows && upto) {
-      const int at = 31 - __clz(upto);
-      if (tid < at + p.len_at[p.first + at]) id = voxel_at(a, block * kRowBlock + p.first + tid);
+    if (i < p.rows) {
+      const int own = p.owner[i >> 3], r = i - p.place[own];
+      if (r < p.len[own]) id = voxel_at(a, p.lo[own] + r);
     }
     const uint32_t real = __ballot_sync(kAll, id >= 0);
-    if (lane == 0) p.real[warp] = real;
-    if (tid < kShort) p.ids[tid] = id;
-    if (a.bias && id >= 0) cells[tid] = a.coords[id];
+    if (lane == 0) p.real[i >> 5] = real;
+    p.ids[i] = id;
   }
   __syncthreads();
   return true;
@@ -134,12 +163,12 @@ __device__ __forceinline__ uint64_t real_rows(const Plan& p, int at, int count) 
 __host__ __device__ constexpr int index_pitch(int cols) { return 8 * (((cols + 7) / 8) | 1); }
 
 // The buckets (times 4) of all pairs of the batch: index[i][j - first of i's segment].  The rest of the tile is never written.
+template <int N>
 __device__ __forceinline__ void fill_index(const SegArgs& a, const Plan& p, const int4* cells, const uint16_t* maps, uint16_t* index, int pitch) {
   const int part = threadIdx.x & 15;
-  for (int i = threadIdx.x >> 4; i < p.rows; i += kThreads / 16) {
-    const uint32_t upto = p.starts & (i >= 31 ? kAll : (2u << i) - 1u);
-    const int at = upto ? 31 - __clz(upto) : 0, len = p.len_at[p.first + at];
-    if (i >= at + len || p.ids[i] < 0) continue;
+  for (int i = threadIdx.x >> 4; i < p.rows; i += N / 16) {
+    if (p.ids[i] < 0) continue;
+    const int own = p.owner[i >> 3], at = p.place[own], len = p.len[own];
     const int4 mine = cells[i];
 #pragma unroll 3
     for (int j = part; j < len; j += 16) index[i * pitch + j] = (uint16_t)bucket_at(a.maps, maps, mine, cells[at + j]);
@@ -153,10 +182,10 @@ struct Rows {
   const char* from[N];  // at the block's first head
   int64_t ld[N];        // bytes
 };
-template <typename T, int N>
+template <typename T, int THREADS, int N>
 __device__ __forceinline__ void load_rows(uint32_t to, uint32_t array, uint32_t pitch, const Rows<N>& src, const int32_t* ids, int rows, int chunks, int real) {
   const int part = threadIdx.x & 7;
-  for (int r = threadIdx.x >> 3; r < rows; r += kThreads / 8) {
+  for (int r = threadIdx.x >> 3; r < rows; r += THREADS / 8) {
     const int id = ids[r];
     const char* at[N];
 #pragma unroll
@@ -169,6 +198,11 @@ __device__ __forceinline__ void load_rows(uint32_t to, uint32_t array, uint32_t 
       for (int i = 0; i < N; ++i) cp_async16(dst + i * array + c * 16, at[i] + (in ? c * 16 : 0), in);
     }
   }
+}
+// The batch's voxels' cells.
+template <int N>
+__device__ __forceinline__ void load_cells(const SegArgs& a, uint32_t to, const int32_t* ids, int rows) {
+  for (int i = threadIdx.x; i < rows; i += N) cp_async16(to + i * 16, a.coords + max(ids[i], 0), true);
 }
 template <typename T>
 __device__ __forceinline__ const char* first_head(const void* p, int64_t col) { return reinterpret_cast<const char*>(p) + col * (int64_t)sizeof(T); }
@@ -233,24 +267,33 @@ __device__ __forceinline__ void set_columns(float (&c)[NT][4], uint64_t real, fl
   if (!(last & 2)) c[NT - 1][1] = c[NT - 1][3] = to;
 }
 
-// `index`: the fragment's first row's buckets at the chunk's first column (rows g and g + 8 of the tile).
-template <int NT>
-__device__ __forceinline__ void transform(float (&s)[NT][4], const Scoring& sc, const float* bias, const uint16_t* index, int pitch, uint64_t real) {
-  float b[NT][4];
+// `index`: the fragment's first row's buckets at the chunk's first column (rows g and g + 8 of the tile).  HP heads' products, biases `step`
+// entries apart.
+template <int HP, int NT>
+__device__ __forceinline__ void transform(float (&s)[HP][NT][4], const Scoring& sc, const float* bias, int step, const uint16_t* index, int pitch, uint64_t real) {
+  float none[4];
+  if (sc.bias) {
 #pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    b[t][0] = b[t][1] = b[t][2] = b[t][3] = 0.f;
-    if (sc.bias) {
+    for (int t = 0; t < NT; ++t) {
       int bk[4];
       buckets_of(bk, index + t * 8, pitch);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) b[t][e] = bias_at(bias, bk[e]);
-    }
-  }
-  float none[4];
+      for (int h = 0; h < HP; ++h) {
+        float b[4];
 #pragma unroll
-  for (int t = 0; t < NT; ++t) score_of<false>(sc, s[t], b[t], none);
-  set_columns<NT>(s, real, -INFINITY);
+        for (int e = 0; e < 4; ++e) b[e] = bias_at(bias + h * step, bk[e]);
+        score_of<false>(sc, s[h][t], b, none);
+      }
+    }
+  } else {
+    const float b[4] = {};
+#pragma unroll
+    for (int h = 0; h < HP; ++h)
+#pragma unroll
+      for (int t = 0; t < NT; ++t) score_of<false>(sc, s[h][t], b, none);
+  }
+#pragma unroll
+  for (int h = 0; h < HP; ++h) set_columns<NT>(s[h], real, -INFINITY);
 }
 
 __device__ __forceinline__ float quad_max(float v) {
@@ -262,7 +305,7 @@ __device__ __forceinline__ float quad_sum(float v) {
   return v + __shfl_xor_sync(kAll, v, 2);
 }
 // 1 / l; a row without keys (l = 0) gives 0.
-__device__ __forceinline__ float inverse(float l) { return l == 0.f ? 0.f : 1.f / l; }
+__device__ __forceinline__ float inverse(float l) { return l == 0.f ? 0.f : __fdividef(1.f, l); }
 
 // Running maximum and sum of a fragment's two rows, and the weighted sums.
 template <int DT>
@@ -297,13 +340,16 @@ __device__ __forceinline__ void soften(Flow<DT>& f, float (&s)[NT][4]) {
       }
     }
     f.m[r] = m;
+    const F2 down = pair(-base, -base);
+    F2 sum = pair(l, 0.f);
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      s[t][2 * r] = ex2_approx(s[t][2 * r] - base);
-      s[t][2 * r + 1] = ex2_approx(s[t][2 * r + 1] - base);
-      l += s[t][2 * r] + s[t][2 * r + 1];
+      const float2 x = parts(add(two(s[t], 2 * r), down));
+      s[t][2 * r] = ex2_approx(x.x);
+      s[t][2 * r + 1] = ex2_approx(x.y);
+      sum = add(sum, two(s[t], 2 * r));
     }
-    f.l[r] = l;
+    f.l[r] = sum_of(sum);
   }
 }
 
@@ -314,7 +360,7 @@ constexpr int kMaxTiles = 8;       // tiles that start in one block's rows (at m
 // The tiles of `tile` rows of segments longer than `above` that start in rows [base, base + tile).
 __device__ __forceinline__ int find_tiles(const SegArgs& a, Tile* tiles, int* count, int base, int tile, int above) {
   if (threadIdx.x == 0) *count = 0;
-  const int2 near = segments_near(a, base + 1, base + tile, false, false);
+  const int2 near = segments_near<kThreads>(a, base + 1, base + tile, false, false);
   __syncthreads();
   for (int s = near.x + (int)threadIdx.x; s < near.y; s += kThreads) {
     const int lo = a.seg_start[s], hi = a.seg_start[s + 1];

@@ -6,23 +6,25 @@
 
 namespace dsvt_train {
 
-// Heads of a block that holds its segments whole: rows of at most 400 bytes, which leaves room for three blocks of 36-voxel sets.
+// Heads of a block that holds its segments whole: rows of at most 400 bytes, which leaves room for two blocks on an SM.
 template <typename T, int DT>
 constexpr int kHeads = DT * sizeof(T) <= 48 ? 8 : DT * sizeof(T) <= 96 ? 4 : DT * sizeof(T) <= 128 ? 2 : 1;
 
+constexpr int kShortThreads = 256;
+
 struct ShortLayout {
-  int heads, batch;                            // of a block; rows at a time
+  int heads, batch, per, ranges;               // of a block; rows at a time; rows of a range, and ranges of the call
   int pitch_idx, limit;                        // entries to a row of the bucket tile; longest segment
   uint32_t pitch, array;                       // bytes of a row and of an array of rows
   uint32_t maps, bias, cells, index, rows, bytes;
 };
 
 template <typename T>
-static ShortLayout short_layout(const SegArgs& a, int heads, int limit, int arrays) {
+static ShortLayout short_layout(const SegArgs& a, int heads, int limit, int arrays, int batch) {
   ShortLayout l = {};
   l.heads = heads;
   l.limit = limit;
-  l.batch = limit > kBatch ? limit : kBatch;
+  l.batch = limit > batch ? (limit + 7) / 8 * 8 : batch;
   l.pitch = (uint32_t)(heads * a.dim * sizeof(T) + 16);
   l.array = l.batch * l.pitch;
   uint32_t at = (sizeof(Plan) + 15) / 16 * 16;
@@ -34,27 +36,38 @@ static ShortLayout short_layout(const SegArgs& a, int heads, int limit, int arra
     l.index = take(((size_t)(l.batch + 16) * l.pitch_idx + 64) * 2);
     l.bias = take((size_t)heads * a.buckets * 4);  // (a look-up of an unwritten bucket ends within 4 KB of a head's first: the rows follow)
   }
-  // A tile of 16 rows may begin at an array's last row, and longer segments go in chunks of up to 40: what follows the rows is read,
-  // and not used.
-  l.rows = take((size_t)arrays * l.array + (limit <= 40 ? 16 : 40) * l.pitch);
+  // (a tile of 16 rows may begin at an array's last 8: what follows is read, and not used)
+  l.rows = take((size_t)arrays * l.array + 8 * l.pitch);
   if (at - l.rows < 4096) at = l.rows + 4096;
   l.bytes = at;
   return l;
 }
 
-// A tile of 16 queries against its segment's keys, NT tiles of them at a time: all of them where ONLY.
-template <typename T, int DT, int NT, bool ONLY>
-__device__ __forceinline__ void attend_tile(Flow<DT>& f, uint32_t q, uint32_t k, uint32_t v, uint32_t pitch, int dim, const Scoring& sc, const float* bias,
-                                            const uint16_t* index, int pitch_idx, uint64_t keys) {
-  float s[NT][4];
-  scores<T, DT, NT>(s, q, k, pitch, dim);
-  transform<NT>(s, sc, bias, index, pitch_idx, keys);
-  soften<ONLY>(f, s);
-  weigh<T, DT, NT, false>(f.acc, s, v, pitch, dim, keys);
+// Rows of a range: an equal share for every block that can be resident, within bounds: few enough that ranges of more and fewer short
+// segments even out, enough that a block's tables and searches are spread.
+static void set_ranges(ShortLayout& l, int n, int resident, int most) {
+  int per = (n + resident - 1) / resident;
+  per = per < 16 ? 16 : per > most ? most : per;
+  l.per = per;
+  l.ranges = (n + per - 1) / per;
+}
+
+// HP heads' tiles of 16 queries against their segment's keys, NT tiles of them at a time: all of them where ONLY.  `step`: bytes between heads.
+template <typename T, int DT, int NT, bool ONLY, int HP>
+__device__ __forceinline__ void attend_tile(Flow<DT> (&f)[HP], uint32_t q, uint32_t k, uint32_t v, uint32_t step, uint32_t pitch, int dim, const Scoring& sc, const float* bias,
+                                            int buckets, const uint16_t* index, int pitch_idx, uint64_t keys) {
+  float s[HP][NT][4];
+#pragma unroll
+  for (int h = 0; h < HP; ++h) scores<T, DT, NT>(s[h], q + h * step, k + h * step, pitch, dim);
+  transform<HP, NT>(s, sc, bias, buckets, index, pitch_idx, keys);
+#pragma unroll
+  for (int h = 0; h < HP; ++h) soften<ONLY>(f[h], s[h]);
+#pragma unroll
+  for (int h = 0; h < HP; ++h) weigh<T, DT, NT, false>(f[h].acc, s[h], v + h * step, pitch, dim);
 }
 
 template <typename T, int DT>
-__global__ void __launch_bounds__(kThreads, DT <= 24 && sizeof(T) == 2 ? 3 : DT <= 32 ? 2 : 1) short_forward_kernel(const __grid_constant__ SegArgs a, const ShortLayout L, const Scoring sc) {
+__global__ void __launch_bounds__(kShortThreads, DT <= 24 && sizeof(T) == 2 ? 3 : DT <= 32 ? 2 : 1) short_forward_kernel(const __grid_constant__ SegArgs a, const ShortLayout L, const Scoring sc) {
   extern __shared__ __align__(16) unsigned char smem[];
   constexpr int HG = kHeads<T, DT>;
   const int dim = kExact<DT> ? DT : a.dim;
@@ -67,72 +80,94 @@ __global__ void __launch_bounds__(kThreads, DT <= 24 && sizeof(T) == 2 ? 3 : DT 
   const int head0 = blockIdx.y * HG, heads = min(HG, a.heads - head0);
   const uint32_t pitch = kExact<DT> ? HG * DT * sizeof(T) + 16 : L.pitch;
   const uint32_t q0 = smem_u32(smem + L.rows), k0 = q0 + L.array, v0 = k0 + L.array;
-  make_plan(a, plan, blockIdx.x, gridDim.x, L.limit);
+  const Range range = start_range<kShortThreads>(a, plan, blockIdx.x, L.ranges, L.per);
   const int chunks = HG * dim * (int)sizeof(T) / 16, real = heads * dim * (int)sizeof(T) / 16;
   const int64_t col = (int64_t)head0 * dim;
   const Rows<3> src = {{first_head<T>(a.q, col), first_head<T>(a.k, col), first_head<T>(a.v, col)},
                        {a.ld_q * (int64_t)sizeof(T), a.ld_k * (int64_t)sizeof(T), a.ld_v * (int64_t)sizeof(T)}};
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, h = warp % HG;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  constexpr int HP = 1;
   bool staged = false;
-  while (next_batch(a, plan, cells, blockIdx.x, L.batch)) {
-  load_rows<T, 3>(q0, L.array, pitch, src, plan.ids, plan.rows, chunks, real);
+  while (next_batch<kShortThreads>(a, plan, range, L.limit, L.batch)) {
+  if (a.bias) {
+    load_cells<kShortThreads>(a, smem_u32(cells), plan.ids, plan.rows);
+    cp_commit();
+  }
+  load_rows<T, kShortThreads, 3>(q0, L.array, pitch, src, plan.ids, plan.rows, chunks, real);
   cp_commit();
   if (a.bias) {
     if (!staged) {  // (while the rows are on their way)
-      stage_tables(a, maps, bias, head0, HG);
-      __syncthreads();
+      stage_tables<kShortThreads>(a, maps, bias, head0, HG);
       staged = true;
     }
-    fill_index(a, plan, cells, maps, index, L.pitch_idx);
+    cp_wait<1>();
+    __syncthreads();
+    fill_index<kShortThreads>(a, plan, cells, maps, index, L.pitch_idx);
   }
   cp_wait<0>();
   __syncthreads();
-  if (h < heads) {
-    const uint32_t at_head = h * dim * sizeof(T);
+  for (int unit = warp; unit < plan.items * (HG / HP); unit += kShortThreads / 32) {
+    const int h = unit % (HG / HP) * HP;
+    if (h >= heads) continue;
+    const Item item = plan.item[unit / (HG / HP)];
+    const uint32_t at_head = h * dim * sizeof(T), step = dim * sizeof(T);
     const float* mine = bias + h * a.buckets;
-    for (int it = warp / HG; it < plan.items; it += kWarps / HG) {
-      const Item item = plan.item[it];
-      const int row = item.at + 16 * item.tile;
-      const uint32_t q = q0 + row * pitch + at_head, k = k0 + item.at * pitch + at_head, v = v0 + item.at * pitch + at_head;
-      const uint16_t* at = index + row * L.pitch_idx;
-      Flow<DT> f;
-      f.start();
-      const uint64_t keys = real_rows(plan, item.at, item.len);
-#define DSVT_ATTEND(NT) attend_tile<T, DT, NT, true>(f, q, k, v, pitch, dim, sc, mine, at, L.pitch_idx, keys)
-      if (item.len <= 16) {
-        if (item.len <= 8) DSVT_ATTEND(1);
-        else DSVT_ATTEND(2);
-      } else if (item.len <= 32) {
-        if (item.len <= 24) DSVT_ATTEND(3);
-        else DSVT_ATTEND(4);
-      } else {
-        for (int j = 0; j < item.len; j += 40)
-          attend_tile<T, DT, 5, false>(f, q, k + j * pitch, v + j * pitch, pitch, dim, sc, mine, at + j, L.pitch_idx, real_rows(plan, item.at + j, min(40, item.len - j)));
+    const int row = item.at + 16 * item.tile;
+    const uint32_t q = q0 + row * pitch + at_head, k = k0 + item.at * pitch + at_head, v = v0 + item.at * pitch + at_head;
+    const uint16_t* at = index + row * L.pitch_idx;
+    Flow<DT> f[HP];
+#pragma unroll
+    for (int i = 0; i < HP; ++i) f[i].start();
+#define DSVT_ATTEND(NT) attend_tile<T, DT, NT, true, HP>(f, q, k, v, step, pitch, dim, sc, mine, a.buckets, at, L.pitch_idx, real_rows(plan, item.at, item.len))
+#define DSVT_ATTEND_PART(NT)                                                                                                 \
+  attend_tile<T, DT, NT, false, HP>(f, q, k + j * pitch, v + j * pitch, step, pitch, dim, sc, mine, a.buckets, at + j, L.pitch_idx, \
+                                    real_rows(plan, item.at + j, min(8 * NT, item.len - j)))
+    const int tiles = (item.len + 7) >> 3;
+    switch (tiles) {
+      case 1: DSVT_ATTEND(1); break;
+      case 2: DSVT_ATTEND(2); break;
+      case 3: DSVT_ATTEND(3); break;
+      case 4: DSVT_ATTEND(4); break;
+      case 5: DSVT_ATTEND(5); break;
+      default: {  // in parts of 3 to 5 tiles
+        int parts = (tiles + 4) / 5, left = tiles;
+        for (int j = 0; left > 0; --parts) {
+          const int now = (left + parts - 1) / parts;
+          if (now == 5) DSVT_ATTEND_PART(5);
+          else if (now == 4) DSVT_ATTEND_PART(4);
+          else DSVT_ATTEND_PART(3);
+          j += 8 * now;
+          left -= now;
+        }
       }
+    }
 #undef DSVT_ATTEND
-      // the result takes the place of the queries (this warp's alone: a head's channels of a tile's rows)
-      const float i0 = inverse(quad_sum(f.l[0])), i1 = inverse(quad_sum(f.l[1]));
-      const int r0 = 16 * item.tile + (lane >> 2);
-      T* to = reinterpret_cast<T*>(smem + L.rows + (item.at + r0) * pitch + at_head) + (lane & 3) * 2;
-      __syncwarp();
+#undef DSVT_ATTEND_PART
+    // the result takes the place of the queries (this warp's alone: its heads' channels of a tile's rows)
+    const int r0 = 16 * item.tile + (lane >> 2);
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < HP; ++i) {
+      const float i0 = inverse(quad_sum(f[i].l[0])), i1 = inverse(quad_sum(f[i].l[1]));
+      T* to = reinterpret_cast<T*>(smem + L.rows + (item.at + r0) * pitch + at_head + i * step) + (lane & 3) * 2;
 #pragma unroll
       for (int n = 0; n < DT / 8; ++n) {
         if (!kExact<DT> && n * 8 >= dim) break;
-        if (r0 < item.len) store2<T>(to + n * 8, f.acc[n][0] * i0, f.acc[n][1] * i0);
-        if (r0 + 8 < item.len) store2<T>(reinterpret_cast<T*>(reinterpret_cast<char*>(to) + 8 * pitch) + n * 8, f.acc[n][2] * i1, f.acc[n][3] * i1);
+        if (r0 < item.len) store2<T>(to + n * 8, f[i].acc[n][0] * i0, f[i].acc[n][1] * i0);
+        if (r0 + 8 < item.len) store2<T>(reinterpret_cast<T*>(reinterpret_cast<char*>(to) + 8 * pitch) + n * 8, f[i].acc[n][2] * i1, f[i].acc[n][3] * i1);
       }
     }
   }
   __syncthreads();
   const int part = threadIdx.x & 7;
-  for (int r = threadIdx.x >> 3; r < plan.rows; r += kThreads / 8) {
+  for (int r = threadIdx.x >> 3; r < plan.rows; r += kShortThreads / 8) {
     const int id = plan.ids[r];
     if (id < 0) continue;
     char* to = (char*)a.out + (id * a.ld_out + col) * (int64_t)sizeof(T);
 #pragma unroll 4
     for (int c = part; c < real; c += 8) *reinterpret_cast<uint4*>(to + c * 16) = *reinterpret_cast<const uint4*>(smem + L.rows + r * pitch + c * 16);
   }
-  if (plan.next == kRowBlock) break;
+  if (plan.cursor >= range.end) break;
   __syncthreads();
   }
 }
@@ -147,7 +182,8 @@ struct LongLayout {
 template <typename T, int DT>
 struct LongShape {
   static constexpr int HG = DT * sizeof(T) <= 64 ? 4 : DT * sizeof(T) <= 128 ? 2 : 1, WH = HG < 2 ? HG : 2, HPW = HG / WH, rows = 16 * kWarps / WH;
-  static constexpr int NT = sizeof(T) == 2 ? 8 : 6, chunk = 8 * NT;
+  static constexpr bool three = sizeof(T) == 2 && DT <= 24;  // blocks on an SM: three of chunks of 32 rows rather than two of 64 (565 and 591 us)
+  static constexpr int NT = three ? 4 : sizeof(T) == 2 ? 8 : 6, chunk = 8 * NT;
 };
 
 template <typename T, int DT>
@@ -194,7 +230,7 @@ struct Passing {
 };
 
 template <typename T, int DT>
-__global__ void __launch_bounds__(kThreads) long_forward_kernel(const __grid_constant__ SegArgs a, const LongLayout L, const Scoring sc, int above) {
+__global__ void __launch_bounds__(kThreads, LongShape<T, DT>::three ? 3 : 1) long_forward_kernel(const __grid_constant__ SegArgs a, const LongLayout L, const Scoring sc, int above) {
   extern __shared__ __align__(16) unsigned char smem[];
   using S = LongShape<T, DT>;
   __shared__ Tile tiles[kMaxTiles];
@@ -211,7 +247,7 @@ __global__ void __launch_bounds__(kThreads) long_forward_kernel(const __grid_con
   const int head0 = blockIdx.y * S::HG, heads = min(S::HG, a.heads - head0);
   const uint32_t pitch = kExact<DT> ? S::HG * DT * sizeof(T) + 16 : L.pitch;
   const uint32_t q0 = smem_u32(smem + L.rows);
-  stage_tables(a, maps, bias, head0, S::HG);
+  stage_tables<kThreads>(a, maps, bias, head0, S::HG);
   const int chunks = S::HG * dim * (int)sizeof(T) / 16, real = heads * dim * (int)sizeof(T) / 16;
   const int64_t col = (int64_t)head0 * dim;
   const Rows<1> own = {{first_head<T>(a.q, col)}, {a.ld_q * (int64_t)sizeof(T)}};
@@ -235,18 +271,18 @@ __global__ void __launch_bounds__(kThreads) long_forward_kernel(const __grid_con
       }
     };
     auto load = [&](int c) {
-      load_rows<T, 2>(pass.array(c, 0, 2), L.chunk, pitch, passing, pass.ids(c), S::chunk, chunks, real);
+      load_rows<T, kThreads, 2>(pass.array(c, 0, 2), L.chunk, pitch, passing, pass.ids(c), S::chunk, chunks, real);
       cp_commit();
     };
     pass.fetch_id(tile.lo);
     publish(0);
     pass.fetch_id(tile.lo + S::chunk);
     __syncthreads();
-    load_rows<T, 1>(q0, 0, pitch, own, ids, S::rows, chunks, real);
+    load_rows<T, kThreads, 1>(q0, 0, pitch, own, ids, S::rows, chunks, real);
     load(0);
-    Flow<DT> f[S::HPW];
+    Flow<DT> f[S::HPW][1];
 #pragma unroll
-    for (int i = 0; i < S::HPW; ++i) f[i].start();
+    for (int i = 0; i < S::HPW; ++i) f[i][0].start();
     const int parts = (tile.hi - tile.lo + S::chunk - 1) / S::chunk;
     for (int c = 0; c < parts; ++c) {
       if (c + 1 < parts) publish(c + 1);
@@ -275,8 +311,8 @@ __global__ void __launch_bounds__(kThreads) long_forward_kernel(const __grid_con
         const int h = (warp % S::WH) * S::HPW + i;
         if (h < heads && row < rows) {
           const uint32_t at_head = h * dim * sizeof(T);
-          attend_tile<T, DT, S::NT, false>(f[i], q0 + row * pitch + at_head, pass.array(c, 0, 2) + at_head, pass.array(c, 1, 2) + at_head, pitch, dim, sc,
-                                           bias + h * a.buckets, index + row * L.pitch_idx, L.pitch_idx, keys);
+          attend_tile<T, DT, S::NT, false, 1>(f[i], q0 + row * pitch + at_head, pass.array(c, 0, 2) + at_head, pass.array(c, 1, 2) + at_head, 0, pitch, dim, sc,
+                                              bias + h * a.buckets, 0, index + row * L.pitch_idx, L.pitch_idx, keys);
         }
       }
     }
@@ -284,14 +320,14 @@ __global__ void __launch_bounds__(kThreads) long_forward_kernel(const __grid_con
     for (int i = 0; i < S::HPW; ++i) {
       const int h = (warp % S::WH) * S::HPW + i;
       if (h >= heads || row >= rows) continue;
-      const float i0 = inverse(quad_sum(f[i].l[0])), i1 = inverse(quad_sum(f[i].l[1]));
+      const float i0 = inverse(quad_sum(f[i][0].l[0])), i1 = inverse(quad_sum(f[i][0].l[1]));
       const int r0 = row + (lane >> 2), id0 = ids[r0], id1 = ids[r0 + 8];
       T* to = (T*)a.out + col + h * dim + (lane & 3) * 2;
 #pragma unroll
       for (int n = 0; n < DT / 8; ++n) {
         if (!kExact<DT> && n * 8 >= dim) break;
-        if (id0 >= 0) store2<T>(to + id0 * a.ld_out + n * 8, f[i].acc[n][0] * i0, f[i].acc[n][1] * i0);
-        if (id1 >= 0) store2<T>(to + id1 * a.ld_out + n * 8, f[i].acc[n][2] * i1, f[i].acc[n][3] * i1);
+        if (id0 >= 0) store2<T>(to + id0 * a.ld_out + n * 8, f[i][0].acc[n][0] * i0, f[i][0].acc[n][1] * i0);
+        if (id1 >= 0) store2<T>(to + id1 * a.ld_out + n * 8, f[i][0].acc[n][2] * i1, f[i][0].acc[n][3] * i1);
       }
     }
   }
@@ -315,13 +351,15 @@ static int allow_smem(dsvt_ctx* ctx) {
 template <typename T, int DT>
 int forward_of(dsvt_ctx* ctx, const SegArgs& a) {
   int limit = a.max_len <= kShort ? a.max_len : 64;
-  ShortLayout l = short_layout<T>(a, kHeads<T, DT>, limit, 3);
-  if (l.bytes > kSmemMost) l = short_layout<T>(a, kHeads<T, DT>, limit = 64, 3);
+  ShortLayout l = short_layout<T>(a, kHeads<T, DT>, limit, 3, kBatch);
+  if (l.bytes > kSmemMost) l = short_layout<T>(a, kHeads<T, DT>, limit = 64, 3, kBatch);
   const Scoring sc = scoring_of(a);
+  const int groups = (int)dsvt_ceil_div(a.heads, kHeads<T, DT>);
+  set_ranges(l, a.n, (int)dsvt_ceil_div((DT <= 24 && sizeof(T) == 2 ? 3 : 2) * ctx->sm_count, groups), 128);
   constexpr auto kernel = short_forward_kernel<T, DT>;
   int rc = allow_smem<kernel>(ctx);
   if (rc != DSVT_OK) return rc;
-  launch_pdl(kernel, dim3((unsigned)dsvt_ceil_div(a.n, kRowBlock), (unsigned)dsvt_ceil_div(a.heads, kHeads<T, DT>)), dim3(kThreads), l.bytes, ctx->stream, a, l, sc);
+  launch_pdl(kernel, dim3((unsigned)l.ranges, (unsigned)groups), dim3(kShortThreads), l.bytes, ctx->stream, a, l, sc);
   DSVT_LAUNCHED(ctx);
   if (limit >= a.max_len) return DSVT_OK;
   using S = LongShape<T, DT>;

@@ -58,24 +58,28 @@ __device__ __forceinline__ float lds(uint32_t a) {
   return v;
 }
 
-#define DSVT_MMA16(NAME, TYPE)                                                                                                       \
-  __device__ __forceinline__ void NAME(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) { \
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32." TYPE "." TYPE ".f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"  \
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])                                                                    \
-                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));                                                            \
-  }                                                                                                                                  \
-  __device__ __forceinline__ void NAME##_k8(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t b0) {                                  \
-    asm volatile("mma.sync.aligned.m16n8k8.row.col.f32." TYPE "." TYPE ".f32 {%0,%1,%2,%3}, {%4,%5}, {%6}, {%0,%1,%2,%3};"            \
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])                                                                    \
-                 : "r"(a0), "r"(a1), "r"(b0));                                                                                       \
+// c += a b; FRESH: c = a b.
+#define DSVT_MMA(NAME, SHAPE, TYPE, ARGS, A, B, ...)                                                                                  \
+  template <bool FRESH>                                                                                                               \
+  __device__ __forceinline__ void NAME(float (&c)[4], ARGS) {                                                                         \
+    if (FRESH)                                                                                                                        \
+      asm("mma.sync.aligned." SHAPE ".row.col.f32." TYPE "." TYPE ".f32 {%0,%1,%2,%3}, {" A "}, {" B "}, {%4,%4,%4,%4};"      \
+                   : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "f"(0.f), __VA_ARGS__);                                         \
+    else                                                                                                                              \
+      asm("{.reg .f32 z; mov.f32 z, %4; mma.sync.aligned." SHAPE ".row.col.f32." TYPE "." TYPE ".f32 {%0,%1,%2,%3}, {" A "}, {" B "}, {%0,%1,%2,%3};}" \
+                   : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "f"(0.f), __VA_ARGS__);                                         \
   }
-DSVT_MMA16(mma_bf16, "bf16")
-DSVT_MMA16(mma_f16, "f16")
-__device__ __forceinline__ void mma_tf32(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
+#define DSVT_COMMA ,
+#define DSVT_MMA_K16(NAME, SHAPE, TYPE)                                                                                                \
+  DSVT_MMA(NAME, SHAPE, TYPE, uint32_t a0 DSVT_COMMA uint32_t a1 DSVT_COMMA uint32_t a2 DSVT_COMMA uint32_t a3 DSVT_COMMA uint32_t b0 DSVT_COMMA uint32_t b1, \
+           "%5,%6,%7,%8", "%9,%10", "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1))
+#define DSVT_MMA_K8(NAME, SHAPE, TYPE) \
+  DSVT_MMA(NAME, SHAPE, TYPE, uint32_t a0 DSVT_COMMA uint32_t a1 DSVT_COMMA uint32_t b0, "%5,%6", "%7", "r"(a0), "r"(a1), "r"(b0))
+DSVT_MMA_K16(mma_bf16, "m16n8k16", "bf16")
+DSVT_MMA_K8(mma_bf16_k8, "m16n8k8", "bf16")
+DSVT_MMA_K16(mma_f16, "m16n8k16", "f16")
+DSVT_MMA_K8(mma_f16_k8, "m16n8k8", "f16")
+DSVT_MMA_K16(mma_tf32, "m16n8k8", "tf32")
 __device__ __forceinline__ uint32_t tf32(float v) {
   uint32_t r;
   asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(r) : "f"(v));
@@ -93,14 +97,18 @@ template <typename T>
 struct Mma;
 template <>
 struct Mma<__nv_bfloat16> {
-  static __device__ __forceinline__ void k16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) { mma_bf16(c, a0, a1, a2, a3, b0, b1); }
-  static __device__ __forceinline__ void k8(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t b0) { mma_bf16_k8(c, a0, a1, b0); }
+  template <bool FRESH>
+  static __device__ __forceinline__ void k16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) { mma_bf16<FRESH>(c, a0, a1, a2, a3, b0, b1); }
+  template <bool FRESH>
+  static __device__ __forceinline__ void k8(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t b0) { mma_bf16_k8<FRESH>(c, a0, a1, b0); }
   static __device__ __forceinline__ uint32_t pack(float lo, float hi) { return dsvt_tc::pack_bf16(lo, hi); }
 };
 template <>
 struct Mma<__half> {
-  static __device__ __forceinline__ void k16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) { mma_f16(c, a0, a1, a2, a3, b0, b1); }
-  static __device__ __forceinline__ void k8(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t b0) { mma_f16_k8(c, a0, a1, b0); }
+  template <bool FRESH>
+  static __device__ __forceinline__ void k16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) { mma_f16<FRESH>(c, a0, a1, a2, a3, b0, b1); }
+  template <bool FRESH>
+  static __device__ __forceinline__ void k8(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t b0) { mma_f16_k8<FRESH>(c, a0, a1, b0); }
   static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
     const __half2 h = __floats2half2_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&h);
@@ -111,71 +119,90 @@ struct Mma<__half> {
 template <int DT>
 constexpr bool kExact = DT <= 32;
 
+// One step of scores(): channels k * 16 (fp32: k * 8) on.
+template <typename T, int NT, bool FRESH>
+__device__ __forceinline__ void scores_k16(float (&c)[NT][4], uint32_t ra, uint32_t rb, uint32_t rl, uint32_t pitch) {
+  uint32_t f[4];
+  ldsm4(f, ra);
+#pragma unroll
+  for (int p = 0; p < NT / 2; ++p) {
+    uint32_t g[4];
+    ldsm4(g, rb + p * 16 * pitch);
+    Mma<T>::template k16<FRESH>(c[2 * p], f[0], f[1], f[2], f[3], g[0], g[1]);
+    Mma<T>::template k16<FRESH>(c[2 * p + 1], f[0], f[1], f[2], f[3], g[2], g[3]);
+  }
+  if (NT & 1) {
+    uint32_t g0, g1;
+    ldsm2(g0, g1, rl);
+    Mma<T>::template k16<FRESH>(c[NT - 1], f[0], f[1], f[2], f[3], g0, g1);
+  }
+}
+template <typename T, int NT, bool FRESH>
+__device__ __forceinline__ void scores_k8(float (&c)[NT][4], uint32_t a, uint32_t b, uint32_t pitch) {
+  const int lane = threadIdx.x & 31;
+  uint32_t f0, f1;
+  ldsm2(f0, f1, a + (lane & 15) * pitch);
+#pragma unroll
+  for (int p = 0; p < NT / 4; ++p) {
+    uint32_t g[4];
+    ldsm4(g, b + (p * 32 + lane) * pitch);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) Mma<T>::template k8<FRESH>(c[4 * p + i], f0, f1, g[i]);
+  }
+  if (NT & 2) {
+    uint32_t g0, g1;
+    ldsm2(g0, g1, b + (NT / 4 * 32 + (lane & 15)) * pitch);
+    Mma<T>::template k8<FRESH>(c[NT / 4 * 4], f0, f1, g0);
+    Mma<T>::template k8<FRESH>(c[NT / 4 * 4 + 1], f0, f1, g1);
+  }
+  if (NT & 1) Mma<T>::template k8<FRESH>(c[NT - 1], f0, f1, ldsm1(b + ((NT - 1) * 8 + (lane & 7)) * pitch));
+}
+template <int NT, bool FRESH>
+__device__ __forceinline__ void scores_tf32(float (&c)[NT][4], float (&s)[NT][4], uint32_t ra, uint32_t rb, uint32_t pitch) {
+  Parts f[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) f[i] = split(lds(ra + (i & 1) * 8 * pitch + (i >> 1) * 16));
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const Parts g0 = split(lds(rb + t * 8 * pitch)), g1 = split(lds(rb + t * 8 * pitch + 16));
+    mma_tf32<FRESH>(s[t], f[0].lo, f[1].lo, f[2].lo, f[3].lo, g0.hi, g1.hi);
+    mma_tf32<false>(s[t], f[0].hi, f[1].hi, f[2].hi, f[3].hi, g0.lo, g1.lo);
+    mma_tf32<FRESH>(c[t], f[0].hi, f[1].hi, f[2].hi, f[3].hi, g0.hi, g1.hi);
+  }
+}
+
 // C[i][j] for the 16 rows at a and the 8 NT rows at b; both addresses are of a head's first channel, rows `pitch` bytes apart.
 template <typename T, int DT, int NT>
 __device__ __forceinline__ void scores(float (&c)[NT][4], uint32_t a, uint32_t b, uint32_t pitch, int dim) {
   const int lane = threadIdx.x & 31;
-#pragma unroll
-  for (int t = 0; t < NT; ++t) c[t][0] = c[t][1] = c[t][2] = c[t][3] = 0.f;
   if constexpr (sizeof(T) == 2) {
     const uint32_t ra = a + (lane & 15) * pitch + (lane >> 4) * 16;
     const uint32_t rb = b + ((lane & 7) + (lane >> 4) * 8) * pitch + ((lane >> 3) & 1) * 16;  // (two tiles; the last of an odd number: its own)
     const uint32_t rl = b + ((NT - 1) * 8 + (lane & 7)) * pitch + ((lane >> 3) & 1) * 16;
-#pragma unroll
-    for (int k = 0; k < (DT + 15) / 16; ++k) {
-      if (!kExact<DT> && k * 16 >= dim) break;
-      if (kExact<DT> ? k * 16 + 16 <= DT : k * 16 + 16 <= dim) {
-        uint32_t f[4];
-        ldsm4(f, ra + k * 32);
-#pragma unroll
-        for (int p = 0; p < NT / 2; ++p) {
-          uint32_t g[4];
-          ldsm4(g, rb + p * 16 * pitch + k * 32);
-          Mma<T>::k16(c[2 * p], f[0], f[1], f[2], f[3], g[0], g[1]);
-          Mma<T>::k16(c[2 * p + 1], f[0], f[1], f[2], f[3], g[2], g[3]);
-        }
-        if (NT & 1) {
-          uint32_t g0, g1;
-          ldsm2(g0, g1, rl + k * 32);
-          Mma<T>::k16(c[NT - 1], f[0], f[1], f[2], f[3], g0, g1);
-        }
-      } else {  // the last 8 channels
-        uint32_t f0, f1;
-        ldsm2(f0, f1, a + (lane & 15) * pitch + k * 32);
-#pragma unroll
-        for (int p = 0; p < NT / 4; ++p) {
-          uint32_t g[4];
-          ldsm4(g, b + (p * 32 + lane) * pitch + k * 32);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) Mma<T>::k8(c[4 * p + i], f0, f1, g[i]);
-        }
-        if (NT & 2) {
-          uint32_t g0, g1;
-          ldsm2(g0, g1, b + (NT / 4 * 32 + (lane & 15)) * pitch + k * 32);
-          Mma<T>::k8(c[NT / 4 * 4], f0, f1, g0);
-          Mma<T>::k8(c[NT / 4 * 4 + 1], f0, f1, g1);
-        }
-        if (NT & 1) Mma<T>::k8(c[NT - 1], f0, f1, ldsm1(b + ((NT - 1) * 8 + (lane & 7)) * pitch + k * 32));
+    if constexpr (kExact<DT>) {
+      scores_k16<T, NT, true>(c, ra, rb, rl, pitch);
+      if constexpr (DT >= 32) scores_k16<T, NT, false>(c, ra + 32, rb + 32, rl + 32, pitch);
+      if constexpr (DT % 16 == 8) scores_k8<T, NT, false>(c, a + DT / 16 * 32, b + DT / 16 * 32, pitch);
+    } else {
+      if (dim == 8) {
+        scores_k8<T, NT, true>(c, a, b, pitch);
+        return;
       }
+      scores_k16<T, NT, true>(c, ra, rb, rl, pitch);
+#pragma unroll 1
+      for (int k = 1; k * 16 + 16 <= dim; ++k) scores_k16<T, NT, false>(c, ra + k * 32, rb + k * 32, rl + k * 32, pitch);
+      if (dim & 8) scores_k8<T, NT, false>(c, a + (dim >> 4) * 32, b + (dim >> 4) * 32, pitch);
     }
   } else {
     float s[NT][4];  // hi lo + lo hi
-#pragma unroll
-    for (int t = 0; t < NT; ++t) s[t][0] = s[t][1] = s[t][2] = s[t][3] = 0.f;
     const uint32_t ra = a + (lane >> 2) * pitch + (lane & 3) * 4, rb = b + (lane >> 2) * pitch + (lane & 3) * 4;
+    scores_tf32<NT, true>(c, s, ra, rb, pitch);
+    if constexpr (kExact<DT>) {
 #pragma unroll
-    for (int k = 0; k < DT / 8; ++k) {
-      if (!kExact<DT> && k * 8 >= dim) break;
-      Parts f[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) f[i] = split(lds(ra + (i & 1) * 8 * pitch + k * 32 + (i >> 1) * 16));
-#pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        const Parts g0 = split(lds(rb + t * 8 * pitch + k * 32)), g1 = split(lds(rb + t * 8 * pitch + k * 32 + 16));
-        mma_tf32(s[t], f[0].lo, f[1].lo, f[2].lo, f[3].lo, g0.hi, g1.hi);
-        mma_tf32(s[t], f[0].hi, f[1].hi, f[2].hi, f[3].hi, g0.lo, g1.lo);
-        mma_tf32(c[t], f[0].hi, f[1].hi, f[2].hi, f[3].hi, g0.hi, g1.hi);
-      }
+      for (int k = 1; k < DT / 8; ++k) scores_tf32<NT, false>(c, s, ra + k * 32, rb + k * 32, pitch);
+    } else {
+#pragma unroll 1
+      for (int k = 1; k < dim / 8; ++k) scores_tf32<NT, false>(c, s, ra + k * 32, rb + k * 32, pitch);
     }
 #pragma unroll
     for (int t = 0; t < NT; ++t)
@@ -184,74 +211,58 @@ __device__ __forceinline__ void scores(float (&c)[NT][4], uint32_t a, uint32_t b
   }
 }
 
-// acc += W B: W[i][j] over the 8 NT rows j at b.  Bit j of `real` says whether row j counts: what lies in the others is not looked at,
-// finite or not.  WIDE: W in tf32 (float16's gradients).
+// acc += W B: W[i][j] over the 8 NT rows j at b.  Rows that hold no voxel are zeros there, and columns of W without one are zero: what lies
+// in other segments' rows is not touched, finite or not.  WIDE: W in tf32 (float16's gradients).
 template <typename T, int DT, int NT, bool WIDE>
-__device__ __forceinline__ void weigh(float (&acc)[DT / 8][4], const float (&w)[NT][4], uint32_t b, uint32_t pitch, int dim, uint64_t real) {
+__device__ __forceinline__ void weigh(float (&acc)[DT / 8][4], const float (&w)[NT][4], uint32_t b, uint32_t pitch, int dim) {
   const int lane = threadIdx.x & 31, q2 = (lane & 3) * 2;
   if constexpr (sizeof(T) == 2) {
 #pragma unroll
     for (int p = 0; p < (NT + 1) / 2; ++p) {  // 16 rows at a time, and the last 8 of an odd number of tiles
       const bool half = 2 * p + 1 == NT;
-      const uint32_t bits = (uint32_t)(real >> (16 * p)) & (half ? 0xffu : 0xffffu);
-      const bool ragged = bits != (half ? 0xffu : 0xffffu);
-      uint32_t m0 = kAll, m1 = kAll;
-      if (ragged) {
-        const uint32_t mine = bits >> q2;
-        m0 = ((mine & 1) ? 0xffffu : 0u) | ((mine & 2) ? 0xffff0000u : 0u);
-        m1 = ((mine & 0x100) ? 0xffffu : 0u) | ((mine & 0x200) ? 0xffff0000u : 0u);
-      }
+      const int o = half ? 2 * p : 2 * p + 1;
       uint32_t a[4] = {};
       if (!WIDE) {
         a[0] = Mma<T>::pack(w[2 * p][0], w[2 * p][1]);
         a[1] = Mma<T>::pack(w[2 * p][2], w[2 * p][3]);
         if (!half) {
-          a[2] = Mma<T>::pack(w[2 * p + 1 < NT ? 2 * p + 1 : 0][0], w[2 * p + 1 < NT ? 2 * p + 1 : 0][1]);
-          a[3] = Mma<T>::pack(w[2 * p + 1 < NT ? 2 * p + 1 : 0][2], w[2 * p + 1 < NT ? 2 * p + 1 : 0][3]);
+          a[2] = Mma<T>::pack(w[o][0], w[o][1]);
+          a[3] = Mma<T>::pack(w[o][2], w[o][3]);
         }
       }
       auto tile = [&](int n, uint32_t b0, uint32_t b1) {
-        b0 &= m0;
-        b1 &= m1;
         if (!WIDE) {
-          if (half) Mma<T>::k8(acc[n], a[0], a[1], b0);
-          else Mma<T>::k16(acc[n], a[0], a[1], a[2], a[3], b0, b1);
+          if (half) Mma<T>::template k8<false>(acc[n], a[0], a[1], b0);
+          else Mma<T>::template k16<false>(acc[n], a[0], a[1], a[2], a[3], b0, b1);
         } else {  // eight rows each; their order in the product is that of the accumulators: 0, 2, 4, 6, 1, 3, 5, 7
           const float2 u = __half22float2(*reinterpret_cast<const __half2*>(&b0));
-          mma_tf32(acc[n], tf32(w[2 * p][0]), tf32(w[2 * p][2]), tf32(w[2 * p][1]), tf32(w[2 * p][3]), __float_as_uint(u.x), __float_as_uint(u.y));
+          mma_tf32<false>(acc[n], tf32(w[2 * p][0]), tf32(w[2 * p][2]), tf32(w[2 * p][1]), tf32(w[2 * p][3]), __float_as_uint(u.x), __float_as_uint(u.y));
           if (!half) {
-            constexpr int last = NT - 1;
-            const int o = 2 * p + 1 < NT ? 2 * p + 1 : last;
             const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&b1));
-            mma_tf32(acc[n], tf32(w[o][0]), tf32(w[o][2]), tf32(w[o][1]), tf32(w[o][3]), __float_as_uint(v.x), __float_as_uint(v.y));
+            mma_tf32<false>(acc[n], tf32(w[o][0]), tf32(w[o][2]), tf32(w[o][1]), tf32(w[o][3]), __float_as_uint(v.x), __float_as_uint(v.y));
           }
         }
       };
-      if (half) {
-        const uint32_t rb = b + (p * 16 + (lane & 7)) * pitch + ((lane >> 3) & 1) * 16;
+      const uint32_t rb = half ? b + (p * 16 + (lane & 7)) * pitch + ((lane >> 3) & 1) * 16 : b + (p * 16 + (lane & 15)) * pitch + (lane >> 4) * 16;
 #pragma unroll
-        for (int n = 0; n < DT / 8; n += 2) {
-          if (!kExact<DT> && n * 8 >= dim) break;
+      for (int n = 0; n < DT / 8; n += 2) {
+        if (!kExact<DT> && n * 8 >= dim) break;
+        const bool two = kExact<DT> ? n + 2 <= DT / 8 : n * 8 + 16 <= dim;
+        const int n1 = n + 1 < DT / 8 ? n + 1 : n;
+        if (half) {
           uint32_t g0, g1;  // (behind the last channel: the next head's, or the end of the row, not used)
           ldsm2_t(g0, g1, rb + n * 16);
           tile(n, g0, 0u);
-          if (kExact<DT> ? n + 2 <= DT / 8 : n * 8 + 16 <= dim) tile(n + 1 < DT / 8 ? n + 1 : n, g1, 0u);
-        }
-      } else {
-        const uint32_t rb = b + (p * 16 + (lane & 15)) * pitch + (lane >> 4) * 16;
-#pragma unroll
-        for (int n = 0; n < DT / 8; n += 2) {
-          if (!kExact<DT> && n * 8 >= dim) break;
-          if (kExact<DT> ? n + 2 <= DT / 8 : n * 8 + 16 <= dim) {
-            uint32_t g[4];
-            ldsm4_t(g, rb + n * 16);
-            tile(n, g[0], g[1]);
-            tile(n + 1 < DT / 8 ? n + 1 : n, g[2], g[3]);
-          } else {
-            uint32_t g0, g1;
-            ldsm2_t(g0, g1, b + (p * 16 + (lane & 15)) * pitch + n * 16);
-            tile(n, g0, g1);
-          }
+          if (two) tile(n1, g1, 0u);
+        } else if (two) {
+          uint32_t g[4];
+          ldsm4_t(g, rb + n * 16);
+          tile(n, g[0], g[1]);
+          tile(n1, g[2], g[3]);
+        } else {
+          uint32_t g0, g1;
+          ldsm2_t(g0, g1, b + (p * 16 + (lane & 15)) * pitch + n * 16);
+          tile(n, g0, g1);
         }
       }
     }
@@ -271,17 +282,23 @@ __device__ __forceinline__ void weigh(float (&acc)[DT / 8][4], const float (&w)[
       float c[4] = {}, s[4] = {};
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-        const uint32_t mine = (uint32_t)(real >> (8 * t)) >> q2;
-        const float x0 = lds(rb + t * 8 * pitch + n * 32), x1 = lds(rb + (t * 8 + 1) * pitch + n * 32);
-        const Parts g0 = split((mine & 1) ? x0 : 0.f), g1 = split((mine & 2) ? x1 : 0.f);
-        mma_tf32(s, a[t][0].lo, a[t][1].lo, a[t][2].lo, a[t][3].lo, g0.hi, g1.hi);
-        mma_tf32(s, a[t][0].hi, a[t][1].hi, a[t][2].hi, a[t][3].hi, g0.lo, g1.lo);
-        mma_tf32(c, a[t][0].hi, a[t][1].hi, a[t][2].hi, a[t][3].hi, g0.hi, g1.hi);
+        const Parts g0 = split(lds(rb + t * 8 * pitch + n * 32)), g1 = split(lds(rb + (t * 8 + 1) * pitch + n * 32));
+        mma_tf32<false>(s, a[t][0].lo, a[t][1].lo, a[t][2].lo, a[t][3].lo, g0.hi, g1.hi);
+        mma_tf32<false>(s, a[t][0].hi, a[t][1].hi, a[t][2].hi, a[t][3].hi, g0.lo, g1.lo);
+        mma_tf32<false>(c, a[t][0].hi, a[t][1].hi, a[t][2].hi, a[t][3].hi, g0.hi, g1.hi);
       }
 #pragma unroll
       for (int e = 0; e < 4; ++e) acc[n][e] += c[e] + s[e];
     }
   }
+}
+
+// Two neighbours of a tile's four values.
+__device__ __forceinline__ F2 two(const float (&z)[4], int e) { return pair(z[e], z[e + 1]); }
+__device__ __forceinline__ void put(float (&z)[4], int e, F2 v) {
+  const float2 f = parts(v);
+  z[e] = f.x;
+  z[e + 1] = f.y;
 }
 
 // The scores' transformation: products -> scale, cap, bias, in units of log 2.
@@ -316,10 +333,11 @@ __device__ __forceinline__ float bias_log2(float b) { return b == -INFINITY ? b 
 template <bool SLOPE>
 __device__ __forceinline__ void score_of(const Scoring& s, float (&z)[4], const float (&bias)[4], float (&slope)[4]) {
   if (s.cap == 0.f) {
+    const F2 scale = pair(s.scale, s.scale);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      z[e] = fmaf(z[e], s.scale, bias[e]);
-      if (SLOPE) slope[e] = 1.f;
+    for (int e = 0; e < 4; e += 2) {
+      put(z, e, fma2(pair(z[e], z[e + 1]), scale, pair(bias[e], bias[e + 1])));
+      if (SLOPE) slope[e] = slope[e + 1] = 1.f;
     }
   } else {
 #pragma unroll
