@@ -10,8 +10,10 @@
 // inputs give the same bits: v = (hi 2^-17 + lo 2^-35) limit with |hi|, |lo| <= 2^17, two words of shared memory to a bucket, which
 // take 16,000 values before they are emptied into floats (short: the block's own partial sums) or 64-bit integers in global memory
 // (long).  limit is a power of two that bounds |ds|, from the first pass: |p dp| + |p D| <= max_j |p dp| + |D| max_j p, and at most four
-// times that.  A value is off by 2^-36 of the limit.  Integer additions in shared memory are also the fast ones here: 1.3 ns a warp,
-// fp32's 6 ns, 64-bit 11 ns.
+// times that.  A value is off by 2^-36 of the limit.  Integer additions in shared memory are also the fast ones here: 1.4 ns a warp where
+// the addresses differ, fp32's 6 ns, 64-bit 11 ns.  Where they are the same they follow one another (8 lanes to an address: 5 ns), and
+// neighbouring keys and queries have the same displacements; so the four lanes that share a key add to tables of their own where there
+// is room, or two and two.
 #pragma once
 #include "segment_forward.cuh"
 
@@ -45,9 +47,9 @@ static __device__ __noinline__ void odd_value(int* at, uint32_t* spoilt, int ent
 }
 
 struct Tally {
-  int* hist;           // [heads][2][buckets]
+  int* hist;           // [copies][heads][2][buckets]
   uint32_t* spoilt;    // bits [heads][buckets]
-  int buckets;
+  int buckets, copies, copy;  // copy: entries of one
   float limit, to_hi;  // to_hi = 2^kHiBits / limit
   bool on;
   __device__ __forceinline__ void bound(float b) {
@@ -56,24 +58,62 @@ struct Tally {
     limit = __int_as_float((e + 127) << 23);
     to_hi = __int_as_float((kHiBits - e + 127) << 23);
   }
-  // Two values; x, y: their buckets times 4.
-  __device__ __forceinline__ void add2(int h, int x, int y, float v, float w) const {
-    char* base = reinterpret_cast<char*>(hist + 2 * h * buckets);
-    int *to = reinterpret_cast<int*>(base + x), *tu = reinterpret_cast<int*>(base + y);
-    if (!(fmaxf(fabsf(v), fabsf(w)) <= limit) || v != v || w != w) {  // (a maximum passes over a NaN)
-      odd_value(to, spoilt, h * buckets + (x >> 2), v, limit, to_hi, buckets);
-      odd_value(tu, spoilt, h * buckets + (y >> 2), w, limit, to_hi, buckets);
+  template <int N>
+  __device__ __forceinline__ void clear_all(int heads) const {
+    for (int i = threadIdx.x; i < copies * copy; i += N) hist[i] = 0;
+    for (int i = threadIdx.x; i < (heads * buckets + 31) / 32; i += N) spoilt[i] = 0;
+  }
+  // Entry i of the table [heads][buckets]: its words, which are cleared, and whether a value of it was not finite.
+  __device__ __forceinline__ bool take(int i, long long& hi, long long& lo) const {
+    const int h = i / buckets, at = 2 * h * buckets + i - h * buckets;
+    hi = lo = 0;
+    for (int c = 0; c < copies; ++c) {
+      int* p = hist + c * copy + at;
+      hi += p[0];
+      lo += p[buckets];
+      p[0] = p[buckets] = 0;
+    }
+    return spoilt[i >> 5] >> (i & 31) & 1;
+  }
+  // A chunk's values of head h; bk: their buckets times 4.  SOME: those whose bit, 4 t + e, is set.
+  template <int NT, bool SOME>
+  __device__ __forceinline__ void count(int h, const int (&bk)[NT][4], const float (&v)[NT][4], uint32_t which) const {
+    char* base = reinterpret_cast<char*>(hist + (threadIdx.x & (copies - 1)) * copy + 2 * h * buckets);
+    float most = 0.f;
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (!SOME || (which >> (4 * t + e) & 1)) asm("max.NaN.f32 %0, %0, %1;" : "+f"(most) : "f"(fabsf(v[t][e])));
+    if (__any_sync(kAll, !(most <= limit))) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (!SOME || (which >> (4 * t + e) & 1))
+            odd_value(reinterpret_cast<int*>(base + bk[t][e]), spoilt, h * buckets + (bk[t][e] >> 2), v[t][e], limit, to_hi, buckets);
       return;
     }
-    const F2 z = pair(v, w), scale = pair(to_hi, to_hi), magic = pair(kMagic, kMagic);
-    const F2 t = fma2(z, scale, magic), minus = pair(-1.f, -1.f);
-    const F2 r = fma2(z, scale, mul(add(t, pair(-kMagic, -kMagic)), minus));
-    const F2 u = fma2(r, pair((float)(1 << kLoBits), (float)(1 << kLoBits)), magic);
+    const F2 scale = pair(to_hi, to_hi), magic = pair(kMagic, kMagic), back = pair(-kMagic, -kMagic), minus = pair(-1.f, -1.f);
+    const F2 lo = pair((float)(1 << kLoBits), (float)(1 << kLoBits));
     const int zero = __float_as_int(kMagic);
-    atomicAdd(to, __float_as_int(parts(t).x) - zero);
-    atomicAdd(to + buckets, __float_as_int(parts(u).x) - zero);
-    atomicAdd(tu, __float_as_int(parts(t).y) - zero);
-    atomicAdd(tu + buckets, __float_as_int(parts(u).y) - zero);
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; e += 2) {
+        const F2 z = two(v[t], e), x = fma2(z, scale, magic);
+        const F2 u = fma2(fma2(z, scale, mul(add(x, back), minus)), lo, magic);
+        if (!SOME || (which >> (4 * t + e) & 1)) {
+          int* p = reinterpret_cast<int*>(base + bk[t][e]);
+          atomicAdd(p, __float_as_int(parts(x).x) - zero);
+          atomicAdd(p + buckets, __float_as_int(parts(u).x) - zero);
+        }
+        if (!SOME || (which >> (4 * t + e + 1) & 1)) {
+          int* q = reinterpret_cast<int*>(base + bk[t][e + 1]);
+          atomicAdd(q, __float_as_int(parts(x).y) - zero);
+          atomicAdd(q + buckets, __float_as_int(parts(u).y) - zero);
+        }
+      }
   }
 };
 
@@ -136,27 +176,16 @@ __device__ __forceinline__ void differ_weights(const float (&s)[NT][4], float (&
   }
 }
 
-// The same from products, s = q k.
+// The same from scores.
 template <int NT>
-__device__ __forceinline__ void differ_rows(float (&s)[NT][4], float (&dp)[NT][4], const Scoring& sc, const float* bias, const uint16_t* index, int pitch,
-                                            const float3 (&st)[2], uint64_t real) {
+__device__ __forceinline__ void differ_rows(const float (&s)[NT][4], float (&dp)[NT][4], const float3 (&st)[2]) {
 #pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    float slope[4];
-    score_tile<true>(s[t], slope, sc, bias, index + t * 8, pitch, (uint32_t)(real >> (8 * t)));
+  for (int r = 0; r < 2; ++r) {
+    const F2 down = pair(-st[r].x, -st[r].x), inv = pair(st[r].y, st[r].y), D = pair(-st[r].z, -st[r].z);
 #pragma unroll
-    for (int r = 0; r < 2; ++r) {
-      const float2 x = parts(add(two(s[t], 2 * r), pair(-st[r].x, -st[r].x)));
-      const F2 p = mul(pair(ex2_approx(x.x), ex2_approx(x.y)), pair(st[r].y, st[r].y));
-      F2 dz = mul(p, add(two(dp[t], 2 * r), pair(-st[r].z, -st[r].z)));
-      if (sc.cap != 0.f) dz = mul(dz, two(slope, 2 * r));
-      put(dp[t], 2 * r, dz);
-    }
-    // (a column without a key: its weight is zero, but a product of what lies there need not be a number)
-    if (((uint32_t)(real >> (8 * t)) & 0xffu) != 0xffu) {
-      const uint32_t mine = (uint32_t)(real >> (8 * t)) >> ((threadIdx.x & 3) * 2);
-      if (!(mine & 1)) dp[t][0] = dp[t][2] = 0.f;
-      if (!(mine & 2)) dp[t][1] = dp[t][3] = 0.f;
+    for (int t = 0; t < NT; ++t) {
+      const float2 x = parts(add(two(s[t], 2 * r), down));
+      put(dp[t], 2 * r, mul(mul(pair(ex2_approx(x.x), ex2_approx(x.y)), inv), add(two(dp[t], 2 * r), D)));
     }
   }
 }
@@ -167,28 +196,12 @@ struct ColumnStats {
   int step;
 };
 
-// The second pass's chunk: rows are keys, columns queries.  s: products k q -> p; dp: products v do -> dz.  `index`: buckets, at the first
-// row and column of the fragment (ROWS: [key][query], else [query][key]); `stats`: at the first column.
-template <int NT, bool ROWS>
-__device__ __forceinline__ void differ_columns(float (&s)[NT][4], float (&dp)[NT][4], const Scoring& sc, const float* bias, const uint16_t* index, int pitch,
-                                               const ColumnStats& stats, uint64_t real, const Tally& tally, int h, bool count0, bool count1) {
-  const int g = (threadIdx.x & 31) >> 2, q2 = (threadIdx.x & 3) * 2;
+// The second pass's chunk: rows are keys, columns queries.  s: scores -> p; dp: products v do -> ds.
+template <int NT>
+__device__ __forceinline__ void differ_columns(float (&s)[NT][4], float (&dp)[NT][4], const ColumnStats& stats) {
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
-    int bk[4] = {};
-    float b[4] = {}, slope[4];
-    if (sc.bias) {
-      if (ROWS) {
-        buckets_of(bk, index + t * 8, pitch);
-      } else {
-        const uint16_t* at = index + (t * 8 + q2) * pitch + g;
-        bk[0] = at[0] & kBucketMask; bk[1] = at[pitch] & kBucketMask; bk[2] = at[8] & kBucketMask; bk[3] = at[pitch + 8] & kBucketMask;
-      }
-#pragma unroll
-      for (int e = 0; e < 4; ++e) b[e] = bias_at(bias, bk[e]);
-    }
-    score_of<true>(sc, s[t], b, slope);
-    const float* st = stats.at + t * 8 + q2;
+    const float* st = stats.at + t * 8 + (threadIdx.x & 3) * 2;
     const float2 m = *reinterpret_cast<const float2*>(st), i = *reinterpret_cast<const float2*>(st + stats.step), D = *reinterpret_cast<const float2*>(st + 2 * stats.step);
     const F2 down = pair(-m.x, -m.y), inv = pair(i.x, i.y), less = pair(-D.x, -D.y);
 #pragma unroll
@@ -198,22 +211,6 @@ __device__ __forceinline__ void differ_columns(float (&s)[NT][4], float (&dp)[NT
       put(s[t], e, p);
       put(dp[t], e, mul(p, add(two(dp[t], e), less)));
     }
-    if (((uint32_t)(real >> (8 * t)) & 0xffu) != 0xffu) {  // columns without a query: whatever lies there
-      const uint32_t mine = (uint32_t)(real >> (8 * t)) >> q2;
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (!((mine >> (e & 1)) & 1)) {
-          s[t][e] = dp[t][e] = slope[e] = 0.f;
-          bk[e] = 0;  // (an unwritten bucket may lie outside of the table)
-        }
-    }
-    if (tally.on) {
-      if (count0) tally.add2(h, bk[0], bk[1], dp[t][0], dp[t][1]);
-      if (count1) tally.add2(h, bk[2], bk[3], dp[t][2], dp[t][3]);
-    }
-    if (sc.cap != 0.f)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) dp[t][e] *= slope[e];
   }
 }
 
@@ -260,67 +257,96 @@ __device__ __forceinline__ void products(float (&s)[NT][4], float (&dp)[NT][4], 
   scores<T, DT, NT>(dp, x.o, x.cv, x.pitch, x.dim);
   set_columns<NT>(dp, keys, 0.f);  // (whatever lies there)
 }
+// dp: ds -> dz; s is written over.
+template <typename T, int DT, int NT>
+__device__ __forceinline__ void through_cap(float (&s)[NT][4], float (&dp)[NT][4], uint32_t a, uint32_t b, const Operands& x, const Scoring& sc, uint64_t real) {
+  if (sc.cap == 0.f) return;
+  scores<T, DT, NT>(s, a, b, x.pitch, x.dim);
+  cap_slope<NT>(dp, s, sc);
+  set_columns<NT>(dp, real, 0.f);
+}
 // A segment whose keys are one chunk: everything of the tile's rows at once.
 template <typename T, int DT, int NT>
 __device__ __forceinline__ void rows_at_once(float (&acc)[DT / 8][4], float3 (&st)[2], float (&bound)[2], const Operands& x, const Scoring& sc, uint64_t keys) {
-  float s1[1][NT][4], dp[NT][4];
-  float(&s)[NT][4] = s1[0];
+  float s[NT][4], dp[NT][4];
   products<T, DT, NT>(s, dp, x, keys);
-  transform<1, NT>(s1, sc, x.bias, 0, x.index, x.pitch_idx, keys);
+  transform<NT>(s, sc, x.bias, x.index, x.pitch_idx, keys);
   RowSums f;
   f.start();
   sum_rows<NT>(f, s, dp);
   st[0] = row_stats(f, 0, &bound[0]);
   st[1] = row_stats(f, 1, &bound[1]);
-  if (sc.cap == 0.f) {
-    differ_weights<NT>(s, dp, st);
-  } else {
-    scores<T, DT, NT>(s, x.q, x.ck, x.pitch, x.dim);
-    differ_rows<NT>(s, dp, sc, x.bias, x.index, x.pitch_idx, st, keys);
-  }
+  differ_weights<NT>(s, dp, st);
+  through_cap<T, DT, NT>(s, dp, x.q, x.ck, x, sc, keys);
   weigh<T, DT, NT, kWide<T>>(acc, dp, x.ck, x.pitch, x.dim);
 }
 template <typename T, int DT, int NT>
 __device__ __forceinline__ void rows_first(RowSums& f, const Operands& x, const Scoring& sc, uint64_t keys) {
-  float s1[1][NT][4], dp[NT][4];
-  float(&s)[NT][4] = s1[0];
+  float s[NT][4], dp[NT][4];
   products<T, DT, NT>(s, dp, x, keys);
-  transform<1, NT>(s1, sc, x.bias, 0, x.index, x.pitch_idx, keys);
+  transform<NT>(s, sc, x.bias, x.index, x.pitch_idx, keys);
   sum_rows<NT>(f, s, dp);
 }
 template <typename T, int DT, int NT>
 __device__ __forceinline__ void rows_second(float (&acc)[DT / 8][4], const float3 (&st)[2], const Operands& x, const Scoring& sc, uint64_t keys) {
   float s[NT][4], dp[NT][4];
   products<T, DT, NT>(s, dp, x, keys);
-  differ_rows<NT>(s, dp, sc, x.bias, x.index, x.pitch_idx, st, keys);
+  transform<NT>(s, sc, x.bias, x.index, x.pitch_idx, keys);
+  differ_rows<NT>(s, dp, st);
+  through_cap<T, DT, NT>(s, dp, x.q, x.ck, x, sc, keys);
   weigh<T, DT, NT, kWide<T>>(acc, dp, x.ck, x.pitch, x.dim);
 }
-// By keys.
+// By keys.  `rows`: bit i says whether row i of the tile holds a voxel.
 template <typename T, int DT, int NT, bool ROWS>
 __device__ __forceinline__ void columns(float (&dk)[DT / 8][4], float (&dv)[DT / 8][4], const Operands& x, const Scoring& sc, const ColumnStats& stats, uint64_t queries,
-                                        const Tally& tally, int h, bool count0, bool count1) {
+                                        const Tally& tally, int h, uint32_t rows) {
   float s[NT][4], dp[NT][4];
+  int bk[NT][4];
   scores<T, DT, NT>(s, x.k, x.cq, x.pitch, x.dim);
   scores<T, DT, NT>(dp, x.v, x.co, x.pitch, x.dim);
-  differ_columns<NT, ROWS>(s, dp, sc, x.bias, x.index, x.pitch_idx, stats, queries, tally, h, count0, count1);
-  weigh<T, DT, NT, kWide<T>>(dk, dp, x.cq, x.pitch, x.dim);
+  score_tiles<NT, ROWS>(s, bk, sc, x.bias, x.index, x.pitch_idx);
+  differ_columns<NT>(s, dp, stats);
+  set_columns<NT>(s, queries, 0.f);  // (whatever lies there)
+  set_columns<NT>(dp, queries, 0.f);
+  if (tally.on) {
+    const uint64_t full = ((uint64_t)1 << (8 * NT)) - 1;
+    if (ROWS && rows == 0xffffu && (queries & full) == full) {  // (of short segments hardly a tile is full: no code of its own)
+      tally.count<NT, false>(h, bk, dp, 0u);
+    } else {  // what lies in other rows and columns does not count
+      const int g = (threadIdx.x & 31) >> 2, q2 = (threadIdx.x & 3) * 2;
+      const uint32_t r0 = rows >> g & 1, r1 = rows >> (g + 8) & 1;
+      uint32_t which = 0;
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const uint32_t c = (uint32_t)(queries >> (8 * t + q2)) & 3u;
+        which |= ((r0 ? c : 0u) | (r1 ? c << 2 : 0u)) << (4 * t);
+      }
+      tally.count<NT, true>(h, bk, dp, which);
+    }
+  }
   weigh<T, DT, NT, false>(dv, s, x.co, x.pitch, x.dim);
+  through_cap<T, DT, NT>(s, dp, x.k, x.cq, x, sc, queries);
+  weigh<T, DT, NT, kWide<T>>(dk, dp, x.cq, x.pitch, x.dim);
 }
 
 // ---- short segments ------------------------------------------------------------------------------------------------
 struct BackLayout {
   ShortLayout s;
+  int copies;  // of the tally
   uint32_t stats, hist, spoilt, bytes;
 };
+// As many tables of a tally, up to four, as fit into `room` bytes.
+static int tally_copies(int bytes, int room) { return 4 * bytes <= room ? 4 : 2 * bytes <= room ? 2 : 1; }
 
 template <typename T, int DT>
-static BackLayout back_layout(const SegArgs& a, int limit) {
+static BackLayout back_layout(const SegArgs& a, int limit, int batch) {
   BackLayout l = {};
-  l.s = short_layout<T>(a, kBackHeads<T, DT>, limit, 4, 64);
+  l.s = short_layout<T>(a, kBackHeads<T, DT>, limit, 4, batch);
   uint32_t at = l.s.bytes;
   l.stats = at; at += l.s.heads * 3 * (l.s.batch + 16) * 4;
   if (a.dbias) {
-    l.hist = at; at += l.s.heads * 2 * a.buckets * 4;
+    l.copies = tally_copies(l.s.heads * 2 * a.buckets * 4, 16 * 1024);
+    l.hist = at; at += l.copies * l.s.heads * 2 * a.buckets * 4;
     l.spoilt = at; at += (l.s.heads * a.buckets + 31) / 32 * 4;
   }
   l.bytes = (at + 15) / 16 * 16;
@@ -348,13 +374,14 @@ __global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) short_backward_ker
   tally.hist = reinterpret_cast<int*>(smem + L.hist);
   tally.spoilt = reinterpret_cast<uint32_t*>(smem + L.spoilt);
   tally.buckets = a.buckets;
+  tally.copies = L.copies;
+  tally.copy = HG * 2 * a.buckets;
   tally.on = a.dbias != nullptr;
   tally.bound(0.f);
   stage_tables<kThreads>(a, maps, bias, head0, HG);
   float* mine = work.partial + (int64_t)blockIdx.x * work.table + head0 * a.buckets;
   if (tally.on) {
-    for (int i = threadIdx.x; i < HG * 2 * a.buckets; i += kThreads) tally.hist[i] = 0;
-    for (int i = threadIdx.x; i < (HG * a.buckets + 31) / 32; i += kThreads) tally.spoilt[i] = 0;
+    tally.clear_all<kThreads>(HG);
     // what the long segments' kernels add to starts at zero
     const int first = (blockIdx.y * gridDim.x + blockIdx.x) * kThreads + threadIdx.x, step = gridDim.x * gridDim.y * kThreads;
     for (int i = first; i < 2 * work.table; i += step) work.total[i] = 0;
@@ -365,12 +392,10 @@ __global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) short_backward_ker
   int pending = 0;
   auto empty = [&]() {  // all threads; a barrier before and after
     for (int i = threadIdx.x; i < heads * a.buckets; i += kThreads) {
-      const int h = i / a.buckets, at = 2 * h * a.buckets + i - h * a.buckets;
-      const float v = tally_value(tally.hist[at], tally.hist[at + a.buckets], tally.limit);
-      float sum = emptied ? mine[i] + v : v;
-      if (tally.spoilt[i >> 5] >> (i & 31) & 1) sum = NAN;
-      mine[i] = sum;
-      tally.hist[at] = tally.hist[at + a.buckets] = 0;
+      long long hi, lo;
+      const bool spoilt = tally.take(i, hi, lo);
+      const float v = tally_value(hi, lo, tally.limit), sum = emptied ? mine[i] + v : v;
+      mine[i] = spoilt ? NAN : sum;
     }
     emptied = true;
     pending = 0;
@@ -430,21 +455,18 @@ __global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) short_backward_ker
           RowSums f;
           f.start();
           const int tiles = (item.len + 7) >> 3;
-          for (int pass = 0; pass < 2; ++pass) {  // in parts of 3 and 4 tiles
-            int parts = (tiles + 3) / 4, left = tiles;
-            for (int j = 0; left > 0; --parts) {
-              const int now = (left + parts - 1) / parts;
+          for (int pass = 0; pass < 2; ++pass) {  // two tiles at a time
+            for (int j = 0; j < item.len; j += 16) {
+              const int now = min(2, tiles - (j >> 3));
               const uint64_t keys = real_rows(plan, item.at + j, min(8 * now, item.len - j));
               to_chunk(j);
               if (pass == 0) {
-                if (now == 4) rows_first<T, DT, 4>(f, x, sc, keys);
-                else rows_first<T, DT, 3>(f, x, sc, keys);
+                if (now == 2) rows_first<T, DT, 2>(f, x, sc, keys);
+                else rows_first<T, DT, 1>(f, x, sc, keys);
               } else {
-                if (now == 4) rows_second<T, DT, 4>(acc, st, x, sc, keys);
-                else rows_second<T, DT, 3>(acc, st, x, sc, keys);
+                if (now == 2) rows_second<T, DT, 2>(acc, st, x, sc, keys);
+                else rows_second<T, DT, 1>(acc, st, x, sc, keys);
               }
-              j += 8 * now;
-              left -= now;
             }
             if (pass == 0) {
               st[0] = row_stats(f, 0, &bound[0]);
@@ -487,19 +509,18 @@ __global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) short_backward_ker
         clear<DT>(dk);
         clear<DT>(dv);
         x.k = k0 + row * pitch + at_head; x.v = v0 + row * pitch + at_head;
-        for (int j = 0; j < item.len; j += 32) {
-          const int cols = min(32, item.len - j);
+        const uint32_t tile_rows = (uint32_t)real_rows(plan, row, min(16, item.len - 16 * item.tile));
+        // (Two tiles at a time and not four: half the code, and no spilled registers.  Kernels of this size miss in the instruction cache:
+        // 32,000 pillars bf16 148 us with four, 127 with two; fp32, 12,345 with a cap, 352 and 255.)
+        for (int j = 0; j < item.len; j += 16) {
+          const int cols = min(16, item.len - j);
           const uint64_t queries = real_rows(plan, item.at + j, cols);
           const uint32_t at = (item.at + j) * pitch + at_head;
           const ColumnStats from = {stats + 3 * h * stat_rows + item.at + j, stat_rows};
           x.cq = q0 + at; x.co = o0 + at;
           x.index = index + (item.at + j) * L.s.pitch_idx + 16 * item.tile;
-          switch ((cols + 7) >> 3) {
-            case 1: columns<T, DT, 1, false>(dk, dv, x, sc, from, queries, tally, h, id0 >= 0, id1 >= 0); break;
-            case 2: columns<T, DT, 2, false>(dk, dv, x, sc, from, queries, tally, h, id0 >= 0, id1 >= 0); break;
-            case 3: columns<T, DT, 3, false>(dk, dv, x, sc, from, queries, tally, h, id0 >= 0, id1 >= 0); break;
-            default: columns<T, DT, 4, false>(dk, dv, x, sc, from, queries, tally, h, id0 >= 0, id1 >= 0);
-          }
+          if (cols > 8) columns<T, DT, 2, false>(dk, dv, x, sc, from, queries, tally, h, tile_rows);
+          else columns<T, DT, 1, false>(dk, dv, x, sc, from, queries, tally, h, tile_rows);
         }
         store_rows<T, DT>(dk, a.scale, a.dk, a.ld_dk, col + h * dim, dim, id0, id1);
         store_rows<T, DT>(dv, 1.f, a.dv, a.ld_dv, col + h * dim, dim, id0, id1);
@@ -523,7 +544,7 @@ struct BackShape {
 };
 
 struct BackLongLayout {
-  int pitch_idx;
+  int pitch_idx, copies;
   uint32_t pitch, tile, chunk;
   uint32_t maps, bias, cells, passing_cells, ids, index, stats, hist, spoilt, rows, passing, bytes;
 };
@@ -549,7 +570,8 @@ static BackLongLayout back_long_layout(const SegArgs& a, bool by_keys) {
   if (by_keys) {
     l.stats = take((size_t)3 * S::HG * 3 * S::chunk * 4);
     if (a.dbias) {
-      l.hist = take((size_t)S::HG * 2 * a.buckets * 4);
+      l.copies = tally_copies(S::HG * 2 * a.buckets * 4, 38 * 1024);
+      l.hist = take((size_t)l.copies * S::HG * 2 * a.buckets * 4);
       l.spoilt = take((size_t)(S::HG * a.buckets + 31) / 32 * 4);
     }
   }
@@ -583,21 +605,20 @@ __global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) long_backward_kern
   tally.hist = reinterpret_cast<int*>(smem + L.hist);
   tally.spoilt = reinterpret_cast<uint32_t*>(smem + L.spoilt);
   tally.buckets = a.buckets;
+  tally.copies = L.copies;
+  tally.copy = S::HG * 2 * a.buckets;
   tally.on = BY_KEYS && a.dbias != nullptr;
   if (tally.on) {
     tally.bound(__uint_as_float(*work.bound));
-    for (int i = threadIdx.x; i < S::HG * 2 * a.buckets; i += kThreads) tally.hist[i] = 0;
-    for (int i = threadIdx.x; i < (S::HG * a.buckets + 31) / 32; i += kThreads) tally.spoilt[i] = 0;
+    tally.clear_all<kThreads>(S::HG);
   }
   auto empty = [&]() {  // all threads; a barrier before and after
     for (int i = threadIdx.x; i < heads * a.buckets; i += kThreads) {
-      const int h = i / a.buckets, at = 2 * h * a.buckets + i - h * a.buckets;
-      const long long hi = tally.hist[at], lo = tally.hist[at + a.buckets];
-      unsigned long long* to = work.total + head0 * a.buckets + i;
-      if (hi) atomicAdd(to, (unsigned long long)hi);
-      if (lo) atomicAdd(to + work.table, (unsigned long long)lo);
-      if (tally.spoilt[i >> 5] >> (i & 31) & 1) { const int w = head0 * a.buckets + i; atomicOr(work.spoilt + (w >> 5), 1u << (w & 31)); }
-      tally.hist[at] = tally.hist[at + a.buckets] = 0;
+      long long hi, lo;
+      const int w = head0 * a.buckets + i;
+      if (tally.take(i, hi, lo)) atomicOr(work.spoilt + (w >> 5), 1u << (w & 31));
+      if (hi) atomicAdd(work.total + w, (unsigned long long)hi);
+      if (lo) atomicAdd(work.total + w + work.table, (unsigned long long)lo);
     }
   };
   stage_tables<kThreads>(a, maps, bias, head0, S::HG);
@@ -617,16 +638,27 @@ __global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) long_backward_kern
     auto cells_of = [&](int c) { return reinterpret_cast<int4*>(smem + L.passing_cells) + c % 3 * S::chunk; };
     auto stats_of = [&](int c) { return reinterpret_cast<float*>(smem + L.stats) + c % 3 * (S::HG * 3 * S::chunk); };  // [heads][3][chunk]
     auto array = [&](int c, int which) { return smem_u32(smem + L.passing) + ((c & 1) * 2 + which) * L.chunk; };
+    // Rows of whole tiles and chunks are dealt out, so that the 8 rows and 4 columns of a score tile that a warp counts at once lie apart:
+    // neighbours' displacements would meet in the same bucket, and additions to one address follow one another.
+    auto dealt = [&](int place, int count) { return BY_KEYS ? place % 8 * (count / 8) + place / 8 : place; };
     __syncthreads();  // (the tile before is done with the shared memory)
     if (threadIdx.x < S::rows) {
-      const int id = (int)threadIdx.x < rows ? voxel_at(a, tile.row + threadIdx.x) : -1;
+      const int at = rows == S::rows ? dealt(threadIdx.x, S::rows) : threadIdx.x;
+      const int id = at < rows ? voxel_at(a, tile.row + at) : -1;
       ids[threadIdx.x] = id;
       if (a.bias) cells[threadIdx.x] = id >= 0 ? a.coords[id] : make_int4(0, 0, 0, 0);
     }
+    auto chunk_row = [&](int c, int place) {
+      const int from = tile.lo + c * S::chunk;
+      return from + (from + S::chunk <= tile.hi ? dealt(place, S::chunk) : place);
+    };
     int next = -1;  // this thread's voxel of the next chunk
     auto fetch_id = [&](int c) {
-      const int at = tile.lo + c * S::chunk + (int)threadIdx.x;
-      next = threadIdx.x < S::chunk && at < tile.hi ? voxel_at(a, at) : -1;
+      next = -1;
+      if (threadIdx.x < S::chunk) {
+        const int at = chunk_row(c, threadIdx.x);
+        if (at < tile.hi) next = voxel_at(a, at);
+      }
     };
     auto publish = [&](int c) {
       if (threadIdx.x < S::chunk) {
@@ -635,7 +667,7 @@ __global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) long_backward_kern
       }
       if (BY_KEYS)
         for (int i = threadIdx.x; i < heads * S::chunk; i += kThreads) {
-          const int h = i / S::chunk, j = i % S::chunk, at = tile.lo + c * S::chunk + j;
+          const int h = i / S::chunk, j = i % S::chunk, at = chunk_row(c, j);
           const float* from = work.stats + ((int64_t)(head0 - work.head0 + h) * work.n + at) * 3;
 #pragma unroll
           for (int k = 0; k < 3; ++k) stats_of(c)[(3 * h + k) * S::chunk + j] = at < tile.hi ? from[k] : 0.f;
@@ -686,7 +718,8 @@ __global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) long_backward_kern
           }
           __syncthreads();
         }
-        uint64_t there = __ballot_sync(kAll, lane < S::chunk && ids_of(c)[lane] >= 0);
+        const uint64_t there = __ballot_sync(kAll, lane < S::chunk && ids_of(c)[lane] >= 0);
+        const uint32_t tile_rows = BY_KEYS ? __ballot_sync(kAll, lane < 16 && ids[row + lane] >= 0) : 0u;
 #pragma unroll
         for (int i = 0; i < HPW; ++i) {
           const int h = (warp % S::WH) * HPW + i;
@@ -703,7 +736,7 @@ __global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) long_backward_kern
             x.co = x.cv = array(c, 1) + j * pitch + at_head;
             x.index = index + row * L.pitch_idx + j;
             if constexpr (BY_KEYS) {
-              columns<T, DT, NT, true>(acc[i], dv[i], x, sc, ColumnStats{stats_of(c) + 3 * h * S::chunk + j, S::chunk}, bits, tally, h, ids[row + g] >= 0, ids[row + g + 8] >= 0);
+              columns<T, DT, NT, true>(acc[i], dv[i], x, sc, ColumnStats{stats_of(c) + 3 * h * S::chunk + j, S::chunk}, bits, tally, h, tile_rows);
             } else {
               if (sweep == 0) rows_first<T, DT, NT>(f[i], x, sc, bits);
               else rows_second<T, DT, NT>(acc[i], st[i], x, sc, bits);
@@ -775,8 +808,11 @@ static __global__ void __launch_bounds__(kThreads) bias_grad_kernel(const BackWo
 template <typename T, int DT>
 int backward_of(dsvt_ctx* ctx, const SegArgs& a) {
   int limit = a.max_len <= kShort ? a.max_len : 64;
-  BackLayout l = back_layout<T, DT>(a, limit);
-  while (l.bytes > kSmemMost) l = back_layout<T, DT>(a, limit = limit > 64 ? 64 : limit / 2);
+  // the largest batch that leaves room for two blocks on an SM (32,000 pillars bf16: 64 rows 103 us, 80 rows 97), if one does
+  int batch = 96;
+  BackLayout l = back_layout<T, DT>(a, limit, batch);
+  while (l.bytes > kSmemHalf && batch > 48) l = back_layout<T, DT>(a, limit, batch -= 8);
+  while (l.bytes > kSmemMost) l = back_layout<T, DT>(a, limit = limit > 64 ? 64 : limit / 2, batch);
   const Scoring sc = scoring_of(a);
   const int groups = (int)dsvt_ceil_div(a.heads, kBackHeads<T, DT>);
   BackWork w = {};
@@ -790,10 +826,10 @@ int backward_of(dsvt_ctx* ctx, const SegArgs& a) {
   w.table = a.dbias ? a.heads * a.buckets : 0;
   w.n = a.n;
   // blocks that stay: two to an SM where they fit, and as many as have room for their partial sums
-  const int per_sm = DT <= 32 && l.bytes <= kSmemMost / 2 ? 2 : 1;
+  const int per_sm = DT <= 32 && l.bytes <= kSmemHalf ? 2 : 1;
   int64_t stay = dsvt_ceil_div(per_sm * ctx->sm_count, groups);
   if (w.table > 0 && stay > (int64_t)kPartialWords / w.table) stay = kPartialWords / w.table;
-  set_ranges(l.s, a.n, (int)stay, 128);
+  set_ranges(l.s, a.n, (int)stay, limit < a.max_len ? 128 : 1 << 20);
   if (stay > l.s.ranges) stay = l.s.ranges;
   w.blocks = (int)stay;
   constexpr auto kernel = short_backward_kernel<T, DT>;

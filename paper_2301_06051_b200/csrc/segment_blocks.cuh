@@ -225,30 +225,6 @@ __device__ __forceinline__ void buckets_of(int (&bk)[4], const uint16_t* index, 
 }
 __device__ __forceinline__ float bias_at(const float* bias, int bk) { return *reinterpret_cast<const float*>(reinterpret_cast<const char*>(bias) + bk); }
 
-// A tile of scores of queries (rows) and keys (columns) from products; -inf where a column holds no key.
-template <bool SLOPE>
-__device__ __forceinline__ void score_tile(float (&s)[4], float (&slope)[4], const Scoring& sc, const float* bias, const uint16_t* index, int pitch, uint32_t bits) {
-  float b[4] = {};
-  if (sc.bias) {
-    int bk[4];
-    buckets_of(bk, index, pitch);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) b[e] = bias_at(bias, bk[e]);
-  }
-  score_of<SLOPE>(sc, s, b, slope);
-  if ((bits & 0xffu) != 0xffu) {
-    const uint32_t mine = bits >> ((threadIdx.x & 3) * 2);
-    if (!(mine & 1)) {
-      s[0] = s[2] = -INFINITY;
-      if (SLOPE) slope[0] = slope[2] = 0.f;
-    }
-    if (!(mine & 2)) {
-      s[1] = s[3] = -INFINITY;
-      if (SLOPE) slope[1] = slope[3] = 0.f;
-    }
-  }
-}
-
 // Sets the columns that hold no row.  Without gaps only the last tile has some.
 template <int NT>
 __device__ __forceinline__ void set_columns(float (&c)[NT][4], uint64_t real, float to) {
@@ -267,33 +243,39 @@ __device__ __forceinline__ void set_columns(float (&c)[NT][4], uint64_t real, fl
   if (!(last & 2)) c[NT - 1][1] = c[NT - 1][3] = to;
 }
 
-// `index`: the fragment's first row's buckets at the chunk's first column (rows g and g + 8 of the tile).  HP heads' products, biases `step`
-// entries apart.
-template <int HP, int NT>
-__device__ __forceinline__ void transform(float (&s)[HP][NT][4], const Scoring& sc, const float* bias, int step, const uint16_t* index, int pitch, uint64_t real) {
-  float none[4];
+// Scores from products, with the buckets' offsets in bk (by ROWS of the index as in buckets_of, else with the index's rows as columns).
+// `index`: at the tile's first row and the chunk's first column.
+template <int NT, bool ROWS>
+__device__ __forceinline__ void score_tiles(float (&s)[NT][4], int (&bk)[NT][4], const Scoring& sc, const float* bias, const uint16_t* index, int pitch) {
+  if (sc.cap != 0.f) cap_products<NT>(s, sc);
+  const F2 scale = pair(sc.scale, sc.scale);
   if (sc.bias) {
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      int bk[4];
-      buckets_of(bk, index + t * 8, pitch);
-#pragma unroll
-      for (int h = 0; h < HP; ++h) {
-        float b[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) b[e] = bias_at(bias + h * step, bk[e]);
-        score_of<false>(sc, s[h][t], b, none);
+      if (ROWS) {
+        buckets_of(bk[t], index + t * 8, pitch);
+      } else {
+        const uint16_t* at = index + (t * 8 + (threadIdx.x & 3) * 2) * pitch + ((threadIdx.x & 31) >> 2);
+        bk[t][0] = at[0] & kBucketMask; bk[t][1] = at[pitch] & kBucketMask; bk[t][2] = at[8] & kBucketMask; bk[t][3] = at[pitch + 8] & kBucketMask;
       }
     }
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; e += 2) put(s[t], e, fma2(two(s[t], e), scale, pair(bias_at(bias, bk[t][e]), bias_at(bias, bk[t][e + 1]))));
   } else {
-    const float b[4] = {};
 #pragma unroll
-    for (int h = 0; h < HP; ++h)
+    for (int t = 0; t < NT; ++t)
 #pragma unroll
-      for (int t = 0; t < NT; ++t) score_of<false>(sc, s[h][t], b, none);
+      for (int e = 0; e < 4; e += 2) put(s[t], e, mul(two(s[t], e), scale));
   }
-#pragma unroll
-  for (int h = 0; h < HP; ++h) set_columns<NT>(s[h], real, -INFINITY);
+}
+// Scores of queries (rows) and keys (columns); -inf where a column holds no key.
+template <int NT>
+__device__ __forceinline__ void transform(float (&s)[NT][4], const Scoring& sc, const float* bias, const uint16_t* index, int pitch, uint64_t real) {
+  int bk[NT][4];
+  score_tiles<NT, true>(s, bk, sc, bias, index, pitch);
+  set_columns<NT>(s, real, -INFINITY);
 }
 
 __device__ __forceinline__ float quad_max(float v) {

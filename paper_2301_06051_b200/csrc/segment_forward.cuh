@@ -43,8 +43,8 @@ static ShortLayout short_layout(const SegArgs& a, int heads, int limit, int arra
   return l;
 }
 
-// Rows of a range: an equal share for every block that can be resident, within bounds: few enough that ranges of more and fewer short
-// segments even out, enough that a block's tables and searches are spread.
+// Rows of a range: an equal share for every block that can be resident, at most `most`, where ranges of more and fewer short segments
+// have to even out.  (Sets of 32,000 pillars, backward: ranges of 128 rows 117 us, an equal share 97.)
 static void set_ranges(ShortLayout& l, int n, int resident, int most) {
   int per = (n + resident - 1) / resident;
   per = per < 16 ? 16 : per > most ? most : per;
@@ -52,18 +52,15 @@ static void set_ranges(ShortLayout& l, int n, int resident, int most) {
   l.ranges = (n + per - 1) / per;
 }
 
-// HP heads' tiles of 16 queries against their segment's keys, NT tiles of them at a time: all of them where ONLY.  `step`: bytes between heads.
-template <typename T, int DT, int NT, bool ONLY, int HP>
-__device__ __forceinline__ void attend_tile(Flow<DT> (&f)[HP], uint32_t q, uint32_t k, uint32_t v, uint32_t step, uint32_t pitch, int dim, const Scoring& sc, const float* bias,
-                                            int buckets, const uint16_t* index, int pitch_idx, uint64_t keys) {
-  float s[HP][NT][4];
-#pragma unroll
-  for (int h = 0; h < HP; ++h) scores<T, DT, NT>(s[h], q + h * step, k + h * step, pitch, dim);
-  transform<HP, NT>(s, sc, bias, buckets, index, pitch_idx, keys);
-#pragma unroll
-  for (int h = 0; h < HP; ++h) soften<ONLY>(f[h], s[h]);
-#pragma unroll
-  for (int h = 0; h < HP; ++h) weigh<T, DT, NT, false>(f[h].acc, s[h], v + h * step, pitch, dim);
+// A tile of 16 queries against its segment's keys, NT tiles of them at a time: all of them where ONLY.
+template <typename T, int DT, int NT, bool ONLY>
+__device__ __forceinline__ void attend_tile(Flow<DT>& f, uint32_t q, uint32_t k, uint32_t v, uint32_t pitch, int dim, const Scoring& sc, const float* bias,
+                                            const uint16_t* index, int pitch_idx, uint64_t keys) {
+  float s[NT][4];
+  scores<T, DT, NT>(s, q, k, pitch, dim);
+  transform<NT>(s, sc, bias, index, pitch_idx, keys);
+  soften<ONLY>(f, s);
+  weigh<T, DT, NT, false>(f.acc, s, v, pitch, dim);
 }
 
 template <typename T, int DT>
@@ -86,7 +83,6 @@ __global__ void __launch_bounds__(kShortThreads, DT <= 24 && sizeof(T) == 2 ? 3 
   const Rows<3> src = {{first_head<T>(a.q, col), first_head<T>(a.k, col), first_head<T>(a.v, col)},
                        {a.ld_q * (int64_t)sizeof(T), a.ld_k * (int64_t)sizeof(T), a.ld_v * (int64_t)sizeof(T)}};
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  constexpr int HP = 1;
   bool staged = false;
   while (next_batch<kShortThreads>(a, plan, range, L.limit, L.batch)) {
   if (a.bias) {
@@ -106,22 +102,21 @@ __global__ void __launch_bounds__(kShortThreads, DT <= 24 && sizeof(T) == 2 ? 3 
   }
   cp_wait<0>();
   __syncthreads();
-  for (int unit = warp; unit < plan.items * (HG / HP); unit += kShortThreads / 32) {
-    const int h = unit % (HG / HP) * HP;
-    if (h >= heads) continue;
-    const Item item = plan.item[unit / (HG / HP)];
-    const uint32_t at_head = h * dim * sizeof(T), step = dim * sizeof(T);
+  const int h = warp % HG;
+  for (int it = warp / HG; it < plan.items; it += kShortThreads / 32 / HG) {
+    if (h >= heads) break;
+    const Item item = plan.item[it];
+    const uint32_t at_head = h * dim * sizeof(T);
     const float* mine = bias + h * a.buckets;
     const int row = item.at + 16 * item.tile;
     const uint32_t q = q0 + row * pitch + at_head, k = k0 + item.at * pitch + at_head, v = v0 + item.at * pitch + at_head;
     const uint16_t* at = index + row * L.pitch_idx;
-    Flow<DT> f[HP];
-#pragma unroll
-    for (int i = 0; i < HP; ++i) f[i].start();
-#define DSVT_ATTEND(NT) attend_tile<T, DT, NT, true, HP>(f, q, k, v, step, pitch, dim, sc, mine, a.buckets, at, L.pitch_idx, real_rows(plan, item.at, item.len))
-#define DSVT_ATTEND_PART(NT)                                                                                                 \
-  attend_tile<T, DT, NT, false, HP>(f, q, k + j * pitch, v + j * pitch, step, pitch, dim, sc, mine, a.buckets, at + j, L.pitch_idx, \
-                                    real_rows(plan, item.at + j, min(8 * NT, item.len - j)))
+    Flow<DT> f;
+    f.start();
+#define DSVT_ATTEND(NT) attend_tile<T, DT, NT, true>(f, q, k, v, pitch, dim, sc, mine, at, L.pitch_idx, real_rows(plan, item.at, item.len))
+#define DSVT_ATTEND_PART(NT)                                                                               \
+  attend_tile<T, DT, NT, false>(f, q, k + j * pitch, v + j * pitch, pitch, dim, sc, mine, at + j, L.pitch_idx, \
+                                real_rows(plan, item.at + j, min(8 * NT, item.len - j)))
     const int tiles = (item.len + 7) >> 3;
     switch (tiles) {
       case 1: DSVT_ATTEND(1); break;
@@ -143,19 +138,16 @@ __global__ void __launch_bounds__(kShortThreads, DT <= 24 && sizeof(T) == 2 ? 3 
     }
 #undef DSVT_ATTEND
 #undef DSVT_ATTEND_PART
-    // the result takes the place of the queries (this warp's alone: its heads' channels of a tile's rows)
+    // the result takes the place of the queries (this warp's alone: its head's channels of a tile's rows)
     const int r0 = 16 * item.tile + (lane >> 2);
+    const float i0 = inverse(quad_sum(f.l[0])), i1 = inverse(quad_sum(f.l[1]));
+    T* to = reinterpret_cast<T*>(smem + L.rows + (item.at + r0) * pitch + at_head) + (lane & 3) * 2;
     __syncwarp();
 #pragma unroll
-    for (int i = 0; i < HP; ++i) {
-      const float i0 = inverse(quad_sum(f[i].l[0])), i1 = inverse(quad_sum(f[i].l[1]));
-      T* to = reinterpret_cast<T*>(smem + L.rows + (item.at + r0) * pitch + at_head + i * step) + (lane & 3) * 2;
-#pragma unroll
-      for (int n = 0; n < DT / 8; ++n) {
-        if (!kExact<DT> && n * 8 >= dim) break;
-        if (r0 < item.len) store2<T>(to + n * 8, f[i].acc[n][0] * i0, f[i].acc[n][1] * i0);
-        if (r0 + 8 < item.len) store2<T>(reinterpret_cast<T*>(reinterpret_cast<char*>(to) + 8 * pitch) + n * 8, f[i].acc[n][2] * i1, f[i].acc[n][3] * i1);
-      }
+    for (int n = 0; n < DT / 8; ++n) {
+      if (!kExact<DT> && n * 8 >= dim) break;
+      if (r0 < item.len) store2<T>(to + n * 8, f.acc[n][0] * i0, f.acc[n][1] * i0);
+      if (r0 + 8 < item.len) store2<T>(reinterpret_cast<T*>(reinterpret_cast<char*>(to) + 8 * pitch) + n * 8, f.acc[n][2] * i1, f.acc[n][3] * i1);
     }
   }
   __syncthreads();
@@ -230,7 +222,7 @@ struct Passing {
 };
 
 template <typename T, int DT>
-__global__ void __launch_bounds__(kThreads, LongShape<T, DT>::three ? 3 : 1) long_forward_kernel(const __grid_constant__ SegArgs a, const LongLayout L, const Scoring sc, int above) {
+__global__ void __launch_bounds__(kThreads, LongShape<T, DT>::three ? 3 : DT <= 32 ? 2 : 1) long_forward_kernel(const __grid_constant__ SegArgs a, const LongLayout L, const Scoring sc, int above) {
   extern __shared__ __align__(16) unsigned char smem[];
   using S = LongShape<T, DT>;
   __shared__ Tile tiles[kMaxTiles];
@@ -280,9 +272,9 @@ __global__ void __launch_bounds__(kThreads, LongShape<T, DT>::three ? 3 : 1) lon
     __syncthreads();
     load_rows<T, kThreads, 1>(q0, 0, pitch, own, ids, S::rows, chunks, real);
     load(0);
-    Flow<DT> f[S::HPW][1];
+    Flow<DT> f[S::HPW];
 #pragma unroll
-    for (int i = 0; i < S::HPW; ++i) f[i][0].start();
+    for (int i = 0; i < S::HPW; ++i) f[i].start();
     const int parts = (tile.hi - tile.lo + S::chunk - 1) / S::chunk;
     for (int c = 0; c < parts; ++c) {
       if (c + 1 < parts) publish(c + 1);
@@ -311,8 +303,8 @@ __global__ void __launch_bounds__(kThreads, LongShape<T, DT>::three ? 3 : 1) lon
         const int h = (warp % S::WH) * S::HPW + i;
         if (h < heads && row < rows) {
           const uint32_t at_head = h * dim * sizeof(T);
-          attend_tile<T, DT, S::NT, false, 1>(f[i], q0 + row * pitch + at_head, pass.array(c, 0, 2) + at_head, pass.array(c, 1, 2) + at_head, 0, pitch, dim, sc,
-                                              bias + h * a.buckets, 0, index + row * L.pitch_idx, L.pitch_idx, keys);
+          attend_tile<T, DT, S::NT, false>(f[i], q0 + row * pitch + at_head, pass.array(c, 0, 2) + at_head, pass.array(c, 1, 2) + at_head, pitch, dim, sc,
+                                           bias + h * a.buckets, index + row * L.pitch_idx, L.pitch_idx, keys);
         }
       }
     }
@@ -320,14 +312,14 @@ __global__ void __launch_bounds__(kThreads, LongShape<T, DT>::three ? 3 : 1) lon
     for (int i = 0; i < S::HPW; ++i) {
       const int h = (warp % S::WH) * S::HPW + i;
       if (h >= heads || row >= rows) continue;
-      const float i0 = inverse(quad_sum(f[i][0].l[0])), i1 = inverse(quad_sum(f[i][0].l[1]));
+      const float i0 = inverse(quad_sum(f[i].l[0])), i1 = inverse(quad_sum(f[i].l[1]));
       const int r0 = row + (lane >> 2), id0 = ids[r0], id1 = ids[r0 + 8];
       T* to = (T*)a.out + col + h * dim + (lane & 3) * 2;
 #pragma unroll
       for (int n = 0; n < DT / 8; ++n) {
         if (!kExact<DT> && n * 8 >= dim) break;
-        if (id0 >= 0) store2<T>(to + id0 * a.ld_out + n * 8, f[i][0].acc[n][0] * i0, f[i][0].acc[n][1] * i0);
-        if (id1 >= 0) store2<T>(to + id1 * a.ld_out + n * 8, f[i][0].acc[n][2] * i1, f[i][0].acc[n][3] * i1);
+        if (id0 >= 0) store2<T>(to + id0 * a.ld_out + n * 8, f[i].acc[n][0] * i0, f[i].acc[n][1] * i0);
+        if (id1 >= 0) store2<T>(to + id1 * a.ld_out + n * 8, f[i].acc[n][2] * i1, f[i].acc[n][3] * i1);
       }
     }
   }
@@ -335,6 +327,7 @@ __global__ void __launch_bounds__(kThreads, LongShape<T, DT>::three ? 3 : 1) lon
 
 // Up to kShort rows a segment is held whole where that leaves room for two blocks on an SM, or at least for one; in calls with longer
 // ones up to 64 rows, and the longer ones go through in tiles.
+constexpr uint32_t kSmemHalf = 112 * 1024;  // two blocks
 constexpr uint32_t kSmemMost = 226 * 1024;  // (of 227 KB; the rest for what kernels declare themselves)
 
 // (once per kernel and device: the call costs more than a launch's share of it)
@@ -355,7 +348,7 @@ int forward_of(dsvt_ctx* ctx, const SegArgs& a) {
   if (l.bytes > kSmemMost) l = short_layout<T>(a, kHeads<T, DT>, limit = 64, 3, kBatch);
   const Scoring sc = scoring_of(a);
   const int groups = (int)dsvt_ceil_div(a.heads, kHeads<T, DT>);
-  set_ranges(l, a.n, (int)dsvt_ceil_div((DT <= 24 && sizeof(T) == 2 ? 3 : 2) * ctx->sm_count, groups), 128);
+  set_ranges(l, a.n, (int)dsvt_ceil_div((DT <= 24 && sizeof(T) == 2 ? 3 : 2) * ctx->sm_count, groups), limit < a.max_len ? 128 : 1 << 20);
   constexpr auto kernel = short_forward_kernel<T, DT>;
   int rc = allow_smem<kernel>(ctx);
   if (rc != DSVT_OK) return rc;

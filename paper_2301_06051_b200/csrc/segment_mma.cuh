@@ -301,15 +301,18 @@ __device__ __forceinline__ void put(float (&z)[4], int e, F2 v) {
   z[e + 1] = f.y;
 }
 
-// The scores' transformation: products -> scale, cap, bias, in units of log 2.
+// From products to scores in units of log 2: capped first, where there is a cap, then fma(x, scale, bias).  (The cap is a pass of its
+// own, and where its derivative is needed the products are formed again: what has no cap is straight-line code.)
 struct Scoring {
-  float scale;   // of the product, to tanh's argument with a cap, else to units of log 2
+  float scale;   // of a product to units of log 2; 1 behind a cap
+  float inner;   // with a cap: of a product to tanh's argument
   float cap;     // in units of log 2, or 0
   bool bias;
 };
 static inline Scoring scoring_of(const SegArgs& a) {
   Scoring s;
-  s.scale = a.cap > 0.f ? a.scale / a.cap : a.scale * kLog2e;
+  s.scale = a.cap > 0.f ? 1.f : a.scale * kLog2e;
+  s.inner = a.cap > 0.f ? a.scale / a.cap : 0.f;
   s.cap = a.cap * kLog2e;
   s.bias = a.bias != nullptr;
   return s;
@@ -329,24 +332,23 @@ __device__ __forceinline__ float tanh_of(float x) {
 // A bias entry in units of log 2.  (Clamped: the lowest float stays the lowest, whatever is added, and differences of two are zero.)
 __device__ __forceinline__ float bias_log2(float b) { return b == -INFINITY ? b : fmaxf(b * kLog2e, -3.402823466e38f); }
 
-// A tile's four scores; with `slope`, the derivative of the cap too.
-template <bool SLOPE>
-__device__ __forceinline__ void score_of(const Scoring& s, float (&z)[4], const float (&bias)[4], float (&slope)[4]) {
-  if (s.cap == 0.f) {
-    const F2 scale = pair(s.scale, s.scale);
+template <int NT>
+__device__ __forceinline__ void cap_products(float (&s)[NT][4], const Scoring& sc) {
 #pragma unroll
-    for (int e = 0; e < 4; e += 2) {
-      put(z, e, fma2(pair(z[e], z[e + 1]), scale, pair(bias[e], bias[e + 1])));
-      if (SLOPE) slope[e] = slope[e + 1] = 1.f;
-    }
-  } else {
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s[t][e] = sc.cap * tanh_of(s[t][e] * sc.inner);
+}
+// x *= the cap's derivative at the products z.
+template <int NT>
+__device__ __forceinline__ void cap_slope(float (&x)[NT][4], const float (&z)[NT][4], const Scoring& sc) {
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const float t = tanh_of(z[e] * s.scale);
-      if (SLOPE) slope[e] = fmaf(-t, t, 1.f);
-      z[e] = fmaf(t, s.cap, bias[e]);
+      const float u = tanh_of(z[t][e] * sc.inner);
+      x[t][e] *= fmaf(-u, u, 1.f);
     }
-  }
 }
 
 // ---- loading -------------------------------------------------------------------------------------------------------
