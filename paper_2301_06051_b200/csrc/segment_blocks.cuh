@@ -17,12 +17,13 @@ struct Item { uint8_t at, len, tile, pad; };
 // A batch of segments in shared memory.  A segment's place is a multiple of 8 rows, so that tiles of 8 rows are its own; the places
 // behind its end are zeros.
 struct Plan {
-  int rows, items, pairs;              // (pairs: of queries and keys)
+  int rows, items, pairs, longest;     // (pairs: of queries and keys; longest: segment's length)
   int cursor;                          // the first segment that has not been looked at
   int lo[kShort / 8];                  // by segment: first row, length, place
   uint8_t len[kShort / 8], place[kShort / 8];
   uint8_t owner[kShort / 8];           // by 8 places: the segment
   uint32_t real[kShort / 32 + 3];      // bit i: place i holds a voxel
+  uint16_t span[kShort];               // by place: its segment's place, and length << 8; 0 where there is no voxel
   int32_t ids[kShort];
   Item item[kShort / 8];
 };
@@ -81,7 +82,7 @@ template <int N>
 __device__ __forceinline__ bool next_batch(const SegArgs& a, Plan& p, const Range& range, int limit, int most) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   if (warp == 0) {
-    int at = 0, segments = 0, items = 0, pairs = 0, cursor = p.cursor;
+    int at = 0, segments = 0, items = 0, pairs = 0, longest = 0, cursor = p.cursor;
     bool open = true;
     while (open && cursor < range.end) {  // 32 segments at a time
       const int s = cursor + lane;
@@ -108,6 +109,7 @@ __device__ __forceinline__ bool next_batch(const SegArgs& a, Plan& p, const Rang
         for (int t = 0; t < tiles; ++t) p.item[items + upto - tiles + t] = Item{(uint8_t)place, (uint8_t)len, (uint8_t)t, 0};
         for (int t = 0; t < size; t += 8) p.owner[(place + t) >> 3] = (uint8_t)slot;
         pairs += len * len;
+        longest = max(longest, len);
       }
       if (taken) {
         const int last = 31 - __clz(taken);
@@ -124,8 +126,10 @@ __device__ __forceinline__ bool next_batch(const SegArgs& a, Plan& p, const Rang
         open = at + 8 <= most;
       }
     }
-    for (int m = 16; m > 0; m >>= 1) pairs += __shfl_xor_sync(kAll, pairs, m);
+    pairs = __reduce_add_sync(kAll, pairs);
+    longest = __reduce_max_sync(kAll, longest);
     if (lane == 0) {
+      p.longest = longest;
       p.rows = at;
       p.items = items;
       p.pairs = pairs;
@@ -136,14 +140,16 @@ __device__ __forceinline__ bool next_batch(const SegArgs& a, Plan& p, const Rang
   if (p.items == 0) return false;
   if (tid < 3) p.real[kShort / 32 + tid] = 0;
   for (int i = tid; i < kShort; i += N) {
-    int id = -1;
+    int id = -1, span = 0;
     if (i < p.rows) {
-      const int own = p.owner[i >> 3], r = i - p.place[own];
-      if (r < p.len[own]) id = voxel_at(a, p.lo[own] + r);
+      const int own = p.owner[i >> 3], at = p.place[own], len = p.len[own];
+      if (i - at < len) id = voxel_at(a, p.lo[own] + i - at);
+      span = at | len << 8;
     }
     const uint32_t real = __ballot_sync(kAll, id >= 0);
     if (lane == 0) p.real[i >> 5] = real;
     p.ids[i] = id;
+    p.span[i] = (uint16_t)(id >= 0 ? span : 0);
   }
   __syncthreads();
   return true;
@@ -162,16 +168,29 @@ __device__ __forceinline__ uint64_t real_rows(const Plan& p, int at, int count) 
 // rows of a score tile's fragment lie in different banks.
 __host__ __device__ constexpr int index_pitch(int cols) { return 8 * (((cols + 7) / 8) | 1); }
 
-// The buckets (times 4) of all pairs of the batch: index[i][j - first of i's segment].  The rest of the tile is never written.
+// The buckets (times 4) of all pairs of the batch: index[i][j - first of i's segment].  The rest of the tile is never written.  Four rows
+// at a time, so that their look-ups overlap.
 template <int N>
 __device__ __forceinline__ void fill_index(const SegArgs& a, const Plan& p, const int4* cells, const uint16_t* maps, uint16_t* index, int pitch) {
-  const int part = threadIdx.x & 15;
-  for (int i = threadIdx.x >> 4; i < p.rows; i += N / 16) {
-    if (p.ids[i] < 0) continue;
-    const int own = p.owner[i >> 3], at = p.place[own], len = p.len[own];
-    const int4 mine = cells[i];
-#pragma unroll 3
-    for (int j = part; j < len; j += 16) index[i * pitch + j] = (uint16_t)bucket_at(a.maps, maps, mine, cells[at + j]);
+  const int part = threadIdx.x & 15, rows = p.rows, longest = p.longest;
+  constexpr int step = N / 16;
+  for (int i = threadIdx.x >> 4; i < rows; i += 4 * step) {
+    int at[4], len[4];
+    int4 mine[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int r = min(i + u * step, rows - 1), span = i + u * step < rows ? p.span[r] : 0;
+      at[u] = span & 255;
+      len[u] = span >> 8;
+      mine[u] = cells[r];
+    }
+    for (int j = part; j < longest; j += 16) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int b = bucket_at(a.maps, maps, mine[u], cells[at[u] + min(j, max(len[u] - 1, 0))]);
+        if (j < len[u]) index[(i + u * step) * pitch + j] = (uint16_t)b;
+      }
+    }
   }
 }
 
