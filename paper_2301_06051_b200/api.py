@@ -135,15 +135,15 @@ def _type(t: torch.Tensor) -> int:
     return TYPES[t.dtype]
 
 
-def _rows(t: torch.Tensor, like: torch.Tensor):
+def _rows(t: torch.Tensor, shape, dtype):
     """Pointer and row stride of rows [n, heads, head_dim] whose heads lie one after the other."""
-    n, heads, dim = t.shape
-    if t.shape != like.shape or t.dtype != like.dtype or not t.is_cuda:
+    if t.shape != shape or t.dtype is not dtype or not t.is_cuda:
         raise ValueError("rows of one shape and type, on the device")
-    s = t.stride()
-    if (dim > 1 and s[2] != 1) or (heads > 1 and s[1] != dim):
+    row, head, one = t.stride()
+    n, heads, dim = shape
+    if (one != 1 and dim > 1) or (head != dim and heads > 1):
         raise ValueError("the heads of a row lie one after the other")
-    return t.data_ptr(), s[0] if n > 1 else heads * dim
+    return t.data_ptr(), row if n > 1 else heads * dim
 
 
 def _int32(t: Optional[torch.Tensor], shape=None):
@@ -488,22 +488,20 @@ class Context:
 
     # ---- dsvt_segment_attention ----
     def _segment_params(self, q, k, v, seg, bias, scale, cap):
-        n, heads, dim = q.shape
-        p = SegmentAttentionParams()
-        p.n, p.heads, p.head_dim, p.type = n, heads, dim, _type(q)
-        p.q, p.ld_q = _rows(q, q)
-        p.k, p.ld_k = _rows(k, q)
-        p.v, p.ld_v = _rows(v, q)
-        p.order, p.seg_start, p.num_segments = _int32(seg.order, (n,)), _int32(seg.start), _int32(seg.num)
-        p.cap_segments, p.max_len = seg.start.numel() - 1, seg.max_len
-        p.scale, p.cap = dim ** -0.5 if scale is None else scale, cap
+        shape, dtype = q.shape, q.dtype
+        n, heads, dim = shape
+        kind = _type(q)
+        (qp, ld_q), (kp, ld_k), (vp, ld_v) = _rows(q, shape, dtype), _rows(k, shape, dtype), _rows(v, shape, dtype)
+        p = SegmentAttentionParams(n, heads, dim, kind, qp, kp, vp, ld_q, ld_k, ld_v, _int32(seg.order, (n,)), _int32(seg.start),
+                                   _int32(seg.num), seg.start.numel() - 1, seg.max_len, dim ** -0.5 if scale is None else scale, cap)
         if bias is not None:
-            if bias.table.shape[0] != heads:
-                raise ValueError("a bias for %d heads, and %d heads" % (bias.table.shape[0], heads))
+            table = bias.table
+            if table.shape[0] != heads:
+                raise ValueError("a bias for %d heads, and %d heads" % (table.shape[0], heads))
             if seg.coords is None:
                 raise ValueError("a relative position bias needs the segments' coords")
-            p.bias, p.buckets = _ptr(bias.table), bias.table.shape[1]
-            p.coords, p.bucket_of, p.extent = _int32(seg.coords, (n, 4)), bias._index_at, bias._extent
+            p.bias, p.buckets, p.coords, p.bucket_of, p.extent = (_ptr(table), table.shape[1], _int32(seg.coords, (n, 4)),
+                                                                  bias._index_at, bias._extent)
         return p
 
     def segment_attention(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, seg: Segments,
@@ -514,7 +512,7 @@ class Context:
         p = self._segment_params(q, k, v, seg, bias, scale, cap)
         if out is None:
             out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        rc = self.lib.dsvt_segment_attention(self._h, C.byref(p), *_rows(out, q))
+        rc = self.lib.dsvt_segment_attention(self._h, C.byref(p), *_rows(out, q.shape, q.dtype))
         self._check(rc, "dsvt_segment_attention")
         return out
 
@@ -531,8 +529,9 @@ class Context:
             dbias = torch.empty_like(bias.table)
         if dbias is not None and (bias is None or dbias.shape != bias.table.shape or dbias.dtype != torch.float32):
             raise ValueError("dbias is a float32 tensor of the bias table's shape")
-        rc = self.lib.dsvt_segment_attention_backward(self._h, C.byref(p), *_rows(d_out, q), *_rows(dq, q), *_rows(dk, q),
-                                                      *_rows(dv, q), _ptr(dbias))
+        shape, dtype = q.shape, q.dtype
+        rc = self.lib.dsvt_segment_attention_backward(self._h, C.byref(p), *_rows(d_out, shape, dtype), *_rows(dq, shape, dtype),
+                                                      *_rows(dk, shape, dtype), *_rows(dv, shape, dtype), _ptr(dbias))
         self._check(rc, "dsvt_segment_attention_backward")
         return dq, dk, dv, dbias
 
