@@ -447,6 +447,8 @@ int dsvt_segment_attention(dsvt_ctx* ctx, const dsvt_segment_attention_params* p
  * are left as they were; dbias is written in full (a value that is not finite makes its entry NaN).  The same inputs give the same bits.
  *
  * dbias adds up dS = P (dP - D), D = sum P dP, in whole multiples of at most 2^-33 times the call's largest max_j |P dP| + |D| max_j P.
+ * The call works in the context's workspace, as partitions and layers do: calls of one context, captured ones among them, must not
+ * overlap on the GPU.
  *
  * Needs heads * buckets <= 2^18 with dbias (else DSVT_ERR_UNSUPPORTED), and n <= 1,700,000 where max_len is above 24 (else
  * DSVT_ERR_CAPACITY).
@@ -471,7 +473,8 @@ int dsvt_layer_norm(dsvt_ctx* ctx, int type, const void* x, const void* residual
 /*
  * The gradients of dsvt_layer_norm from that of its output, dy: dx ([n][C] of `type`; the residual's is the same; may be x, residual
  * or dy), dg and db (float [C], written in full; each may be NULL).  Statistics are taken from x and residual again; the forward
- * pass saves nothing.  The same inputs give the same bits.
+ * pass saves nothing.  The same inputs give the same bits.  The call works in the context's workspace (see
+ * dsvt_segment_attention_backward).
  */
 int dsvt_layer_norm_backward(dsvt_ctx* ctx, int type, const void* x, const void* residual, const void* dy, int32_t n,
                              int32_t C, const float* g, float eps, void* dx, float* dg, float* db);

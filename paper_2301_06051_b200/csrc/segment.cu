@@ -1,5 +1,5 @@
 // dsvt_segment_attention and its backward pass: the calls' checks.
-#include <string.h>
+#include <math.h>
 
 #include "segment.cuh"
 
@@ -12,8 +12,8 @@ bool bad_rows(const void* p, int64_t ld, int64_t width, int size) {
 
 int check(const dsvt_ctx* ctx, const dsvt_segment_attention_params* p, SegArgs* a) {
   if (!ctx || !p || p->n < 0 || p->heads < 1 || p->head_dim < 1 || !type_known(p->type)) return DSVT_ERR_INVALID_ARG;
-  if (p->cap_segments < 0 || p->max_len < 1 || !(p->cap >= 0.f)) return DSVT_ERR_INVALID_ARG;
-  if (p->head_dim % 8 != 0 || p->head_dim > kMaxDim || p->heads > 65535) return DSVT_ERR_UNSUPPORTED;
+  if (p->cap_segments < 0 || p->max_len < 1 || !(p->cap >= 0.f) || isinf(p->cap)) return DSVT_ERR_INVALID_ARG;
+  if (p->head_dim % 8 != 0 || p->head_dim > kMaxDim || p->heads > kMaxHeads) return DSVT_ERR_UNSUPPORTED;
   if (p->n > ctx->max_voxels) return DSVT_ERR_CAPACITY;
   const int64_t width = (int64_t)p->heads * p->head_dim;
   const int size = type_size(p->type);

@@ -6,7 +6,7 @@
 
 namespace dsvt_train {
 
-constexpr int kMaxExtent = 128, kMaxBuckets = 1024, kMaxDim = 128;
+constexpr int kMaxExtent = 128, kMaxBuckets = 1024, kMaxDim = 128, kMaxHeads = 65535;
 constexpr int64_t kMaxBiasTable = 1 << 18;  // entries of a bias whose gradient is asked for: what the workspace has room for
 
 // The additive bucket indexes of the displacements along x, y and z: at [0, 2L-1), [at_y, at_y + 2W-1), [at_z, ...).

@@ -29,9 +29,10 @@ struct BackWork {
   float* partial;               // [blocks][table]: the short ones' sums
   unsigned long long* total;    // [2][table]: the long ones', hi and lo
   uint32_t* spoilt;             // [table / 32] bits: a value that was not finite
-  uint32_t* bound;              // the long ones' largest |ds| may be, as a float's bits
+  uint32_t* bounds;             // [launches]: what the long ones' |ds| is at most, as a float's bits
   float* stats;                 // [heads of a launch][n][3]
-  int32_t table, blocks, head0, head_end, n;  // (heads of a launch of the long ones)
+  int32_t table, blocks, n;
+  int32_t head0, head_end, at_once, launches;  // heads of a launch of the long ones, how many to a launch, and how many launches
 };
 
 // A value that need not be within the limit (the two passes' roundings of large scores may leave one beyond it), nor finite.
@@ -386,7 +387,7 @@ __global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) short_backward_ker
     const int first = (blockIdx.y * gridDim.x + blockIdx.x) * kThreads + threadIdx.x, step = gridDim.x * gridDim.y * kThreads;
     for (int i = first; i < 2 * work.table; i += step) work.total[i] = 0;
     for (int i = first; i < (work.table + 31) / 32; i += step) work.spoilt[i] = 0;
-    if (first == 0) *work.bound = 0;
+    for (int i = first; i < work.launches; i += step) work.bounds[i] = 0;
   }
   bool emptied = false;
   int pending = 0;
@@ -609,7 +610,7 @@ __global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) long_backward_kern
   tally.copy = S::HG * 2 * a.buckets;
   tally.on = BY_KEYS && a.dbias != nullptr;
   if (tally.on) {
-    tally.bound(__uint_as_float(*work.bound));
+    tally.bound(__uint_as_float(work.bounds[work.head0 / work.at_once]));
     tally.clear_all<kThreads>(S::HG);
   }
   auto empty = [&]() {  // all threads; a barrier before and after
@@ -779,12 +780,12 @@ __global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) long_backward_kern
   }
   if (!BY_KEYS && a.dbias) {
     for (int m = 16; m > 0; m >>= 1) most = fmaxf(most, __shfl_xor_sync(kAll, most, m));
-    if (lane == 0 && most > 0.f) atomicMax(work.bound, __float_as_uint(most));
+    if (lane == 0 && most > 0.f) atomicMax(work.bounds + work.head0 / work.at_once, __float_as_uint(most));
   }
 }
 
 // dbias: the blocks' partial sums in a fixed order, and the long segments' integers.  32 entries to a block, a warp a share of the blocks.
-static __global__ void __launch_bounds__(kThreads) bias_grad_kernel(const BackWork work, bool longer, float* dbias) {
+static __global__ void __launch_bounds__(kThreads) bias_grad_kernel(const BackWork work, int buckets, bool longer, float* dbias) {
   __shared__ float part[kWarps][32];
   pdl_enter();
   const int at = blockIdx.x * 32 + (threadIdx.x & 31), warp = threadIdx.x >> 5;
@@ -798,7 +799,7 @@ static __global__ void __launch_bounds__(kThreads) bias_grad_kernel(const BackWo
   for (int i = 1; i < kWarps; ++i) s += part[i][threadIdx.x];
   if (longer) {
     Tally t;
-    t.bound(__uint_as_float(*work.bound));
+    t.bound(__uint_as_float(work.bounds[at / buckets / work.at_once]));
     s += tally_value((long long)work.total[at], (long long)work.total[at + work.table], t.limit);
     if (work.spoilt[at >> 5] >> (at & 31) & 1) s = NAN;
   }
@@ -820,8 +821,8 @@ int backward_of(dsvt_ctx* ctx, const SegArgs& a) {
   w.partial = reinterpret_cast<float*>(base);
   w.total = reinterpret_cast<unsigned long long*>(base + kPartialWords);
   w.spoilt = base + kPartialWords + kTotalWords;
-  w.bound = w.spoilt + kMaxBiasTable / 32;
-  w.stats = reinterpret_cast<float*>(w.bound + 64);
+  w.bounds = w.spoilt + kMaxBiasTable / 32;
+  w.stats = reinterpret_cast<float*>(w.bounds + kMaxHeads);
   const int64_t stat_words = (int64_t)(4 * ctx->bm_words) - (w.stats - reinterpret_cast<float*>(base));
   w.table = a.dbias ? a.heads * a.buckets : 0;
   w.n = a.n;
@@ -832,25 +833,27 @@ int backward_of(dsvt_ctx* ctx, const SegArgs& a) {
   set_ranges(l.s, a.n, (int)stay, limit < a.max_len ? 128 : 1 << 20);
   if (stay > l.s.ranges) stay = l.s.ranges;
   w.blocks = (int)stay;
+  // as many heads to a launch of the long ones as the workspace has room for the statistics of, whole blocks' if it can be
+  const bool longer = limit < a.max_len;
+  using S = BackShape<T, DT>;
+  int64_t at_once = stat_words / ((int64_t)3 * a.n);
+  if (longer && at_once < 1) return DSVT_ERR_CAPACITY;
+  if (at_once > S::HG) at_once = at_once / S::HG * S::HG;
+  w.at_once = (int)(at_once < 1 ? 1 : at_once < a.heads ? at_once : a.heads);
+  w.launches = (int)dsvt_ceil_div(a.heads, w.at_once);
   constexpr auto kernel = short_backward_kernel<T, DT>;
   int rc = allow_smem<kernel>(ctx);
   if (rc != DSVT_OK) return rc;
   launch_pdl(kernel, dim3((unsigned)stay, groups), dim3(kThreads), l.bytes, ctx->stream, a, l, sc, w);
   DSVT_LAUNCHED(ctx);
-  const bool longer = limit < a.max_len;
   if (longer) {
-    using S = BackShape<T, DT>;
     const BackLongLayout lq = back_long_layout<T, DT>(a, false), lk = back_long_layout<T, DT>(a, true);
     constexpr auto by_queries = long_backward_kernel<T, DT, false>;
     constexpr auto by_keys = long_backward_kernel<T, DT, true>;
     if ((rc = allow_smem<by_queries>(ctx)) != DSVT_OK || (rc = allow_smem<by_keys>(ctx)) != DSVT_OK) return rc;
-    // as many heads to a launch as the workspace has room for the statistics of, whole blocks' if it can be
-    int64_t at_once = stat_words / ((int64_t)3 * a.n);
-    if (at_once < 1) return DSVT_ERR_CAPACITY;
-    if (at_once > S::HG) at_once = at_once / S::HG * S::HG;
-    for (int h = 0; h < a.heads; h += (int)at_once) {
+    for (int h = 0; h < a.heads; h += w.at_once) {
       w.head0 = h;
-      w.head_end = (int)(h + at_once < a.heads ? h + at_once : a.heads);
+      w.head_end = h + w.at_once < a.heads ? h + w.at_once : a.heads;
       const dim3 grid((unsigned)dsvt_ceil_div(a.n, S::rows), (unsigned)dsvt_ceil_div(w.head_end - h, S::HG));
       launch_pdl(by_queries, grid, dim3(kThreads), lq.bytes, ctx->stream, a, lq, sc, w, limit);
       DSVT_LAUNCHED(ctx);
@@ -859,7 +862,7 @@ int backward_of(dsvt_ctx* ctx, const SegArgs& a) {
     }
   }
   if (a.dbias) {
-    launch_pdl(bias_grad_kernel, dim3((unsigned)dsvt_ceil_div(w.table, 32)), dim3(kThreads), 0, ctx->stream, w, longer, a.dbias);
+    launch_pdl(bias_grad_kernel, dim3((unsigned)dsvt_ceil_div(w.table, 32)), dim3(kThreads), 0, ctx->stream, w, a.buckets, longer, a.dbias);
     DSVT_LAUNCHED(ctx);
   }
   return DSVT_OK;
