@@ -147,6 +147,50 @@ def test_what_is_not_finite_stays_in_its_segment(ctx, typ, lens):
     assert torch.isnan(p.forward(ctx)[torch.from_numpy(p.segments[1]).cuda()]).any()
 
 
+@pytest.mark.parametrize("lens", [[17, 20, 5, 36], [150, 20, 200]])
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_a_gradient_that_is_not_finite_reaches_its_buckets_alone(ctx, lens, bad):
+    p = Problem(lens, 4, 24, torch.bfloat16, seed=6, packed=False)
+    voxel, ids = int(p.segments[0][2]), p.segments[0]
+    p.do[voxel] = bad
+    *_, dbias = p.backward(ctx)
+    hit = np.unique(p.buckets(ids)[2])  # of the pairs of that query
+    rest = np.setdiff1d(np.arange(p.table.shape[1]), hit)
+    assert torch.isnan(dbias[:, hit]).all() and torch.isfinite(dbias[:, rest]).all() and len(rest)
+    p.host[3] = p.host[3].clone()
+    p.host[3][voxel] = 0  # the other rows' sums: that row's are zero then
+    want, _ = p.want(back=True)
+    ref.check(dbias[:, rest], tuple(t[:, rest] for t in want["dbias"]), "dbias")
+    assert ctx.status_sync() == 0
+
+
+@pytest.mark.parametrize("lens", [[30, 36, 3], [200, 70]])
+def test_float16_gradients_beyond_its_range_on_the_way(ctx, lens):
+    """dS of a million, results of thousands."""
+    p = Problem(lens, 4, 24, torch.float16, seed=14, packed=False)
+    for i, factor in enumerate((2.0 ** -10, 2.0 ** -10, 64.0, 2000.0)):
+        p.host[i] = (p.host[i].float() * factor).half()
+    p.q, p.k, p.v, p.do = (t.contiguous().cuda() for t in p.host)
+    grads = p.backward(ctx)
+    want, _ = p.want(back=True)
+    assert float(want["dbias"][0].abs().max()) > 65504
+    for name, got in zip(("dq", "dk", "dv", "dbias"), grads):
+        ref.check(got, want[name], name)
+
+
+@pytest.mark.parametrize("typ", TYPES)
+@pytest.mark.parametrize("lens", [[36, 20, 3, 36], [256, 100]])
+def test_a_bias_for_every_displacement(ctx, typ, lens):
+    """One bucket per displacement: the largest tables."""
+    p = Problem(lens, 8, 16, typ, seed=17, spread=16)
+    p.extent = (16, 16, 1)
+    d = np.arange(31)
+    p.index = np.concatenate([31 * d, d, [0]]).astype(np.int32)
+    p.table = torch.randn((8, 961), generator=torch.Generator().manual_seed(1))
+    p.rel = api.BucketBias(p.table.cuda(), p.extent, p.index)
+    _check_both(ctx, p)
+
+
 def test_the_segments_of_a_partition(ctx):
     """Sets and windows as dsvt_partition_rotated leaves them, counts on the device."""
     g = torch.Generator().manual_seed(9)
@@ -451,6 +495,17 @@ def test_layer_norm_without_weights_in_place_and_with_an_offset(ctx, typ):
         t = dict(x=x.cuda(), r=r.cuda(), dy=dy.cuda())
         for name, got in zip(("dx", "dg", "db"), ctx.layer_norm_backward(t["x"], t["dy"], None, residual=t["r"], out=t[at])):
             ref.check(got, want[name], "%s in %s" % (name, at))
+
+
+def test_layer_norm_on_another_stream_than_the_current_one(ctx):
+    """A context's calls run on its own stream, whatever the current one is; waiting for that stream is enough."""
+    own = api.Context(1000, 1, 256, stream=torch.cuda.Stream())
+    x = torch.randn((1000, 192), device="cuda")
+    torch.cuda.synchronize()
+    y = own.layer_norm(x, None, None)
+    own.stream.synchronize()
+    assert torch.equal(y, ctx.layer_norm(x, None, None))
+    own.close()
 
 
 def test_layer_norm_rows_that_are_not_finite_or_constant(ctx):
