@@ -551,7 +551,7 @@ struct BackLongLayout {
 };
 
 template <typename T, int DT>
-static BackLongLayout back_long_layout(const SegArgs& a, bool by_keys) {
+static BackLongLayout back_long_layout(const SegArgs& a, bool by_keys, int copies = 4) {
   using S = BackShape<T, DT>;
   BackLongLayout l = {};
   l.pitch = (uint32_t)(S::HG * a.dim * sizeof(T) + 16);
@@ -566,12 +566,12 @@ static BackLongLayout back_long_layout(const SegArgs& a, bool by_keys) {
     l.cells = take((size_t)S::rows * 16);
     l.passing_cells = take((size_t)3 * S::chunk * 16);
     l.pitch_idx = S::chunk + 8;
-    l.index = take((size_t)S::rows * l.pitch_idx * 2);
+    l.index = take((size_t)(by_keys ? 1 : 2) * S::rows * l.pitch_idx * 2);
   }
   if (by_keys) {
     l.stats = take((size_t)3 * S::HG * 3 * S::chunk * 4);
     if (a.dbias) {
-      l.copies = tally_copies(S::HG * 2 * a.buckets * 4, 38 * 1024);
+      l.copies = copies;
       l.hist = take((size_t)l.copies * S::HG * 2 * a.buckets * 4);
       l.spoilt = take((size_t)(S::HG * a.buckets + 31) / 32 * 4);
     }
@@ -579,7 +579,8 @@ static BackLongLayout back_long_layout(const SegArgs& a, bool by_keys) {
   l.rows = take((size_t)2 * l.tile + 64);
   l.passing = take((size_t)4 * l.chunk + 64);
   l.bytes = at;
-  return l;
+  // (as many tables of the tally as leave room for two blocks on an SM)
+  return by_keys && a.dbias && copies > 1 && at > kSmemHalf ? back_long_layout<T, DT>(a, by_keys, copies / 2) : l;
 }
 
 // A tile of a long segment's queries (BY_KEYS: keys) against all of the segment's keys (queries).
@@ -687,6 +688,17 @@ __global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) long_backward_kern
       clear<DT>(acc[i]);
       if (BY_KEYS) clear<DT>(dv[i]);
     }
+    // (by queries a chunk's buckets are looked up while the one before is worked on; by keys the tally takes that room)
+    auto index_of = [&](int c) { return BY_KEYS ? index : index + (c & 1) * S::rows * L.pitch_idx; };
+    auto look_up = [&](int c) {
+      if (!a.bias) return;
+      uint16_t* to = index_of(c);
+      const int4* passing_cells = cells_of(c);
+      for (int i = threadIdx.x; i < S::rows * S::chunk; i += kThreads) {
+        const int r = i / S::chunk, j = i % S::chunk;
+        to[r * L.pitch_idx + j] = (uint16_t)(BY_KEYS ? bucket_at(a.maps, maps, passing_cells[j], cells[r]) : bucket_at(a.maps, maps, cells[r], passing_cells[j]));
+      }
+    };
     int pending = 0;
     for (int sweep = BY_KEYS ? 1 : 0; sweep < 2; ++sweep) {
       fetch_id(0);
@@ -698,25 +710,24 @@ __global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) long_backward_kern
         load_rows<T, kThreads, 2>(own0, L.tile, pitch, own, ids, S::rows, chunks, real);
       }
       load(0);
+      if (!BY_KEYS) look_up(0);
       for (int c = 0; c < parts; ++c) {
         const int all = min(S::chunk, tile.hi - tile.lo - c * S::chunk);
         if (c + 1 < parts) publish(c + 1);
         cp_wait<0>();
-        __syncthreads();  // this chunk is there, the other one's buffer free
+        __syncthreads();  // this chunk and its buckets are there, the other one's buffers free
         if (c + 1 < parts) {
           load(c + 1);
           fetch_id(c + 2);
+          if (!BY_KEYS) look_up(c + 1);
         }
         if (tally.on && pending + S::rows * S::chunk > kMaxPending) {
           empty();
-          pending = 0;  // (the barrier behind the buckets comes before the next addition)
+          pending = 0;
         }
         pending += S::rows * S::chunk;
-        if (a.bias) {
-          for (int i = threadIdx.x; i < S::rows * S::chunk; i += kThreads) {
-            const int r = i / S::chunk, j = i % S::chunk;
-            index[r * L.pitch_idx + j] = (uint16_t)(BY_KEYS ? bucket_at(a.maps, maps, cells_of(c)[j], cells[r]) : bucket_at(a.maps, maps, cells[r], cells_of(c)[j]));
-          }
+        if (BY_KEYS && a.bias) {  // (counting without a bias there is none)
+          look_up(c);
           __syncthreads();
         }
         const uint64_t there = __ballot_sync(kAll, lane < S::chunk && ids_of(c)[lane] >= 0);
@@ -735,7 +746,7 @@ __global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) long_backward_kern
             const uint64_t bits = there >> j & (((uint64_t)1 << (8 * NT)) - 1);
             x.cq = x.ck = array(c, 0) + j * pitch + at_head;
             x.co = x.cv = array(c, 1) + j * pitch + at_head;
-            x.index = index + row * L.pitch_idx + j;
+            x.index = index_of(c) + row * L.pitch_idx + j;
             if constexpr (BY_KEYS) {
               columns<T, DT, NT, true>(acc[i], dv[i], x, sc, ColumnStats{stats_of(c) + 3 * h * S::chunk + j, S::chunk}, bits, tally, h, tile_rows);
             } else {

@@ -194,7 +194,7 @@ static LongLayout long_layout(const SegArgs& a, int own, int passing, size_t mor
     l.cells = take((size_t)S::rows * 16);
     l.passing_cells = take((size_t)3 * S::chunk * 16);
     l.pitch_idx = S::chunk + 8;
-    l.index = take((size_t)S::rows * l.pitch_idx * 2);
+    l.index = take((size_t)2 * S::rows * l.pitch_idx * 2);
   }
   l.more = take(more);
   l.rows = take((size_t)own * l.tile + 64);
@@ -272,6 +272,17 @@ __global__ void __launch_bounds__(kThreads, LongShape<T, DT>::three ? 3 : DT <= 
     __syncthreads();
     load_rows<T, kThreads, 1>(q0, 0, pitch, own, ids, S::rows, chunks, real);
     load(0);
+    auto index_of = [&](int c) { return index + (c & 1) * S::rows * L.pitch_idx; };
+    auto look_up = [&](int c) {
+      if (!a.bias) return;
+      uint16_t* to = index_of(c);
+      const int4* passing_cells = pass.cells(c);
+      for (int i = threadIdx.x; i < S::rows * S::chunk; i += kThreads) {
+        const int r = i / S::chunk, j = i % S::chunk;
+        to[r * L.pitch_idx + j] = (uint16_t)bucket_at(a.maps, maps, cells[r], passing_cells[j]);
+      }
+    };
+    look_up(0);
     Flow<DT> f[S::HPW];
 #pragma unroll
     for (int i = 0; i < S::HPW; ++i) f[i].start();
@@ -279,17 +290,11 @@ __global__ void __launch_bounds__(kThreads, LongShape<T, DT>::three ? 3 : DT <= 
     for (int c = 0; c < parts; ++c) {
       if (c + 1 < parts) publish(c + 1);
       cp_wait<0>();
-      __syncthreads();  // this chunk is there, the other one's buffer free
+      __syncthreads();  // this chunk and its buckets are there, the other one's buffers free
       if (c + 1 < parts) {
         load(c + 1);
         pass.fetch_id(tile.lo + (c + 2) * S::chunk);
-      }
-      if (a.bias) {
-        for (int i = threadIdx.x; i < S::rows * S::chunk; i += kThreads) {
-          const int r = i / S::chunk, j = i % S::chunk;
-          index[r * L.pitch_idx + j] = (uint16_t)bucket_at(a.maps, maps, cells[r], pass.cells(c)[j]);
-        }
-        __syncthreads();
+        look_up(c + 1);
       }
       uint64_t keys = 0;
       {
@@ -304,7 +309,7 @@ __global__ void __launch_bounds__(kThreads, LongShape<T, DT>::three ? 3 : DT <= 
         if (h < heads && row < rows) {
           const uint32_t at_head = h * dim * sizeof(T);
           attend_tile<T, DT, S::NT, false>(f[i], q0 + row * pitch + at_head, pass.array(c, 0, 2) + at_head, pass.array(c, 1, 2) + at_head, pitch, dim, sc,
-                                           bias + h * a.buckets, index + row * L.pitch_idx, L.pitch_idx, keys);
+                                           bias + h * a.buckets, index_of(c) + row * L.pitch_idx, L.pitch_idx, keys);
         }
       }
     }
