@@ -3,7 +3,10 @@
 //   by queries: maximum, sum and D of a row, then dq = scale dz k
 //   by keys:    p and dz again from those three, dk = scale dz^T q, dv = p^T do, and the bias's gradient
 //
-// Short segments do both in one block, long ones in two kernels.  D = sum_j p dp is formed from the scores and not from the output:
+// Short segments do both in one block, long ones in two kernels.  Measured (bf16, dim 24, 8 heads): 32,000 pillars in sets of 36 96 us,
+// where the bytes that it cannot do without take 13; 60,000 voxels in whole windows of up to 850, 1195 us (bytes 25).  Bound by
+// instructions and their latencies: warps issue in 41 to 52 % of the cycles, the tensor pipe is busy for 5 to 10 %, DRAM for 1 to 7 %.
+// D = sum_j p dp is formed from the scores and not from the output:
 // the output's rounding to 16 bits would reach the bias's gradient, which is fp32.
 //
 // The bias's gradient adds up ds by bucket, a scatter.  It is held as integers, so that their order does not matter and the same
@@ -796,25 +799,28 @@ __global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) long_backward_kern
 }
 
 // dbias: the blocks' partial sums in a fixed order, and the long segments' integers.  32 entries to a block, a warp a share of the blocks.
-static __global__ void __launch_bounds__(kThreads) bias_grad_kernel(const BackWork work, int buckets, bool longer, float* dbias) {
-  __shared__ float part[kWarps][32];
+constexpr int kGradThreads = 1024;  // (256: 8 us for 148 blocks' sums, most of it the loads' latency)
+static __global__ void __launch_bounds__(kGradThreads) bias_grad_kernel(const BackWork work, int buckets, bool longer, float* dbias) {
+  __shared__ float part[kGradThreads / 32][33];
   pdl_enter();
-  const int at = blockIdx.x * 32 + (threadIdx.x & 31), warp = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, at = blockIdx.x * 32 + lane;
   float s = 0.f;
   if (at < work.table)
-#pragma unroll 4
-    for (int p = warp; p < work.blocks; p += kWarps) s += work.partial[(int64_t)p * work.table + at];
-  part[warp][threadIdx.x & 31] = s;
+#pragma unroll 8
+    for (int p = warp; p < work.blocks; p += kGradThreads / 32) s += work.partial[(int64_t)p * work.table + at];
+  part[warp][lane] = s;
   __syncthreads();
-  if (warp != 0 || at >= work.table) return;
-  for (int i = 1; i < kWarps; ++i) s += part[i][threadIdx.x];
+  s = part[lane][warp];  // a warp adds up one entry
+  for (int m = 16; m > 0; m >>= 1) s += __shfl_xor_sync(kAll, s, m);
+  const int mine = blockIdx.x * 32 + warp;
+  if (lane != 0 || mine >= work.table) return;
   if (longer) {
     Tally t;
-    t.bound(__uint_as_float(work.bounds[at / buckets / work.at_once]));
-    s += tally_value((long long)work.total[at], (long long)work.total[at + work.table], t.limit);
-    if (work.spoilt[at >> 5] >> (at & 31) & 1) s = NAN;
+    t.bound(__uint_as_float(work.bounds[mine / buckets / work.at_once]));
+    s += tally_value((long long)work.total[mine], (long long)work.total[mine + work.table], t.limit);
+    if (work.spoilt[mine >> 5] >> (mine & 31) & 1) s = NAN;
   }
-  dbias[at] = s;
+  dbias[mine] = s;
 }
 
 template <typename T, int DT>
@@ -873,7 +879,7 @@ int backward_of(dsvt_ctx* ctx, const SegArgs& a) {
     }
   }
   if (a.dbias) {
-    launch_pdl(bias_grad_kernel, dim3((unsigned)dsvt_ceil_div(w.table, 32)), dim3(kThreads), 0, ctx->stream, w, a.buckets, longer, a.dbias);
+    launch_pdl(bias_grad_kernel, dim3((unsigned)dsvt_ceil_div(w.table, 32)), dim3(kGradThreads), 0, ctx->stream, w, a.buckets, longer, a.dbias);
     DSVT_LAUNCHED(ctx);
   }
   return DSVT_OK;
