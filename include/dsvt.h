@@ -3,8 +3,9 @@
  *
  * The library implements the hot path of the DSVT 3D backbone (arXiv 2301.06051):
  * rotated set partitioning (Sec. 3.2, Eq. 1-3), batched set attention (Eq. 4-5), the DSVT
- * layer and block (Eq. 5, Appendix B.1.1), the attention-style 3D pooling (Eq. 6-7) and the
- * projection of the voxel features to a bird's-eye-view map (Sec. 3.1).
+ * layer and block (Eq. 5, Appendix B.1.1), the attention-style 3D pooling (Eq. 6-7), the
+ * projection of the voxel features to a bird's-eye-view map (Sec. 3.1), and what training a layer needs
+ * between its projections: attention and LayerNorm with their gradients.
  *
  * Conventions that hold for every call unless a comment says otherwise:
  *   - Every data pointer is a DEVICE pointer owned by the caller.  The library reads / writes it
@@ -31,7 +32,8 @@
  *     and features: 1.2e-7 where these are off by 0.8e-7).
  *     precision = DSVT_BF16_FP32ACC: weights are bfloat16 (16-bit storage); products
  *     accumulate in fp32; residual stream, LayerNorm, softmax and GELU are fp32.
- *     Features (x, y, feats, out) and biases / LayerNorm parameters are always float.
+ *     Features (x, y, feats, out) and biases / LayerNorm parameters are always float.  (The training operators, dsvt_segment_attention,
+ *     dsvt_layer_norm and their backward passes, have rows of a storage type of their own, DSVT_TYPE_*, and no weights.)
  */
 #ifndef DSVT_H_
 #define DSVT_H_
