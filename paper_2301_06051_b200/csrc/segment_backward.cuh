@@ -6,8 +6,8 @@
 // Short segments do both in one block, long ones in two kernels.  Measured (bf16, dim 24, 8 heads): 32,000 pillars in sets of 36 96 us,
 // where the bytes that it cannot do without take 13; 60,000 voxels in whole windows of up to 850, 1195 us (bytes 25).  Bound by
 // instructions and their latencies: warps issue in 41 to 52 % of the cycles, the tensor pipe is busy for 5 to 10 %, DRAM for 1 to 7 %.
-// D = sum_j p dp is formed from the scores and not from the output:
-// the output's rounding to 16 bits would reach the bias's gradient, which is fp32.
+// D = sum_j p dp is formed from the scores and not from the output: the output's rounding to 16 bits would reach the bias's gradient,
+// which is fp32.
 //
 // The bias's gradient adds up ds by bucket, a scatter.  It is held as integers, so that their order does not matter and the same
 // inputs give the same bits: v = (hi 2^-17 + lo 2^-35) limit with |hi|, |lo| <= 2^17, two words of shared memory to a bucket, which
@@ -23,6 +23,8 @@
 namespace dsvt_train {
 
 constexpr int kMaxPending = 16000;
+constexpr int kShortBack = 120;  // most rows of a segment that is held whole here: its pairs may all be of one bucket
+static_assert(kShortBack * kShortBack <= kMaxPending && kShortBack <= kShort, "a batch of one segment is counted without being emptied");
 constexpr int kHiBits = 17, kLoBits = 18;
 constexpr float kMagic = 12582912.f;  // 1.5 x 2^23: adding it rounds to a whole number in the low bits
 
@@ -417,121 +419,121 @@ __global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) short_backward_ker
     __syncthreads();
     const Range range = start_range<kThreads>(a, plan, r, L.s.ranges, L.s.per);
     while (next_batch<kThreads>(a, plan, range, L.s.limit, L.s.batch)) {
-    if (threadIdx.x == 0) block_bound = 0;
-    if (a.bias) {
-      load_cells<kThreads>(a, smem_u32(cells), plan.ids, plan.rows);
+      if (threadIdx.x == 0) block_bound = 0;
+      if (a.bias) {
+        load_cells<kThreads>(a, smem_u32(cells), plan.ids, plan.rows);
+        cp_commit();
+      }
+      load_rows<T, kThreads, 4>(q0, L.s.array, pitch, src, plan.ids, plan.rows, chunks, real);
       cp_commit();
-    }
-    load_rows<T, kThreads, 4>(q0, L.s.array, pitch, src, plan.ids, plan.rows, chunks, real);
-    cp_commit();
-    if (a.bias) {
-      cp_wait<1>();
+      if (a.bias) {
+        cp_wait<1>();
+        __syncthreads();
+        fill_index<kThreads>(a, plan, cells, maps, index, L.s.pitch_idx);
+      }
+      cp_wait<0>();
       __syncthreads();
-      fill_index<kThreads>(a, plan, cells, maps, index, L.s.pitch_idx);
-    }
-    cp_wait<0>();
-    __syncthreads();
-    if (h < heads) {
-      float most = 0.f;
-      for (int it = warp / HG; it < plan.items; it += kWarps / HG) {
-        const Item item = plan.item[it];
-        const int row = item.at + 16 * item.tile, r0 = 16 * item.tile + g;
-        x.q = q0 + row * pitch + at_head; x.o = o0 + row * pitch + at_head;
-        auto to_chunk = [&](int j) {
-          const uint32_t at = (item.at + j) * pitch + at_head;
-          x.ck = k0 + at; x.cv = v0 + at;
-          x.index = index + row * L.s.pitch_idx + j;
-        };
-        float acc[DT / 8][4], bound[2];
-        float3 st[2];
-        clear<DT>(acc);
-        to_chunk(0);
-        if (item.len <= 40) {
-          const uint64_t keys = real_rows(plan, item.at, item.len);
-          switch ((item.len + 7) >> 3) {
-            case 1: rows_at_once<T, DT, 1>(acc, st, bound, x, sc, keys); break;
-            case 2: rows_at_once<T, DT, 2>(acc, st, bound, x, sc, keys); break;
-            case 3: rows_at_once<T, DT, 3>(acc, st, bound, x, sc, keys); break;
-            case 4: rows_at_once<T, DT, 4>(acc, st, bound, x, sc, keys); break;
-            default: rows_at_once<T, DT, 5>(acc, st, bound, x, sc, keys);
-          }
-        } else {
-          RowSums f;
-          f.start();
-          const int tiles = (item.len + 7) >> 3;
-          for (int pass = 0; pass < 2; ++pass) {  // two tiles at a time
-            for (int j = 0; j < item.len; j += 16) {
-              const int now = min(2, tiles - (j >> 3));
-              const uint64_t keys = real_rows(plan, item.at + j, min(8 * now, item.len - j));
-              to_chunk(j);
+      if (h < heads) {
+        float most = 0.f;
+        for (int it = warp / HG; it < plan.items; it += kWarps / HG) {
+          const Item item = plan.item[it];
+          const int row = item.at + 16 * item.tile, r0 = 16 * item.tile + g;
+          x.q = q0 + row * pitch + at_head; x.o = o0 + row * pitch + at_head;
+          auto to_chunk = [&](int j) {
+            const uint32_t at = (item.at + j) * pitch + at_head;
+            x.ck = k0 + at; x.cv = v0 + at;
+            x.index = index + row * L.s.pitch_idx + j;
+          };
+          float acc[DT / 8][4], bound[2];
+          float3 st[2];
+          clear<DT>(acc);
+          to_chunk(0);
+          if (item.len <= 40) {
+            const uint64_t keys = real_rows(plan, item.at, item.len);
+            switch ((item.len + 7) >> 3) {
+              case 1: rows_at_once<T, DT, 1>(acc, st, bound, x, sc, keys); break;
+              case 2: rows_at_once<T, DT, 2>(acc, st, bound, x, sc, keys); break;
+              case 3: rows_at_once<T, DT, 3>(acc, st, bound, x, sc, keys); break;
+              case 4: rows_at_once<T, DT, 4>(acc, st, bound, x, sc, keys); break;
+              default: rows_at_once<T, DT, 5>(acc, st, bound, x, sc, keys);
+            }
+          } else {
+            RowSums f;
+            f.start();
+            const int tiles = (item.len + 7) >> 3;
+            for (int pass = 0; pass < 2; ++pass) {  // two tiles at a time
+              for (int j = 0; j < item.len; j += 16) {
+                const int now = min(2, tiles - (j >> 3));
+                const uint64_t keys = real_rows(plan, item.at + j, min(8 * now, item.len - j));
+                to_chunk(j);
+                if (pass == 0) {
+                  if (now == 2) rows_first<T, DT, 2>(f, x, sc, keys);
+                  else rows_first<T, DT, 1>(f, x, sc, keys);
+                } else {
+                  if (now == 2) rows_second<T, DT, 2>(acc, st, x, sc, keys);
+                  else rows_second<T, DT, 1>(acc, st, x, sc, keys);
+                }
+              }
               if (pass == 0) {
-                if (now == 2) rows_first<T, DT, 2>(f, x, sc, keys);
-                else rows_first<T, DT, 1>(f, x, sc, keys);
-              } else {
-                if (now == 2) rows_second<T, DT, 2>(acc, st, x, sc, keys);
-                else rows_second<T, DT, 1>(acc, st, x, sc, keys);
+                st[0] = row_stats(f, 0, &bound[0]);
+                st[1] = row_stats(f, 1, &bound[1]);
               }
             }
-            if (pass == 0) {
-              st[0] = row_stats(f, 0, &bound[0]);
-              st[1] = row_stats(f, 1, &bound[1]);
-            }
           }
+          const int id0 = r0 < item.len ? plan.ids[item.at + r0] : -1, id1 = r0 + 8 < item.len ? plan.ids[item.at + r0 + 8] : -1;
+          if (id0 >= 0) most = fmaxf(most, bound[0]);
+          if (id1 >= 0) most = fmaxf(most, bound[1]);
+          if ((lane & 3) == 0) {
+            float* to = stats + 3 * h * stat_rows + row + g;
+            if (r0 < item.len) { to[0] = st[0].x; to[stat_rows] = st[0].y; to[2 * stat_rows] = st[0].z; }
+            if (r0 + 8 < item.len) { to[8] = st[1].x; to[stat_rows + 8] = st[1].y; to[2 * stat_rows + 8] = st[1].z; }
+          }
+          store_rows<T, DT>(acc, a.scale, a.dq, a.ld_dq, col + h * dim, dim, id0, id1);
         }
-        const int id0 = r0 < item.len ? plan.ids[item.at + r0] : -1, id1 = r0 + 8 < item.len ? plan.ids[item.at + r0 + 8] : -1;
-        if (id0 >= 0) most = fmaxf(most, bound[0]);
-        if (id1 >= 0) most = fmaxf(most, bound[1]);
-        if ((lane & 3) == 0) {
-          float* to = stats + 3 * h * stat_rows + row + g;
-          if (r0 < item.len) { to[0] = st[0].x; to[stat_rows] = st[0].y; to[2 * stat_rows] = st[0].z; }
-          if (r0 + 8 < item.len) { to[8] = st[1].x; to[stat_rows + 8] = st[1].y; to[2 * stat_rows + 8] = st[1].z; }
+        if (tally.on) {
+          for (int m = 16; m > 0; m >>= 1) most = fmaxf(most, __shfl_xor_sync(kAll, most, m));
+          if (lane == 0) atomicMax(&block_bound, __float_as_uint(most));
         }
-        store_rows<T, DT>(acc, a.scale, a.dq, a.ld_dq, col + h * dim, dim, id0, id1);
       }
+      __syncthreads();
       if (tally.on) {
-        for (int m = 16; m > 0; m >>= 1) most = fmaxf(most, __shfl_xor_sync(kAll, most, m));
-        if (lane == 0) atomicMax(&block_bound, __float_as_uint(most));
-      }
-    }
-    __syncthreads();
-    if (tally.on) {
-      const int pairs = plan.pairs;
-      const float b = __uint_as_float(block_bound);
-      if (2.f * b > tally.limit || pending + pairs > kMaxPending) {  // (a value of the second pass may round to more than the bound)
-        if (pending > 0) empty();
-        if (2.f * b > tally.limit) tally.bound(b);
-        __syncthreads();
-      }
-      pending += pairs;
-    }
-    if (h < heads) {
-      for (int it = warp / HG; it < plan.items; it += kWarps / HG) {
-        const Item item = plan.item[it];
-        const int row = item.at + 16 * item.tile, r0 = 16 * item.tile + g;
-        const int id0 = r0 < item.len ? plan.ids[item.at + r0] : -1, id1 = r0 + 8 < item.len ? plan.ids[item.at + r0 + 8] : -1;
-        float dk[DT / 8][4], dv[DT / 8][4];
-        clear<DT>(dk);
-        clear<DT>(dv);
-        x.k = k0 + row * pitch + at_head; x.v = v0 + row * pitch + at_head;
-        const uint32_t tile_rows = (uint32_t)real_rows(plan, row, min(16, item.len - 16 * item.tile));
-        // (Two tiles at a time and not four: half the code, and no spilled registers.  Kernels of this size miss in the instruction cache:
-        // 32,000 pillars bf16 148 us with four, 127 with two; fp32, 12,345 with a cap, 352 and 255.)
-        for (int j = 0; j < item.len; j += 16) {
-          const int cols = min(16, item.len - j);
-          const uint64_t queries = real_rows(plan, item.at + j, cols);
-          const uint32_t at = (item.at + j) * pitch + at_head;
-          const ColumnStats from = {stats + 3 * h * stat_rows + item.at + j, stat_rows};
-          x.cq = q0 + at; x.co = o0 + at;
-          x.index = index + (item.at + j) * L.s.pitch_idx + 16 * item.tile;
-          if (cols > 8) columns<T, DT, 2, false>(dk, dv, x, sc, from, queries, tally, h, tile_rows);
-          else columns<T, DT, 1, false>(dk, dv, x, sc, from, queries, tally, h, tile_rows);
+        const int pairs = plan.pairs;
+        const float b = __uint_as_float(block_bound);
+        if (2.f * b > tally.limit || pending + pairs > kMaxPending) {  // (a value of the second pass may round to more than the bound)
+          if (pending > 0) empty();
+          if (2.f * b > tally.limit) tally.bound(b);
+          __syncthreads();
         }
-        store_rows<T, DT>(dk, a.scale, a.dk, a.ld_dk, col + h * dim, dim, id0, id1);
-        store_rows<T, DT>(dv, 1.f, a.dv, a.ld_dv, col + h * dim, dim, id0, id1);
+        pending += pairs;
       }
-    }
-    if (plan.cursor >= range.end) break;
-    __syncthreads();
+      if (h < heads) {
+        for (int it = warp / HG; it < plan.items; it += kWarps / HG) {
+          const Item item = plan.item[it];
+          const int row = item.at + 16 * item.tile, r0 = 16 * item.tile + g;
+          const int id0 = r0 < item.len ? plan.ids[item.at + r0] : -1, id1 = r0 + 8 < item.len ? plan.ids[item.at + r0 + 8] : -1;
+          float dk[DT / 8][4], dv[DT / 8][4];
+          clear<DT>(dk);
+          clear<DT>(dv);
+          x.k = k0 + row * pitch + at_head; x.v = v0 + row * pitch + at_head;
+          const uint32_t tile_rows = (uint32_t)real_rows(plan, row, min(16, item.len - 16 * item.tile));
+          // (Two tiles at a time and not four: half the code, and no spilled registers.  Kernels of this size miss in the instruction cache:
+          // 32,000 pillars bf16 148 us with four, 127 with two; fp32, 12,345 with a cap, 352 and 255.)
+          for (int j = 0; j < item.len; j += 16) {
+            const int cols = min(16, item.len - j);
+            const uint64_t queries = real_rows(plan, item.at + j, cols);
+            const uint32_t at = (item.at + j) * pitch + at_head;
+            const ColumnStats from = {stats + 3 * h * stat_rows + item.at + j, stat_rows};
+            x.cq = q0 + at; x.co = o0 + at;
+            x.index = index + (item.at + j) * L.s.pitch_idx + 16 * item.tile;
+            if (cols > 8) columns<T, DT, 2, false>(dk, dv, x, sc, from, queries, tally, h, tile_rows);
+            else columns<T, DT, 1, false>(dk, dv, x, sc, from, queries, tally, h, tile_rows);
+          }
+          store_rows<T, DT>(dk, a.scale, a.dk, a.ld_dk, col + h * dim, dim, id0, id1);
+          store_rows<T, DT>(dv, 1.f, a.dv, a.ld_dv, col + h * dim, dim, id0, id1);
+        }
+      }
+      if (plan.cursor >= range.end) break;
+      __syncthreads();
     }
   }
   if (tally.on) {
@@ -825,7 +827,7 @@ static __global__ void __launch_bounds__(kGradThreads) bias_grad_kernel(const Ba
 
 template <typename T, int DT>
 int backward_of(dsvt_ctx* ctx, const SegArgs& a) {
-  int limit = a.max_len <= kShort ? a.max_len : 64;
+  int limit = a.max_len <= kShortBack ? a.max_len : 64;
   // the largest batch that leaves room for two blocks on an SM (32,000 pillars bf16: 64 rows 103 us, 80 rows 97), if one does
   int batch = 96;
   BackLayout l = back_layout<T, DT>(a, limit, batch);

@@ -13,7 +13,8 @@
 
 namespace dsvt_train {
 
-// Heads of a block that holds its segments whole: rows of at most 400 bytes, which leaves room for two blocks on an SM.
+// Heads of a block that holds its segments whole: rows of at most 400 bytes, which leaves room for three blocks of 36-voxel sets on an SM
+// (32,000 pillars: 24 warps an SM at 80 registers 34 us, 16 at 123 45).
 template <typename T, int DT>
 constexpr int kHeads = DT * sizeof(T) <= 48 ? 8 : DT * sizeof(T) <= 96 ? 4 : DT * sizeof(T) <= 128 ? 2 : 1;
 
@@ -92,82 +93,82 @@ __global__ void __launch_bounds__(kShortThreads, DT <= 24 && sizeof(T) == 2 ? 3 
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   bool staged = false;
   while (next_batch<kShortThreads>(a, plan, range, L.limit, L.batch)) {
-  if (a.bias) {
-    load_cells<kShortThreads>(a, smem_u32(cells), plan.ids, plan.rows);
-    cp_commit();
-  }
-  load_rows<T, kShortThreads, 3>(q0, L.array, pitch, src, plan.ids, plan.rows, chunks, real);
-  cp_commit();
-  if (a.bias) {
-    if (!staged) {  // (while the rows are on their way)
-      stage_tables<kShortThreads>(a, maps, bias, head0, HG);
-      staged = true;
+    if (a.bias) {
+      load_cells<kShortThreads>(a, smem_u32(cells), plan.ids, plan.rows);
+      cp_commit();
     }
-    cp_wait<1>();
+    load_rows<T, kShortThreads, 3>(q0, L.array, pitch, src, plan.ids, plan.rows, chunks, real);
+    cp_commit();
+    if (a.bias) {
+      if (!staged) {  // (while the rows are on their way)
+        stage_tables<kShortThreads>(a, maps, bias, head0, HG);
+        staged = true;
+      }
+      cp_wait<1>();
+      __syncthreads();
+      fill_index<kShortThreads>(a, plan, cells, maps, index, L.pitch_idx);
+    }
+    cp_wait<0>();
     __syncthreads();
-    fill_index<kShortThreads>(a, plan, cells, maps, index, L.pitch_idx);
-  }
-  cp_wait<0>();
-  __syncthreads();
-  const int h = warp % HG;
-  for (int it = warp / HG; it < plan.items; it += kShortThreads / 32 / HG) {
-    if (h >= heads) break;
-    const Item item = plan.item[it];
-    const uint32_t at_head = h * dim * sizeof(T);
-    const float* mine = bias + h * a.buckets;
-    const int row = item.at + 16 * item.tile;
-    const uint32_t q = q0 + row * pitch + at_head, k = k0 + item.at * pitch + at_head, v = v0 + item.at * pitch + at_head;
-    const uint16_t* at = index + row * L.pitch_idx;
-    Flow<DT> f;
-    f.start();
+    const int h = warp % HG;
+    for (int it = warp / HG; it < plan.items; it += kShortThreads / 32 / HG) {
+      if (h >= heads) break;
+      const Item item = plan.item[it];
+      const uint32_t at_head = h * dim * sizeof(T);
+      const float* mine = bias + h * a.buckets;
+      const int row = item.at + 16 * item.tile;
+      const uint32_t q = q0 + row * pitch + at_head, k = k0 + item.at * pitch + at_head, v = v0 + item.at * pitch + at_head;
+      const uint16_t* at = index + row * L.pitch_idx;
+      Flow<DT> f;
+      f.start();
 #define DSVT_ATTEND(NT) attend_tile<T, DT, NT, true>(f, q, k, v, pitch, dim, sc, mine, at, L.pitch_idx, real_rows(plan, item.at, item.len))
 #define DSVT_ATTEND_PART(NT)                                                                               \
-  attend_tile<T, DT, NT, false>(f, q, k + j * pitch, v + j * pitch, pitch, dim, sc, mine, at + j, L.pitch_idx, \
-                                real_rows(plan, item.at + j, min(8 * NT, item.len - j)))
-    // Up to 40 keys at once, in 16-bit types; more, and fp32, in parts of up to 24.  (Fewer widths in fp32, and no wider parts: kernels of
-    // this size miss in the instruction cache.  12,345 pillars fp32 38.2 us with five widths, 35.6 with three; sets of 90 in parts of
-    // up to 40 65.1, of up to 24 61.4.)
-    const int tiles = (item.len + 7) >> 3;
-    if (sizeof(T) == 2 && tiles <= 5) {
-      switch (tiles) {
-        case 1: DSVT_ATTEND(1); break;
-        case 2: DSVT_ATTEND(2); break;
-        case 3: DSVT_ATTEND(3); break;
-        case 4: DSVT_ATTEND(4); break;
-        default: DSVT_ATTEND(5);
+    attend_tile<T, DT, NT, false>(f, q, k + j * pitch, v + j * pitch, pitch, dim, sc, mine, at + j, L.pitch_idx, \
+                                  real_rows(plan, item.at + j, min(8 * NT, item.len - j)))
+      // Up to 40 keys at once, in 16-bit types; more, and fp32, in parts of up to 24.  (Fewer widths in fp32, and no wider parts: kernels of
+      // this size miss in the instruction cache.  12,345 pillars fp32 38.2 us with five widths, 35.6 with three; sets of 90 in parts of
+      // up to 40 65.1, of up to 24 61.4.)
+      const int tiles = (item.len + 7) >> 3;
+      if (sizeof(T) == 2 && tiles <= 5) {
+        switch (tiles) {
+          case 1: DSVT_ATTEND(1); break;
+          case 2: DSVT_ATTEND(2); break;
+          case 3: DSVT_ATTEND(3); break;
+          case 4: DSVT_ATTEND(4); break;
+          default: DSVT_ATTEND(5);
+        }
+      } else {
+        for (int j = 0; j < item.len; j += 24) {
+          if (item.len - j > 16) DSVT_ATTEND_PART(3);
+          else if (item.len - j > 8) DSVT_ATTEND_PART(2);
+          else DSVT_ATTEND_PART(1);
+        }
       }
-    } else {
-      for (int j = 0; j < item.len; j += 24) {
-        if (item.len - j > 16) DSVT_ATTEND_PART(3);
-        else if (item.len - j > 8) DSVT_ATTEND_PART(2);
-        else DSVT_ATTEND_PART(1);
-      }
-    }
 #undef DSVT_ATTEND
 #undef DSVT_ATTEND_PART
-    // the result takes the place of the queries (this warp's alone: its head's channels of a tile's rows)
-    const int r0 = 16 * item.tile + (lane >> 2);
-    const float i0 = inverse(quad_sum(f.l[0])), i1 = inverse(quad_sum(f.l[1]));
-    T* to = reinterpret_cast<T*>(smem + L.rows + (item.at + r0) * pitch + at_head) + (lane & 3) * 2;
-    __syncwarp();
+      // the result takes the place of the queries (this warp's alone: its head's channels of a tile's rows)
+      const int r0 = 16 * item.tile + (lane >> 2);
+      const float i0 = inverse(quad_sum(f.l[0])), i1 = inverse(quad_sum(f.l[1]));
+      T* to = reinterpret_cast<T*>(smem + L.rows + (item.at + r0) * pitch + at_head) + (lane & 3) * 2;
+      __syncwarp();
 #pragma unroll
-    for (int n = 0; n < DT / 8; ++n) {
-      if (!kExact<DT> && n * 8 >= dim) break;
-      if (r0 < item.len) store2<T>(to + n * 8, f.acc[n][0] * i0, f.acc[n][1] * i0);
-      if (r0 + 8 < item.len) store2<T>(reinterpret_cast<T*>(reinterpret_cast<char*>(to) + 8 * pitch) + n * 8, f.acc[n][2] * i1, f.acc[n][3] * i1);
+      for (int n = 0; n < DT / 8; ++n) {
+        if (!kExact<DT> && n * 8 >= dim) break;
+        if (r0 < item.len) store2<T>(to + n * 8, f.acc[n][0] * i0, f.acc[n][1] * i0);
+        if (r0 + 8 < item.len) store2<T>(reinterpret_cast<T*>(reinterpret_cast<char*>(to) + 8 * pitch) + n * 8, f.acc[n][2] * i1, f.acc[n][3] * i1);
+      }
     }
-  }
-  __syncthreads();
-  const int part = threadIdx.x & 7;
-  for (int r = threadIdx.x >> 3; r < plan.rows; r += kShortThreads / 8) {
-    const int id = plan.ids[r];
-    if (id < 0) continue;
-    char* to = (char*)a.out + (id * a.ld_out + col) * (int64_t)sizeof(T);
+    __syncthreads();
+    const int part = threadIdx.x & 7;
+    for (int r = threadIdx.x >> 3; r < plan.rows; r += kShortThreads / 8) {
+      const int id = plan.ids[r];
+      if (id < 0) continue;
+      char* to = (char*)a.out + (id * a.ld_out + col) * (int64_t)sizeof(T);
 #pragma unroll 4
-    for (int c = part; c < real; c += 8) *reinterpret_cast<uint4*>(to + c * 16) = *reinterpret_cast<const uint4*>(smem + L.rows + r * pitch + c * 16);
-  }
-  if (plan.cursor >= range.end) break;
-  __syncthreads();
+      for (int c = part; c < real; c += 8) *reinterpret_cast<uint4*>(to + c * 16) = *reinterpret_cast<const uint4*>(smem + L.rows + r * pitch + c * 16);
+    }
+    if (plan.cursor >= range.end) break;
+    __syncthreads();
   }
 }
 
