@@ -388,6 +388,50 @@ def test_a_context_on_its_own_stream_and_captured_graphs():
     own.close()
 
 
+def test_two_contexts_at_once():
+    """Calls of two contexts, each with its stream and workspace, in flight together."""
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    own = [api.Context(3000, 64, 256, stream=s) for s in streams]
+    problems = [Problem([36, 20, 200, 1, 50] * 5, 8, 24, torch.bfloat16, seed=i, packed=False) for i in range(2)]
+    torch.cuda.synchronize()
+    alone = []
+    for c, p in zip(own, problems):
+        with torch.cuda.stream(c.stream):
+            alone.append([t.clone() for t in (p.forward(c), *p.backward(c))])
+        torch.cuda.synchronize()
+    for _ in range(5):
+        together = []
+        for c, p in zip(own, problems):
+            with torch.cuda.stream(c.stream):
+                together.append([p.forward(c), *p.backward(c)])
+        torch.cuda.synchronize()
+        for a, b in zip(alone, together):
+            assert all(torch.equal(x, y) for x, y in zip(a, b))
+    for c in own:
+        assert c.status_sync() == 0
+        c.close()
+
+
+def test_calls_in_turn_with_partitions_and_layers(ctx):
+    """The workspace is the partition's: one leaves nothing behind that the other takes for its own."""
+    g = torch.Generator().manual_seed(4)
+    cells = torch.randperm(3600, generator=g)[:1200]
+    coords = torch.stack([torch.zeros_like(cells), cells // 60, cells % 60, torch.zeros_like(cells)], 1).to(torch.int32).cuda()
+    p = Problem([36, 200, 7], 8, 24, torch.bfloat16, seed=3)
+    first = ctx.partition(coords, 1, (60, 60, 1), (12, 12, 1), 16, 0, extras=True)
+    grads = [t.clone() for t in p.backward(ctx)]
+    x = torch.randn((1200, 192), device="cuda")
+    dx = [t.clone() for t in ctx.layer_norm_backward(x, x, None)]
+    for _ in range(3):
+        again = ctx.partition(coords, 1, (60, 60, 1), (12, 12, 1), 16, 0, extras=True)
+        assert all(torch.equal(a, b) for a, b in zip(p.backward(ctx), grads))
+        assert all(torch.equal(a, b) for a, b in zip(ctx.layer_norm_backward(x, x, None), dx))
+        sets = int(first.num_sets.item())
+        assert int(again.num_sets.item()) == sets and torch.equal(again.set_table[:sets], first.set_table[:sets])
+        assert torch.equal(again.perm, first.perm) and torch.equal(again.win_start, first.win_start)
+    assert ctx.status_sync() == 0
+
+
 def test_refusals(ctx):
     lib, h = ctx.lib, ctx._h
     p = Problem([5, 6], 2, 16, torch.bfloat16, seed=1, packed=False)
