@@ -410,12 +410,12 @@ int dsvt_bev_scatter(dsvt_ctx* ctx, const int32_t* coords, const float* feats, i
  *   seg_start   int32 [cap_segments + 1], ascending, in [0, n]; empty segments are fine.
  *   num_segments device int32 (at most cap_segments count), or NULL for cap_segments.
  *   max_len     host upper bound of the segments' lengths (1 ... n; larger values count as n).  A longer segment is left out and
- *               raises DSVT_STATUS_TABLE_OVERFLOW.  Sets: set_size.  It chooses the kernels: segments of up to some 120 voxels are held in shared
- *               memory whole.
+ *               raises DSVT_STATUS_TABLE_OVERFLOW.  Sets: set_size.  It chooses the kernels: segments of up to some 120
+ *               voxels are held in shared memory whole.
  *   bias        float [heads][buckets], or NULL (then buckets, coords, extent and bucket_of are not looked at).
  *   coords      int32 [n][4] = (b, x, y, z), magnitudes below 2^30; 16-byte aligned.
  *   bucket_of   HOST int32 [(2L-1) + (2W-1) + (2H-1)]: bx, by, bz one after the other, every sum of three in [0, buckets).
- *               T5's buckets (exact for small displacements, then by logarithm) are such tables; so is one bucket per displacement.
+ *               Buckets exact for small displacements, then by logarithm, are such tables; so is one bucket per displacement.
  *   out         rows of `type`, stride ld_out, 16-byte aligned; may not alias the inputs.  Rows of voxels in no segment are
  *               left as they were.
  *
