@@ -401,8 +401,9 @@ int dsvt_bev_scatter(dsvt_ctx* ctx, const int32_t* coords, const float* feats, i
  *
  * A bias entry of -inf masks its pairs, in a row with others one of the lowest float does too; a row whose scores are all
  * -inf gives zeros (and gets and passes on no gradient), one whose scores are all the lowest float equal weights.  (Finite
- * entries below -FLT_MAX / log2(e) count as the lowest float.)  A voxel with features that are not finite spoils the rows of its
- * own segment and no others, in masked pairs too.
+ * entries beyond FLT_MAX / log2(e) in magnitude count as the lowest or the largest float.)  A row with a score of NaN or +inf is
+ * NaN in that head, in out and dq; dk and dv of its segment are too, and dbias of every bucket that the row has a pair of.  A voxel with
+ * features that are not finite spoils the rows of its own segment and no others, in masked pairs too.
  *
  *   q, k, v     rows of `type`, row i at q + i * ld_q (elements), channel c of head h at h * head_dim + c; 16-byte aligned, as are
  *               their row strides.  One projection's output [n][3C] gives q, k = q + C, v = q + 2C, ld = 3C.

@@ -329,8 +329,12 @@ __device__ __forceinline__ float tanh_of(float x) {
   const float far = copysignf(__fdividef(1.f - e, 1.f + e), x);
   return a < 0.25f ? near : far;  // (NaN: far)
 }
-// A bias entry in units of log 2.  (Clamped: the lowest float stays the lowest, whatever is added, and differences of two are zero.)
-__device__ __forceinline__ float bias_log2(float b) { return b == -INFINITY ? b : fmaxf(b * kLog2e, -3.402823466e38f); }
+// A bias entry in units of log 2.  (Clamped where it is finite: the lowest float stays the lowest, whatever is added, differences of two
+// are zero, and the largest is no infinity.  NaN stays NaN: minimum and maximum functions would return the other operand.)
+__device__ __forceinline__ float bias_log2(float b) {
+  const float x = b * kLog2e;
+  return isinf(x) && !isinf(b) ? copysignf(3.402823466e38f, b) : x;
+}
 
 template <int NT>
 __device__ __forceinline__ void cap_products(float (&s)[NT][4], const Scoring& sc) {
