@@ -410,7 +410,7 @@ int dsvt_bev_scatter(dsvt_ctx* ctx, const int32_t* coords, const float* feats, i
  *   order       int32 [n], or NULL for 0, 1, 2, ...;  no voxel twice.
  *   seg_start   int32 [cap_segments + 1], ascending, in [0, n]; empty segments are fine.
  *   num_segments device int32 (at most cap_segments count), or NULL for cap_segments.
- *   max_len     host upper bound of the segments' lengths (1 ... n; larger values count as n).  A longer segment is left out and
+ *   max_len     host upper bound of the segments' lengths (1 ... n, 0 where n is 0; larger values count as n).  A longer segment is left out and
  *               raises DSVT_STATUS_TABLE_OVERFLOW.  Sets: set_size.  It chooses the kernels: segments of up to some 120
  *               voxels are held in shared memory whole.
  *   bias        float [heads][buckets], or NULL (then buckets, coords, extent and bucket_of are not looked at).
@@ -422,6 +422,8 @@ int dsvt_bev_scatter(dsvt_ctx* ctx, const int32_t* coords, const float* feats, i
  *
  * Scores, softmax and sums are fp32.  With 16-bit types the weights P (and in the backward pass P and dS) are rounded to the type
  * for the products with v (do, q, k).  With DSVT_TYPE_F32 operands go through the tensor cores as two tf32 parts (22 bits).
+ *
+ * n = 0 is valid: rows, order, seg_start and coords may be NULL then, and dbias is zeros.
  *
  * Needs head_dim % 8 == 0, head_dim <= 128, buckets <= 1024, extents <= 128, heads <= 65535 (else DSVT_ERR_UNSUPPORTED); n <=
  * max_voxels (else DSVT_ERR_CAPACITY; the number of channels is not limited).  An order entry outside [0, n) is skipped, a

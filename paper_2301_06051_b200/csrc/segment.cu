@@ -12,7 +12,7 @@ bool bad_rows(const void* p, int64_t ld, int64_t width, int size) {
 
 int check(const dsvt_ctx* ctx, const dsvt_segment_attention_params* p, SegArgs* a) {
   if (!ctx || !p || p->n < 0 || p->heads < 1 || p->head_dim < 1 || !type_known(p->type)) return DSVT_ERR_INVALID_ARG;
-  if (p->cap_segments < 0 || p->max_len < 1 || !(p->cap >= 0.f) || isinf(p->cap)) return DSVT_ERR_INVALID_ARG;
+  if (p->cap_segments < 0 || p->max_len < (p->n > 0 ? 1 : 0) || !(p->cap >= 0.f) || isinf(p->cap)) return DSVT_ERR_INVALID_ARG;
   if (p->head_dim % 8 != 0 || p->head_dim > kMaxDim || p->heads > kMaxHeads) return DSVT_ERR_UNSUPPORTED;
   if (p->n > ctx->max_voxels) return DSVT_ERR_CAPACITY;
   const int64_t width = (int64_t)p->heads * p->head_dim;
@@ -33,7 +33,7 @@ int check(const dsvt_ctx* ctx, const dsvt_segment_attention_params* p, SegArgs* 
   a->scale = p->scale; a->cap = p->cap;
   a->status = ctx->status;
   if (!p->bias) return DSVT_OK;
-  if (!p->coords || ((uintptr_t)p->coords & 15) != 0 || !p->bucket_of || p->buckets < 1) return DSVT_ERR_INVALID_ARG;
+  if ((p->n > 0 && !p->coords) || ((uintptr_t)p->coords & 15) != 0 || !p->bucket_of || p->buckets < 1) return DSVT_ERR_INVALID_ARG;
   if (p->buckets > kMaxBuckets) return DSVT_ERR_UNSUPPORTED;
   int64_t low = 0, high = 0;
   int at = 0;

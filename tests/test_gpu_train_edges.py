@@ -81,3 +81,21 @@ def test_a_bias_of_the_largest_float_takes_all_the_weight(ctx, typ, lens):
         bound = (EPS[typ] / 2 + (len(ids) + 24) * ref.U) * size * (1 + EPS[typ]) + EPS[typ] / 2 * want.abs() + 1e-6 * EPS[typ]
         assert ((got[torch.from_numpy(ids)] - want).abs() <= bound).all()
     assert ctx.status_sync() == 0
+
+
+# ---- nothing to do -----------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("max_len", [36, 0])
+def test_no_voxels_with_a_bias(ctx, max_len):
+    index, buckets = api.log_buckets((6, 6, 1), (2, 2, 1), (4, 4, 1))
+    rel = api.BucketBias(torch.randn((4, buckets), device="cuda"), (6, 6, 1), index)
+    e = torch.empty((0, 4, 16), dtype=torch.bfloat16, device="cuda")
+    seg = api.Segments(torch.zeros(3, dtype=torch.int32, device="cuda"), max_len, torch.empty(0, dtype=torch.int32, device="cuda"),
+                       torch.empty((0, 4), dtype=torch.int32, device="cuda"))
+    assert ctx.segment_attention(e, e, e, seg, bias=rel).shape == e.shape
+    dbias = torch.full_like(rel.table, 9.0)
+    grads = ctx.segment_attention_backward(e, e, e, e, seg, bias=rel, dbias=dbias)
+    assert all(t.shape == e.shape for t in grads[:3]) and torch.all(dbias == 0)
+    bad = api.BucketBias(rel.table, (6, 6, 1), np.full(23, 10000))
+    with pytest.raises(api.DsvtError):  # the tables are looked at all the same
+        ctx.segment_attention(e, e, e, seg, bias=bad)
+    assert ctx.status_sync() == 0
