@@ -427,7 +427,9 @@ int dsvt_bev_scatter(dsvt_ctx* ctx, const int32_t* coords, const float* feats, i
  *
  * Needs head_dim % 8 == 0, head_dim <= 128, buckets <= 1024, extents <= 128, heads <= 65535 (else DSVT_ERR_UNSUPPORTED); n <=
  * max_voxels (else DSVT_ERR_CAPACITY; the number of channels is not limited).  An order entry outside [0, n) is skipped, a
- * seg_start entry outside [0, n] or below its predecessor drops its segment, both with DSVT_STATUS_BAD_INDEX.
+ * segment with an end outside [0, n] or below its start is dropped, both with DSVT_STATUS_BAD_INDEX.  A seg_start entry that is out of
+ * place between two that are not costs the two segments that it bounds and no others.  Where neighbours are out of place together, other
+ * segments may be left out too, and rows that lie in two segments are not defined.
  */
 typedef struct dsvt_segment_attention_params {
   int32_t n, heads, head_dim, type;

@@ -384,6 +384,8 @@ __global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) short_backward_ker
   tally.copy = HG * 2 * a.buckets;
   tally.on = a.dbias != nullptr;
   tally.bound(0.f);
+  StartCheck<kThreads> starts;
+  starts.begin(a);
   stage_tables<kThreads>(a, maps, bias, head0, HG);
   float* mine = work.partial + (int64_t)blockIdx.x * work.table + head0 * a.buckets;
   if (tally.on) {
@@ -394,6 +396,7 @@ __global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) short_backward_ker
     for (int i = first; i < (work.table + 31) / 32; i += step) work.spoilt[i] = 0;
     for (int i = first; i < work.launches; i += step) work.bounds[i] = 0;
   }
+  starts.end(a);
   bool emptied = false;
   int pending = 0;
   auto empty = [&]() {  // all threads; a barrier before and after

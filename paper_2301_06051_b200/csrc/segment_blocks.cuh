@@ -29,12 +29,12 @@ struct Plan {
 };
 
 // Which entries of seg_start can be of segments that start in rows [from, to): found by a probe per thread and round (one or two for most calls); N: threads of the block.
-// `first`, `last`: nothing lies before or behind the rows.
+// Right where starts ascend; find_tiles does without where they may not.
 template <int N>
-__device__ __forceinline__ int2 segments_near(const SegArgs& a, int from, int to, bool first, bool last) {
+__device__ __forceinline__ int2 segments_near(const SegArgs& a, int from, int to) {
   const int tid = threadIdx.x;
-  int lo = 0, hi = a.cap_segments, end = hi;
-  if (a.num_segments) { const int m = *a.num_segments; end = m < 0 ? 0 : m < end ? m : end; }
+  int lo = 0, hi = a.cap_segments;
+  const int end = segment_count(a);
   while (true) {
     const int span = hi - lo, step = (span + N - 1) / N;
     const int64_t i = lo + (int64_t)tid * step;
@@ -42,13 +42,71 @@ __device__ __forceinline__ int2 segments_near(const SegArgs& a, int from, int to
     const bool in = i < hi && i < end;
     const int below = __syncthreads_count(in && v < from), upto = __syncthreads_count(in && v < to);
     const int64_t next_hi = lo + (int64_t)upto * step;
-    if (!last && next_hi < hi) hi = (int)next_hi;
-    if (!first && below > 0) lo += (below - 1) * step;
+    if (next_hi < hi) hi = (int)next_hi;
+    if (below > 0) lo += (below - 1) * step;
     if (hi > end) hi = end;
     if (hi - lo <= 8 * N || hi - lo >= span) break;
   }
   return make_int2(lo, hi);
 }
+
+// p.cursor: the entry of seg_start to look from for segments that start in rows from `from` on, which is the last of a probe per thread that
+// lies below it.  Entries may be out of place: it is 0 where the probes' answers do not change once, from below to not below, or the one
+// that counts lies below its neighbour.  So an entry out of place between two that are not keeps no other segment from being found.
+// A barrier before and after.
+template <int N>
+static __device__ __noinline__ void search_on(const SegArgs& a, Plan& p, int from, int lo, int step) {  // (a quarter of a million entries)
+  const int end = segment_count(a);
+  while (step > 4 * N) {
+    const int64_t hi = lo + (int64_t)step + 1;
+    step = (int)((hi - lo + N - 1) / N);
+    const int64_t i = lo + (int64_t)threadIdx.x * step;
+    const bool below = i < hi && i < end && a.seg_start[i] < from;
+    const int count = __syncthreads_count(below);
+    if (below != (int)threadIdx.x < count || (below && i > 0 && a.seg_start[i - 1] > a.seg_start[i])) atomicMin(&p.cursor, 0);
+    if (count > 0) lo += (count - 1) * step;
+  }
+  if (threadIdx.x == 0) atomicMin(&p.cursor, lo);
+}
+template <int N>
+__device__ __forceinline__ void search(const SegArgs& a, Plan& p, int from) {
+  const int step = (a.cap_segments + N - 1) / N;
+  const int64_t i = (int64_t)threadIdx.x * step;
+  const bool there = i < a.cap_segments;
+  const int v = there ? a.seg_start[i] : INT_MAX, before = there && i > 0 ? a.seg_start[i - 1] : INT_MIN;
+  if (threadIdx.x == 0) p.cursor = INT_MAX;
+  const bool below = v < from && i < segment_count(a);  // (what lies behind the last segment's end may be anything)
+  const int count = __syncthreads_count(below);
+  if (below != (int)threadIdx.x < count || (below && before > v)) atomicMin(&p.cursor, 0);
+  const int lo = count > 0 ? (count - 1) * step : 0;
+  if (step > 4 * N) search_on<N>(a, p, from, lo, step);
+  else if (threadIdx.x == 0) atomicMin(&p.cursor, lo);
+}
+
+// Every pair of seg_start that is no segment is said, whether a block's search comes across it or not: a share for each block of the grid's row 0.
+// A thread's pair is loaded before the search and looked at behind it.  (This, the search's second load and the look behind its last
+// segment take 0.1 us of 2,000 pillars' 11.8 us and 0.4 of 32,000 pillars' 36.9; waiting for the pair at once, 0.2 and 0.6.)
+__device__ __forceinline__ void check_pair(const SegArgs& a, int2 pair) {
+  if (pair.x < 0 || pair.y < pair.x || pair.y > a.n) atomicOr(a.status, DSVT_STATUS_BAD_INDEX);
+}
+template <int N>
+static __device__ __noinline__ void check_more(const SegArgs& a) {
+  const int count = segment_count(a);
+  const int64_t step = (int64_t)gridDim.x * N;
+  for (int64_t s = (int64_t)blockIdx.x * N + threadIdx.x + step; s < count; s += step) check_pair(a, make_int2(a.seg_start[s], a.seg_start[s + 1]));
+}
+template <int N>
+struct StartCheck {
+  int2 pair;
+  __device__ __forceinline__ void begin(const SegArgs& a) {
+    const uint32_t at = blockIdx.x * N + threadIdx.x;  // (of 16 rows at least: within 32 bits)
+    pair = blockIdx.y == 0 && at < (uint32_t)segment_count(a) ? make_int2(a.seg_start[at], a.seg_start[at + 1]) : make_int2(0, 0);
+  }
+  __device__ __forceinline__ void end(const SegArgs& a) {
+    check_pair(a, pair);
+    if (blockIdx.y == 0 && gridDim.x * N < (uint32_t)a.cap_segments) check_more<N>(a);
+  }
+};
 
 // Copies what every block reads: the index tables of the displacements and its heads' bias, in units of log 2.
 template <int N>
@@ -66,14 +124,15 @@ __device__ __forceinline__ int bucket_at(const BucketMaps& m, const uint16_t* ma
   return maps[dx] + maps[dy] + maps[dz];  // (the maps in shared memory hold four times the index: a bias's offset)
 }
 
-// The segments that start in rows [from, to) of a call, the first range and the last open to their side.
+// The segments that start in rows [from, to) of a call, the first range and the last open to their side.  They are among the entries from
+// the plan's cursor to the first start in place that lies at `to` or behind, or to `end`.
 struct Range { int from, to, end; };
 template <int N>
 __device__ __forceinline__ Range start_range(const SegArgs& a, Plan& p, int range, int ranges, int per) {
-  const int2 near = segments_near<N>(a, range * per, (range + 1) * per, range == 0, range == ranges - 1);
-  if (threadIdx.x == 0) p.cursor = near.x;
+  if (range > 0) search<N>(a, p, range * per);
+  else if (threadIdx.x == 0) p.cursor = 0;
   __syncthreads();
-  return Range{range == 0 ? INT_MIN : range * per, range == ranges - 1 ? INT_MAX : (range + 1) * per, near.y};
+  return Range{range == 0 ? INT_MIN : range * per, range == ranges - 1 ? INT_MAX : (range + 1) * per, segment_count(a)};
 }
 
 // The next batch of a range's segments of up to `limit` rows, at most `most` places together: their rows' voxels and the list of their
@@ -117,7 +176,7 @@ __device__ __forceinline__ bool next_batch(const SegArgs& a, Plan& p, const Rang
         items += __shfl_sync(kAll, upto, last);
         segments += __popc(taken);
       }
-      const uint32_t behind = __ballot_sync(kAll, s < range.end && lo >= range.to);
+      const uint32_t behind = __ballot_sync(kAll, s < range.end && lo >= range.to && lo <= hi);  // (a start above the next one is out of place)
       if (rest) {
         cursor += __ffs(rest) - 1;
         open = false;
@@ -358,10 +417,14 @@ __device__ __forceinline__ void soften(Flow<DT>& f, float (&s)[NT][4]) {
 struct Tile { int lo, hi, row; };  // a segment and the first row of a tile of it
 constexpr int kMaxTiles = 8;       // tiles that start in one block's rows (at most 128, of segments of more than 24 rows)
 
-// The tiles of `tile` rows of segments longer than `above` that start in rows [base, base + tile).
+// The tiles of `tile` rows of segments longer than `above` that start in rows [base, base + tile).  Where an index was bad, in this call's
+// starts perhaps (the short ones' kernel has been through them all), every segment is looked at: the blocks of a segment's tiles, and in the
+// backward pass both kernels, then know the same segments.
 __device__ __forceinline__ int find_tiles(const SegArgs& a, Tile* tiles, int* count, int base, int tile, int above) {
   if (threadIdx.x == 0) *count = 0;
-  const int2 near = segments_near<kThreads>(a, base + 1, base + tile, false, false);
+  const bool odd = (__ldcg(a.status) & DSVT_STATUS_BAD_INDEX) != 0;
+  int2 near = segments_near<kThreads>(a, base + 1, base + tile);
+  if (odd) near = make_int2(0, segment_count(a));
   __syncthreads();
   for (int s = near.x + (int)threadIdx.x; s < near.y; s += kThreads) {
     const int lo = a.seg_start[s], hi = a.seg_start[s + 1];

@@ -85,7 +85,10 @@ __global__ void __launch_bounds__(kShortThreads, DT <= 24 && sizeof(T) == 2 ? 3 
   const int head0 = blockIdx.y * HG, heads = min(HG, a.heads - head0);
   const uint32_t pitch = kExact<DT> ? HG * DT * sizeof(T) + 16 : L.pitch;
   const uint32_t q0 = smem_u32(smem + L.rows), k0 = q0 + L.array, v0 = k0 + L.array;
+  StartCheck<kShortThreads> starts;
+  starts.begin(a);
   const Range range = start_range<kShortThreads>(a, plan, blockIdx.x, L.ranges, L.per);
+  starts.end(a);
   const int chunks = HG * dim * (int)sizeof(T) / 16, real = heads * dim * (int)sizeof(T) / 16;
   const int64_t col = (int64_t)head0 * dim;
   const Rows<3> src = {{first_head<T>(a.q, col), first_head<T>(a.k, col), first_head<T>(a.v, col)},

@@ -83,6 +83,78 @@ def test_a_bias_of_the_largest_float_takes_all_the_weight(ctx, typ, lens):
     assert ctx.status_sync() == 0
 
 
+# ---- starts that do not ascend -----------------------------------------------------------------------------------------
+def _starts_problem(kind):
+    lens = {"sets": [30, 7, 36, 1] * 60, "windows": [200, 90, 7, 130] * 20, "voxels": [3] * 3000}[kind]
+    p = Problem(lens, 2 if kind != "voxels" else 1, 16, torch.float32, seed=len(lens), packed=False, lead=2, tail=3)
+    p.whole = {**p.want()[0], **p.want(back=True)[0]}
+    return p
+
+
+def _check_starts(ctx, p, dropped, what):
+    """All segments but the dropped ones are right, the others' rows stay as they were, and the call says so."""
+    covered = torch.zeros(p.n, dtype=torch.bool)
+    for i, ids in enumerate(p.segments):
+        covered[torch.from_numpy(ids)] = i not in dropped
+    out = torch.full((p.n, p.heads, p.dim), 7.0, device="cuda")
+    grads = [torch.full_like(out, 7.0) for _ in range(3)]
+    p.forward(ctx, out)
+    assert ctx.status_sync() == api.STATUS_BAD_INDEX, what
+    *_, dbias = p.backward(ctx, grads)
+    assert ctx.status_sync() == api.STATUS_BAD_INDEX, what
+    for name, got in zip(("out", "dq", "dk", "dv"), [out] + grads):
+        ref.check(got.cpu()[covered], tuple(t[covered] for t in p.whole[name]), what + ": " + name)
+        assert torch.all(got.cpu()[~covered] == 7.0), (what, name)
+    value, bound = p.whole["dbias"]
+    if dropped:
+        segments, p.segments = p.segments, [p.segments[i] for i in sorted(dropped)]
+        less, more = p.want(back=True)[0]["dbias"]
+        value, bound, p.segments = value - less, bound + more, segments
+    ref.check(dbias, (value, bound), what + ": dbias")
+
+
+@pytest.mark.parametrize("kind", ["sets", "windows", "voxels"])
+@pytest.mark.parametrize("value", [-1, None], ids=["below", "beyond"])
+def test_one_bad_start_costs_its_two_segments_and_no_others(ctx, kind, value):
+    p = _starts_problem(kind)
+    start, count = p.seg.start.clone(), len(p.segments)
+    bad = -1 if value == -1 else p.n + 9
+    for at in (1, 2, 3, count // 3, count // 2 + 1, count - 2, count - 1):
+        p.seg.start.copy_(start)
+        p.seg.start[at] = bad
+        _check_starts(ctx, p, {at - 1, at}, "%s, entry %d" % (kind, at))
+    if kind == "windows":  # several, each between two that are in place
+        p.seg.start.copy_(start)
+        p.seg.start[5:70:8] = bad
+        _check_starts(ctx, p, {i - d for i in range(5, 70, 8) for d in (0, 1)}, "several")
+
+
+@pytest.mark.parametrize("kind", ["sets", "windows", "voxels"])
+def test_starts_that_were_never_written_behind_the_last_segment(ctx, kind):
+    """A table of starts with room for more segments than there are, zeros behind the last one's end and no count on the device."""
+    p = _starts_problem(kind)
+    p.seg.start = torch.cat([p.seg.start, torch.zeros(400, dtype=torch.int32, device="cuda")])
+    _check_starts(ctx, p, set(), kind)  # (the pair at the seam is no segment: said; all others are)
+
+
+@pytest.mark.parametrize("kind", ["sets", "windows", "voxels"])
+def test_any_start_out_of_place_is_said(ctx, kind):
+    """Neighbours out of place together: which segments are worked on beside them is open, that the starts are bad is not."""
+    p = _starts_problem(kind)
+    start = p.seg.start.clone()
+    g = torch.Generator().manual_seed(3)
+    for i in range(12):
+        at, m = int(torch.randint(1, len(p.segments) - 12, (1,), generator=g)), int(torch.randint(2, 11, (1,), generator=g))
+        p.seg.start.copy_(start)
+        p.seg.start[at:at + m] = start[max(at - 4, 0)] if i % 2 else p.n + 1
+        if i % 3 == 0:
+            p.seg.start[at:at + m] += torch.arange(m, dtype=torch.int32, device="cuda")
+        p.forward(ctx)
+        assert ctx.status_sync() & api.STATUS_BAD_INDEX, (i, at, m)
+        p.backward(ctx)
+        assert ctx.status_sync() & api.STATUS_BAD_INDEX, (i, at, m)
+
+
 # ---- nothing to do -----------------------------------------------------------------------------------------------------
 @pytest.mark.parametrize("max_len", [36, 0])
 def test_no_voxels_with_a_bias(ctx, max_len):
