@@ -454,7 +454,8 @@ int dsvt_segment_attention(dsvt_ctx* ctx, const dsvt_segment_attention_params* p
  * [heads][buckets]; NULL to leave it out, and without a bias).  The forward pass saves nothing for it.  Rows of voxels in no segment
  * are left as they were; dbias is written in full (a value that is not finite makes its entry NaN).  The same inputs give the same bits.
  *
- * dbias adds up dS = P (dP - D), D = sum P dP, in whole multiples of at most 2^-33 times the call's largest max_j |P dP| + |D| max_j P.
+ * dbias adds up dS = P (dP - D), D = sum P dP, in whole multiples of at most 2^-33 times the call's largest max_j |P dP| + |D| max_j P
+ * (2^-145 where that is less).
  * The call works in the context's workspace, as partitions and layers do: calls of one context, captured ones among them, must not
  * overlap on the GPU.
  *

@@ -12,8 +12,8 @@
 // The bias's gradient adds up ds by bucket, a scatter.  It is held as integers, so that their order does not matter and the same
 // inputs give the same bits: v = (hi 2^-17 + lo 2^-35) limit with |hi|, |lo| <= 2^17, two words of shared memory to a bucket, which
 // take 16,000 values before they are emptied into floats (short: the block's own partial sums) or 64-bit integers in global memory
-// (long).  limit is a power of two that bounds |ds|, from the first pass: |p dp| + |p D| <= max_j |p dp| + |D| max_j p, and at most four
-// times that.  A value is off by 2^-36 of the limit.  Integer additions in shared memory are also the fast ones here: 1.4 ns a warp where
+// (long).  limit is a power of two, 2^-110 ... 2^128, that bounds |ds|, from the first pass: |p dp| + |p D| <= max_j |p dp| + |D| max_j p, and
+// at most four times that.  A value is off by 2^-36 of the limit.  Integer additions in shared memory are also the fast ones here: 1.4 ns a warp where
 // the addresses differ, fp32's 6 ns, 64-bit 11 ns.  Where they are the same they follow one another (8 lanes to an address: 5 ns), and
 // neighbouring keys and queries have the same displacements; so the four lanes that share a key add to tables of their own where there
 // is room, or two and two.
@@ -56,12 +56,12 @@ struct Tally {
   int* hist;           // [copies][heads][2][buckets]
   uint32_t* spoilt;    // bits [heads][buckets]
   int buckets, copies, copy;  // copy: entries of one
-  float limit, to_hi;  // to_hi = 2^kHiBits / limit
+  float limit, to_hi;  // to_hi = 2^kHiBits / limit, where a limit of 2^128 is held as the largest float
   bool on;
   __device__ __forceinline__ void bound(float b) {
     int e = (int)((__float_as_uint(b) >> 23) & 255) - 127 + 2;
-    e = min(max(e, -100), 126);
-    limit = __int_as_float((e + 127) << 23);
+    e = min(max(e, -110), 128);
+    limit = e < 128 ? __int_as_float((e + 127) << 23) : 3.402823466e38f;
     to_hi = __int_as_float((kHiBits - e + 127) << 23);
   }
   template <int N>
@@ -124,8 +124,9 @@ struct Tally {
 };
 
 // What the words stand for.
-__device__ __forceinline__ float tally_value(long long hi, long long lo, float limit) {
-  return (float)(((double)hi + (double)lo * (1.0 / (1 << kLoBits))) * (1.0 / (1 << kHiBits)) * (double)limit);
+__device__ __forceinline__ float tally_value(long long hi, long long lo, float to_hi) {
+  const double unit = __hiloint2double((1023 + 127 - (__float_as_int(to_hi) >> 23)) << 20, 0);  // 1 / to_hi
+  return (float)(((double)hi + (double)lo * (1.0 / (1 << kLoBits))) * unit);
 }
 
 // A tile's two rows of the first pass: maximum and sum as in Flow, D and the largest |p dp| before they are divided by the sum.
@@ -163,11 +164,11 @@ __device__ __forceinline__ void sum_rows(RowSums& f, float (&s)[NT][4], const fl
     f.l[r] = sum_of(l); f.d[r] = sum_of(d); f.most[r] = most;
   }
 }
-// Row r's maximum, 1 / sum and D, and the bound of its |ds| (0 where it is not finite: such values are counted apart).
+// Row r's maximum, 1 / sum and D, and the bound of its |ds| (0 where D is not finite: such a row's values are counted apart).
 __device__ __forceinline__ float3 row_stats(const RowSums& f, int r, float* bound) {
   const float inv = inverse(quad_sum(f.l[r])), D = quad_sum(f.d[r]) * inv;
   const float b = quad_max(f.most[r]) * inv + fabsf(D) * fminf(inv, 1.f);
-  *bound = b <= 3e38f ? b : 0.f;
+  *bound = isfinite(D) ? fminf(b, 3.402823466e38f) : 0.f;
   return make_float3(f.m[r] == -INFINITY ? 0.f : f.m[r], inv, D);
 }
 
@@ -403,7 +404,7 @@ __global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) short_backward_ker
     for (int i = threadIdx.x; i < heads * a.buckets; i += kThreads) {
       long long hi, lo;
       const bool spoilt = tally.take(i, hi, lo);
-      const float v = tally_value(hi, lo, tally.limit), sum = emptied ? mine[i] + v : v;
+      const float v = tally_value(hi, lo, tally.to_hi), sum = emptied ? mine[i] + v : v;
       mine[i] = spoilt ? NAN : sum;
     }
     emptied = true;
@@ -822,7 +823,7 @@ static __global__ void __launch_bounds__(kGradThreads) bias_grad_kernel(const Ba
   if (longer) {
     Tally t;
     t.bound(__uint_as_float(work.bounds[mine / buckets / work.at_once]));
-    s += tally_value((long long)work.total[mine], (long long)work.total[mine + work.table], t.limit);
+    s += tally_value((long long)work.total[mine], (long long)work.total[mine + work.table], t.to_hi);
     if (work.spoilt[mine >> 5] >> (mine & 31) & 1) s = NAN;
   }
   dbias[mine] = s;

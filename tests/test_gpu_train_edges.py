@@ -171,3 +171,55 @@ def test_no_voxels_with_a_bias(ctx, max_len):
     with pytest.raises(api.DsvtError):  # the tables are looked at all the same
         ctx.segment_attention(e, e, e, seg, bias=bad)
     assert ctx.status_sync() == 0
+
+
+# ---- the ends of float's range -----------------------------------------------------------------------------------------
+def _two_clusters(rest, near, dp, do):
+    """Voxels 0 and 1 attend to each other alone (`near`: the bias between them), the `rest` others among themselves; the rows' products
+    with v are dp for query 0 where d_out is `do`.  Returns the problem with everything but that zero."""
+    p = Problem([2 + rest], 1, 8, torch.float32, seed=31, ordered=False, packed=False, extent=(4, 4, 1), scale=0.0)
+    p.cells[:] = [100, 0, 0]
+    p.cells[0], p.cells[1] = [0, 0, 0], [1, 0, 0]
+    p.seg.coords.copy_(torch.from_numpy(np.concatenate([np.zeros((p.n, 1)), p.cells], 1).astype(np.int32)))
+    d = np.arange(7)
+    p.index = np.concatenate([7 * d, d, [0]]).astype(np.int32)  # a bucket per displacement
+    p.table = torch.zeros((1, 49))
+    p.table[0, [7 * 6 + 3, 3]] = -math.inf  # between the clusters, either way
+    p.table[0, [7 * 2 + 3, 7 * 4 + 3]] = near
+    p.rel = api.BucketBias(p.table.cuda(), p.extent, p.index)
+    for t in p.host:
+        t.zero_()
+    p.host[2][0, 0, 0], p.host[2][1, 0, 0] = dp
+    p.host[3][0, 0, 0] = do
+    p.q, p.k, p.v, p.do = (t.contiguous().cuda() for t in p.host)
+    return p
+
+
+@pytest.mark.parametrize("rest", [1, 140])
+@pytest.mark.parametrize("near,dp", [(0.0, (1.0, -1.0)), (-7.0, (1.0, 0.5)), (-7.0, (1.0, 0.25))])
+def test_bias_gradients_near_the_largest_float(ctx, rest, near, dp):
+    """dS of up to half the largest float; products and D so large that their bound passes it."""
+    p = _two_clusters(rest, near, dp, 3.2e38)
+    *_, dbias = p.backward(ctx)
+    want, _ = p.want(back=True)
+    assert float(want["dbias"][0].abs().max()) > 1e35
+    ref.check(dbias, want["dbias"], "dbias")
+    assert ctx.status_sync() == 0
+
+
+@pytest.mark.parametrize("lens", [[36, 20, 3, 36], [150, 36]])
+def test_bias_gradients_near_the_smallest_float(ctx, lens):
+    p = Problem(lens, 4, 24, torch.bfloat16, seed=32, packed=False)
+    p.host[3] = (p.host[3].double() * 2.0 ** -122).to(torch.bfloat16)
+    p.do = p.host[3].contiguous().cuda()
+    *_, dbias = p.backward(ctx)
+    value, bound = p.want(back=True)[0]["dbias"]
+    counts = torch.zeros(p.table.shape[1], dtype=torch.float64)
+    for ids in p.segments:
+        counts += torch.from_numpy(np.bincount(p.buckets(ids).reshape(-1), minlength=p.table.shape[1]))
+    # beside the bound of ordinary sizes: results of fp32 operations here are multiples of 2^-149, a dS comes from dim + length and some 16
+    # of them, and the header's multiples are of 2^-145
+    step = (24 + max(lens) + 16) * 2.0 ** -150 + 2.0 ** -146
+    ref.check(dbias, (value, bound + counts * step), "dbias")
+    # the products' bound is a loose one: without it, that many half steps to a dS of 2^-125 or so leave 1e-4 of sums of up to 1000
+    assert (dbias.double().cpu() - value).norm() <= 1e-4 * value.norm()
