@@ -310,11 +310,14 @@ int launch(dsvt_ctx* ctx, NormArgs<T> a, float* dg, float* db) {
   const int groups = threads / (BLOCK ? threads : a.lanes);
   int64_t blocks = dsvt_ceil_div(a.n, groups);
   // as many blocks as can be resident, each about the same number of rows
-  size_t smem = BACK ? 2 * (size_t)a.C * sizeof(float) : 0;
   constexpr int ring = Ring<V, VPL, (int)sizeof(T), BLOCK>::bytes(BACK ? 3 : 2);
-  if (smem < ring) smem = ring;
+  constexpr int sums = BACK ? 2 * (BLOCK ? kMaxC : kWide) * (int)sizeof(float) : 0, room = ring > sums ? ring : sums;
+  const int mine = BACK ? 2 * a.C * (int)sizeof(float) : 0, smem = mine > ring ? mine : ring;
+  if constexpr (room > 47 * 1024) {
+    const int rc = allow_smem<kernel>(ctx, room);
+    if (rc != DSVT_OK) return rc;
+  }
   int per_sm = 0;
-  if (smem > 47 * 1024) DSVT_CUDA_TRY(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
   DSVT_CUDA_TRY(ctx, cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, threads, smem));
   int64_t most = (int64_t)ctx->sm_count * (per_sm > 0 ? per_sm : 1);
   if (BACK && most > (int64_t)(4 * ctx->bm_words) / (2 * a.C)) most = (int64_t)(4 * ctx->bm_words) / (2 * a.C);  // (the workspace)

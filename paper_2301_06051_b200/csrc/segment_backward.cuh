@@ -865,7 +865,7 @@ int backward_of(dsvt_ctx* ctx, const SegArgs& a) {
   w.at_once = (int)(at_once < 1 ? 1 : at_once < a.heads ? at_once : a.heads);
   w.launches = (int)dsvt_ceil_div(a.heads, w.at_once);
   constexpr auto kernel = short_backward_kernel<T, DT>;
-  int rc = allow_smem<kernel>(ctx);
+  int rc = allow_smem<kernel>(ctx, kSmemMost);
   if (rc != DSVT_OK) return rc;
   launch_pdl(kernel, dim3((unsigned)stay, groups), dim3(kThreads), l.bytes, ctx->stream, a, l, sc, w);
   DSVT_LAUNCHED(ctx);
@@ -873,7 +873,7 @@ int backward_of(dsvt_ctx* ctx, const SegArgs& a) {
     const BackLongLayout lq = back_long_layout<T, DT>(a, false), lk = back_long_layout<T, DT>(a, true);
     constexpr auto by_queries = long_backward_kernel<T, DT, false>;
     constexpr auto by_keys = long_backward_kernel<T, DT, true>;
-    if ((rc = allow_smem<by_queries>(ctx)) != DSVT_OK || (rc = allow_smem<by_keys>(ctx)) != DSVT_OK) return rc;
+    if ((rc = allow_smem<by_queries>(ctx, kSmemMost)) != DSVT_OK || (rc = allow_smem<by_keys>(ctx, kSmemMost)) != DSVT_OK) return rc;
     for (int h = 0; h < a.heads; h += w.at_once) {
       w.head0 = h;
       w.head_end = h + w.at_once < a.heads ? h + w.at_once : a.heads;

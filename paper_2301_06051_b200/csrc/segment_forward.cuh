@@ -7,8 +7,6 @@
 // attending; warps of their own for the first three, over a ring of batches, came to the same time (30 us where this took 32), and four
 // blocks of 128 threads or two of 256 with two heads to a warp to more.
 #pragma once
-#include <atomic>
-
 #include "segment_blocks.cuh"
 
 namespace dsvt_train {
@@ -346,17 +344,6 @@ __global__ void __launch_bounds__(kThreads, LongShape<T, DT>::three ? 3 : DT <= 
 constexpr uint32_t kSmemHalf = 112 * 1024;  // two blocks
 constexpr uint32_t kSmemMost = 226 * 1024;  // (of 227 KB; the rest for what kernels declare themselves)
 
-// (once per kernel and device: the call costs more than a launch's share of it)
-template <auto kernel>
-static int allow_smem(dsvt_ctx* ctx) {
-  static std::atomic<uint64_t> done{0};
-  const uint64_t bit = (uint64_t)1 << (ctx->device & 63);
-  if (ctx->device < 64 && (done.load(std::memory_order_relaxed) & bit)) return DSVT_OK;
-  DSVT_CUDA_TRY(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemMost));
-  done.fetch_or(bit, std::memory_order_relaxed);
-  return DSVT_OK;
-}
-
 template <typename T, int DT>
 int forward_of(dsvt_ctx* ctx, const SegArgs& a) {
   int limit = a.max_len <= kShort ? a.max_len : 64;
@@ -366,7 +353,7 @@ int forward_of(dsvt_ctx* ctx, const SegArgs& a) {
   const int groups = (int)dsvt_ceil_div(a.heads, kHeads<T, DT>);
   set_ranges(l, a.n, (int)dsvt_ceil_div((DT <= 24 && sizeof(T) == 2 ? 3 : 2) * ctx->sm_count, groups), limit < a.max_len ? 128 : 1 << 20);
   constexpr auto kernel = short_forward_kernel<T, DT>;
-  int rc = allow_smem<kernel>(ctx);
+  int rc = allow_smem<kernel>(ctx, kSmemMost);
   if (rc != DSVT_OK) return rc;
   launch_pdl(kernel, dim3((unsigned)l.ranges, (unsigned)groups), dim3(kShortThreads), l.bytes, ctx->stream, a, l, sc);
   DSVT_LAUNCHED(ctx);
@@ -374,7 +361,7 @@ int forward_of(dsvt_ctx* ctx, const SegArgs& a) {
   using S = LongShape<T, DT>;
   const LongLayout g = long_layout<T, DT>(a, 1, 2, 0);
   constexpr auto longer = long_forward_kernel<T, DT>;
-  rc = allow_smem<longer>(ctx);
+  rc = allow_smem<longer>(ctx, kSmemMost);
   if (rc != DSVT_OK) return rc;
   launch_pdl(longer, dim3((unsigned)dsvt_ceil_div(a.n, S::rows), (unsigned)dsvt_ceil_div(a.heads, S::HG)), dim3(kThreads), g.bytes, ctx->stream, a, g, sc, limit);
   DSVT_LAUNCHED(ctx);

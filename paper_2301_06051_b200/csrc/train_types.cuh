@@ -2,6 +2,8 @@
 #pragma once
 #include <cuda_fp16.h>
 
+#include <atomic>
+
 #include "dsvt_common.cuh"
 
 namespace dsvt_train {
@@ -63,5 +65,17 @@ struct DeviceGuard {
   }
   ~DeviceGuard() { if (before >= 0) cudaSetDevice(before); }
 };
+
+// Lets a kernel have `bytes` of shared memory.  That is the process's state and not a call's: always the same number for a kernel, so that calls
+// of several threads never take from one another.  (Once per kernel and device: the call costs more than a launch's share of it.)
+template <auto kernel>
+static int allow_smem(dsvt_ctx* ctx, int bytes) {
+  static std::atomic<uint64_t> done{0};
+  const uint64_t bit = (uint64_t)1 << (ctx->device & 63);
+  if (ctx->device < 64 && (done.load(std::memory_order_relaxed) & bit)) return DSVT_OK;
+  DSVT_CUDA_TRY(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
+  done.fetch_or(bit, std::memory_order_relaxed);
+  return DSVT_OK;
+}
 
 }  // namespace dsvt_train

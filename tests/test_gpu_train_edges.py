@@ -223,3 +223,35 @@ def test_bias_gradients_near_the_smallest_float(ctx, lens):
     ref.check(dbias, (value, bound + counts * step), "dbias")
     # the products' bound is a loose one: without it, that many half steps to a dS of 2^-125 or so leave 1e-4 of sums of up to 1000
     assert (dbias.double().cpu() - value).norm() <= 1e-4 * value.norm()
+
+
+# ---- streams and threads -----------------------------------------------------------------------------------------------
+def test_layer_norms_of_two_threads_at_once():
+    """Rows of 8192 and of 6144 channels go through one kernel, whose room in shared memory is the process's."""
+    widths, failed, go = (8192, 6144), [], threading.Barrier(2)
+    own = [api.Context(64, 1, 256, stream=torch.cuda.Stream()) for _ in widths]
+    xs = [torch.randn((37, C), device="cuda") for C in widths]
+    outs = [[torch.empty_like(x), torch.empty(x.shape[1], device="cuda"), torch.empty(x.shape[1], device="cuda")] for x in xs]
+    torch.cuda.synchronize()
+
+    def work(i):
+        at = [t.data_ptr() for t in outs[i]]
+        call = (own[i]._h, 0, xs[i].data_ptr(), None, xs[i].data_ptr(), 37, widths[i], None, 1e-5, *at)
+        go.wait()
+        for _ in range(30000):
+            rc = own[i].lib.dsvt_layer_norm_backward(*call)
+            if rc:
+                failed.append((widths[i], rc, own[i].lib.dsvt_last_cuda_error(own[i]._h)))
+                return
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    [t.start() for t in threads]
+    [t.join() for t in threads]
+    torch.cuda.synchronize()
+    assert not failed, failed
+    for i, x in enumerate(xs):
+        one = torch.ones(x.shape[1], dtype=torch.float64)
+        want = ref.layer_norm(x.double().cpu(), None, one, 0 * one, 1e-5, x.double().cpu())
+        for name, got in zip(("dx", "dg", "db"), outs[i]):
+            ref.check(got, want[name], name)
+        own[i].close()
