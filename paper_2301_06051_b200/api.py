@@ -313,7 +313,11 @@ def partition_noalloc(coords: torch.Tensor, batch: int, grid, window, set_size: 
 
 
 class Context:
-    """Owns a dsvt_ctx bound to the current torch CUDA stream of `device`."""
+    """Owns a dsvt_ctx bound to the current torch CUDA stream of `device`, or to `stream`.
+
+    Calls run on the context's stream, whichever is current: what they read has to be there for it, and who reads their results on
+    another stream waits for it first (Stream.wait_stream).  Results that a call allocates belong to the context's stream, and the
+    stream that is current at the call may use them too until they are dropped."""
 
     def __init__(self, max_voxels: int, max_windows: int, max_channels: int = 256, device: int = 0,
                  stream: Optional[torch.cuda.Stream] = None):
@@ -323,6 +327,7 @@ class Context:
         self.device = torch.device("cuda", device)
         self.stream = stream if stream is not None else torch.cuda.current_stream(self.device)
         self.limits = (int(max_voxels), int(max_windows), int(max_channels))
+        self._raw_stream, self._index, self._current = self.stream.cuda_stream, device, torch._C._cuda_getCurrentRawStream
         self._h = C.c_void_p()
         rc = self.lib.dsvt_create(C.byref(self._h), device, C.c_void_p(self.stream.cuda_stream), int(max_voxels),
                                   int(max_windows), int(max_channels))
@@ -344,6 +349,20 @@ class Context:
             self.close()
         except Exception:
             pass
+
+    def _new(self, shape, dtype=torch.float32, fill=torch.empty) -> torch.Tensor:
+        """Memory for a result.  From the context's stream: the current stream may still read what it gave back, and may hand out at once
+        what is dropped, while this call's kernels have yet to write."""
+        if self._current(self._index) == self._raw_stream:
+            return fill(shape, dtype=dtype, device=self.device)
+        with torch.cuda.stream(self.stream):
+            t = fill(shape, dtype=dtype, device=self.device)
+        t.record_stream(torch.cuda.current_stream(self.device))
+        return t
+
+    def _like(self, t: torch.Tensor) -> torch.Tensor:
+        """_new for a contiguous tensor's shape and type (2 us of host time less)."""
+        return torch.empty_like(t) if self._current(self._index) == self._raw_stream else self._new(t.shape, t.dtype)
 
     def _check(self, rc: int, where: str):
         if rc != OK:
@@ -370,16 +389,14 @@ class Context:
         n = int(coords.shape[0])
         if out is None:
             cap = int(cap_sets) if cap_sets is not None else max(n, 1)
-            dev = self.device
-            out = SetTable(torch.empty((cap, set_size), dtype=torch.int32, device=dev),
-                           torch.zeros(1, dtype=torch.int32, device=dev),
-                           torch.empty(4 * cap + 4, dtype=torch.int32, device=dev), cap, set_size)
+            out = SetTable(self._new((cap, set_size), torch.int32), self._new(1, torch.int32, torch.zeros),
+                           self._new(4 * cap + 4, torch.int32), cap, set_size)
             if extras:
                 nw = int(batch) * (-(-grid[0] // window[0])) * (-(-grid[1] // window[1])) * (-(-grid[2] // window[2]))
-                out.perm = torch.empty(max(n, 1), dtype=torch.int32, device=dev)
-                out.win_start = torch.empty(nw + 1, dtype=torch.int32, device=dev)
-                out.win_count = torch.empty(nw, dtype=torch.int32, device=dev)
-                out.win_setoff = torch.empty(nw + 1, dtype=torch.int32, device=dev)
+                out.perm = self._new(max(n, 1), torch.int32)
+                out.win_start = self._new(nw + 1, torch.int32)
+                out.win_count = self._new(nw, torch.int32)
+                out.win_setoff = self._new(nw + 1, torch.int32)
         rc = self.lib.dsvt_partition(self._h, _ptr(coords), n, int(batch), _i3(grid), _i3(window), int(set_size),
                                      int(axis), _ptr(out.set_table), out.cap_sets, _ptr(out.num_sets),
                                      _ptr(out.set_rowoff), _ptr(out.perm), _ptr(out.win_start), _ptr(out.win_count),
@@ -396,10 +413,8 @@ class Context:
         n = int(coords.shape[0])
         if out is None:
             cap = int(cap_sets) if cap_sets is not None else max(n, 1)
-            dev = self.device
-            out = tuple(SetTable(torch.empty((cap, set_size), dtype=torch.int32, device=dev),
-                                 torch.zeros(1, dtype=torch.int32, device=dev),
-                                 torch.empty(4 * cap + 4, dtype=torch.int32, device=dev), cap, set_size)
+            out = tuple(SetTable(self._new((cap, set_size), torch.int32), self._new(1, torch.int32, torch.zeros),
+                                 self._new(4 * cap + 4, torch.int32), cap, set_size)
                         for _ in range(2))
         t0, t1 = out
         assert t0.cap_sets == t1.cap_sets and t0.set_size == t1.set_size == set_size
@@ -511,7 +526,7 @@ class Context:
         one projection's output.  Without `out` the rows of voxels in no segment are not defined."""
         p = self._segment_params(q, k, v, seg, bias, scale, cap)
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            out = self._new(q.shape, q.dtype)
         rc = self.lib.dsvt_segment_attention(self._h, C.byref(p), *_rows(out, q.shape, q.dtype))
         self._check(rc, "dsvt_segment_attention")
         return out
@@ -523,10 +538,10 @@ class Context:
         be slices of one tensor."""
         p = self._segment_params(q, k, v, seg, bias, scale, cap)
         if out is None:
-            out = tuple(torch.empty(q.shape, dtype=q.dtype, device=q.device) for _ in range(3))
+            out = tuple(self._new(q.shape, q.dtype) for _ in range(3))
         dq, dk, dv = out
         if bias is not None and dbias is None:
-            dbias = torch.empty_like(bias.table)
+            dbias = self._like(bias.table)
         if dbias is not None and (bias is None or dbias.shape != bias.table.shape or dbias.dtype != torch.float32):
             raise ValueError("dbias is a float32 tensor of the bias table's shape")
         shape, dtype = q.shape, q.dtype
@@ -541,7 +556,7 @@ class Context:
         """LayerNorm over the last dimension of x + residual ([n, C]); g and b float32, or None for ones and zeros."""
         n, Cc = x.shape
         if out is None:
-            out = torch.empty_like(x)
+            out = self._like(x)
         rc = self.lib.dsvt_layer_norm(self._h, _type(x), _ptr(x), _same(residual, x), n, Cc, _float(g, Cc), _float(b, Cc), eps,
                                       _same(out, x))
         self._check(rc, "dsvt_layer_norm")
@@ -553,11 +568,11 @@ class Context:
         """(dx, dg, db) of layer_norm(x, g, b, residual); the residual's gradient is dx."""
         n, Cc = x.shape
         if out is None:
-            out = torch.empty_like(x)
+            out = self._like(x)
         if dg is None:
-            dg = torch.empty(Cc, dtype=torch.float32, device=x.device)
+            dg = self._new(Cc)
         if db is None:
-            db = torch.empty(Cc, dtype=torch.float32, device=x.device)
+            db = self._new(Cc)
         rc = self.lib.dsvt_layer_norm_backward(self._h, _type(x), _ptr(x), _same(residual, x), _same(dy, x), n, Cc, _float(g, Cc),
                                                eps, _same(out, x), _float(dg, Cc), _float(db, Cc))
         self._check(rc, "dsvt_layer_norm_backward")
@@ -571,7 +586,7 @@ class Context:
         X, Y, Z = (int(v) for v in grid)
         shape = (batch, Y, X, Cc * Z) if channels_last else (batch, Cc * Z, Y, X)
         if out is None:
-            out = torch.empty(shape, dtype=torch.float32, device=self.device)
+            out = self._new(shape)
         assert tuple(out.shape) == shape and out.dtype == torch.float32
         rc = self.lib.dsvt_bev_scatter(self._h, _ptr(coords), _ptr(feats), n, Cc, int(batch), _i3(grid),
                                        1 if channels_last else 0, _ptr(out))
@@ -586,12 +601,10 @@ class Context:
         int32): the input's voxel count where it lives on the device (dsvt_pool_counted)."""
         n, Cc = int(feats.shape[0]), int(feats.shape[1])
         cap = int(cap_m) if cap_m is not None else max(n, 1)
-        dev = self.device
-        oc = torch.empty((cap, 4), dtype=torch.int32, device=dev)
-        of = torch.empty((cap, Cc), dtype=torch.float32, device=dev)
-        num = torch.zeros(1, dtype=torch.int32, device=dev)
-        reg = torch.empty(max(n, 1), dtype=torch.int32, device=dev) if extras else None
-        slot = torch.empty(max(n, 1), dtype=torch.int32, device=dev) if extras else None
+        oc, of = self._new((cap, 4), torch.int32), self._new((cap, Cc))
+        num = self._new(1, torch.int32, torch.zeros)
+        reg = self._new(max(n, 1), torch.int32) if extras else None
+        slot = self._new(max(n, 1), torch.int32) if extras else None
         tail = (Cc, int(batch), _i3(grid), _i3(pool_shape), _ptr(w["W_q"]), _ptr(w["W_k"]), _ptr(w["W_v"]),
                 _ptr(w["W_o"]), _ptr(w.get("b_q")), _ptr(w.get("b_k")), _ptr(w.get("b_v")), _ptr(w.get("b_o")),
                 _ptr(w.get("slot_pe")), int(w["heads"]), int(mask_empty), int(w["precision"]), _ptr(oc), _ptr(of), cap,

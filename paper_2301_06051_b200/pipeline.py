@@ -305,7 +305,7 @@ class StagedBackbone:
         """Returns (coords, feats) of the last stage.  on_step(tag), if given, is called after every call group."""
         feats, num = x, None  # num: the current stage's voxel count on the device (None: all of coords)
         for i, stage in enumerate(self.stages):
-            y = torch.empty_like(feats)
+            y = self.ctx._new(feats.shape)
             stage.partition(coords, n_dev=num)
             if on_step:
                 on_step("s%d_partition" % i)

@@ -226,6 +226,71 @@ def test_bias_gradients_near_the_smallest_float(ctx, lens):
 
 
 # ---- streams and threads -----------------------------------------------------------------------------------------------
+def _calls(own):
+    """Calls that make their own results, by name: each returns tensors."""
+    p = Problem([36, 20, 200, 1, 50], 8, 24, torch.bfloat16, seed=8, packed=False)
+    x = torch.randn((p.n, 192), device="cuda")
+    cells = torch.randperm(900, generator=torch.Generator().manual_seed(1))[:300]
+    coords = torch.stack([torch.zeros_like(cells), cells // 30, cells % 30, torch.zeros_like(cells)], 1).to(torch.int32).cuda()
+    feats = torch.randn((300, 64), device="cuda")
+    sets = lambda t: [t.set_table, t.set_rowoff, t.num_sets]
+    return {
+        "segment_attention": lambda: [p.forward(own)],
+        "segment_attention_backward": lambda: list(p.backward(own)),
+        "layer_norm": lambda: [own.layer_norm(x, None, None)],
+        "layer_norm_backward": lambda: list(own.layer_norm_backward(x, x, None)),
+        "partition": lambda: sets(own.partition(coords, 1, (30, 30, 1), (12, 12, 1), 16, 0)),
+        "partition_rotated": lambda: [t for s in own.partition_rotated(coords, 1, (30, 30, 1), (12, 12, 1), 16) for t in sets(s)],
+        "bev_scatter": lambda: [own.bev_scatter(coords, feats, 1, (30, 30, 1))],
+    }
+
+
+CALLS = ["segment_attention", "segment_attention_backward", "layer_norm", "layer_norm_backward", "partition", "partition_rotated",
+         "bev_scatter"]
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_a_result_dropped_while_the_contexts_stream_is_busy(name):
+    """Its memory may not go to the current stream's next tensor while the context's stream has still to write it."""
+    own = api.Context(2000, 64, 256, stream=torch.cuda.Stream())
+    call = _calls(own)[name]
+    torch.cuda.synchronize()
+    call()  # (kernels loaded)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(own.stream):
+        torch.cuda._sleep(200_000_000)
+    sizes = [(t.shape, t.dtype) for t in call()]
+    mine = [torch.full(shape, 3, dtype=dtype, device="cuda") for shape, dtype in sizes for _ in range(2)]
+    assert not own.stream.query()  # the kernels are still to come
+    torch.cuda.synchronize()
+    assert all(torch.all(t == 3) for t in mine)
+    assert own.status_sync() == 0
+    own.close()
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_a_result_in_memory_that_the_current_stream_still_reads(name):
+    own = api.Context(2000, 64, 256, stream=torch.cuda.Stream())
+    call = _calls(own)[name]
+    sizes = [(t.shape, t.dtype) for t in call()]
+    torch.cuda.synchronize()
+    old = [torch.full(shape, 3, dtype=dtype, device="cuda") for shape, dtype in sizes for _ in range(2)]
+    torch.cuda.synchronize()
+    torch.cuda._sleep(200_000_000)
+    read = [t.clone() for t in old]
+    del old
+    got = call()
+    own.stream.synchronize()
+    assert not torch.cuda.current_stream().query()  # the reads are still to come
+    torch.cuda.synchronize()
+    assert all(torch.all(t == 3) for t in read)
+    again = call()
+    own.stream.synchronize()
+    if name != "partition" and name != "partition_rotated":  # (tables have rows that no set fills)
+        assert all(torch.equal(a, b) for a, b in zip(got, again) if a is not None)
+    own.close()
+
+
 def test_layer_norms_of_two_threads_at_once():
     """Rows of 8192 and of 6144 channels go through one kernel, whose room in shared memory is the process's."""
     widths, failed, go = (8192, 6144), [], threading.Barrier(2)
