@@ -399,6 +399,8 @@ int dsvt_bev_scatter(dsvt_ctx* ctx, const int32_t* coords, const float* feats, i
  *       -(L - 1) ... L - 1 (W, H), (L, W, H) = extent
  *   out[i] = sum over j of softmax_j(s) v[j]
  *
+ * A cap is finite, in units of log 2 (cap log2(e)) too, and large enough that scale / cap is: DSVT_ERR_INVALID_ARG otherwise.
+ *
  * A bias entry of -inf masks its pairs, in a row with others one of the lowest float does too; a row whose scores are all
  * -inf gives zeros (and gets and passes on no gradient), one whose scores are all the lowest float equal weights.  (Finite
  * entries beyond FLT_MAX / log2(e) in magnitude count as the lowest or the largest float.)  A row with a score of NaN or +inf is

@@ -13,6 +13,8 @@ bool bad_rows(const void* p, int64_t ld, int64_t width, int size) {
 int check(const dsvt_ctx* ctx, const dsvt_segment_attention_params* p, SegArgs* a) {
   if (!ctx || !p || p->n < 0 || p->heads < 1 || p->head_dim < 1 || !type_known(p->type)) return DSVT_ERR_INVALID_ARG;
   if (p->cap_segments < 0 || p->max_len < (p->n > 0 ? 1 : 0) || !(p->cap >= 0.f) || isinf(p->cap)) return DSVT_ERR_INVALID_ARG;
+  // (a cap by which scale cannot be divided, or that is infinite in units of log 2, would make NaN of a score of zero)
+  if (p->cap > 0.f && (isinf(p->scale / p->cap) || isinf(p->cap * kLog2e))) return DSVT_ERR_INVALID_ARG;
   if (p->head_dim % 8 != 0 || p->head_dim > kMaxDim || p->heads > kMaxHeads) return DSVT_ERR_UNSUPPORTED;
   if (p->n > ctx->max_voxels) return DSVT_ERR_CAPACITY;
   const int64_t width = (int64_t)p->heads * p->head_dim;

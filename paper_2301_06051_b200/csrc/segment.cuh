@@ -6,6 +6,7 @@
 
 namespace dsvt_train {
 
+constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kMaxExtent = 128, kMaxBuckets = 1024, kMaxDim = 128, kMaxHeads = 65535;
 constexpr int64_t kMaxBiasTable = 1 << 18;  // entries of a bias whose gradient is asked for: what the workspace has room for
 

@@ -22,7 +22,6 @@
 namespace dsvt_train {
 
 constexpr unsigned kAll = 0xffffffffu;
-constexpr float kLog2e = 1.4426950408889634f;
 
 using dsvt_tc::ex2_approx;
 using dsvt_tc::smem_u32;

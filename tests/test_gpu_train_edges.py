@@ -225,6 +225,22 @@ def test_bias_gradients_near_the_smallest_float(ctx, lens):
     assert (dbias.double().cpu() - value).norm() <= 1e-4 * value.norm()
 
 
+def test_a_cap_beyond_the_arithmetic_is_refused(ctx):
+    p = Problem([20, 5], 2, 16, torch.float32, seed=2)
+    for cap in (1e-44, 1e-40, 3e38):
+        p.cap = cap
+        with pytest.raises(api.DsvtError):
+            p.forward(ctx)
+        with pytest.raises(api.DsvtError):
+            p.backward(ctx)
+    for cap in (1e-30, 1e30):  # almost no score at all, and none that is capped
+        p.cap = cap
+        got = p.forward(ctx)
+        want, covered = p.want()
+        ref.check(got, want["out"], "cap %g" % cap)
+    assert ctx.status_sync() == 0
+
+
 # ---- streams and threads -----------------------------------------------------------------------------------------------
 def _calls(own):
     """Calls that make their own results, by name: each returns tensors."""
