@@ -135,10 +135,17 @@ def _type(t: torch.Tensor) -> int:
     return TYPES[t.dtype]
 
 
-def _rows(t: torch.Tensor, shape, dtype):
+def _at(t: torch.Tensor, index: int):
+    """Refuses what is not on device `index`, the context's: a kernel that reads another GPU's memory, or the host's, may fault."""
+    if t.get_device() != index:
+        raise ValueError("tensors on the context's device, cuda:%d" % index)
+
+
+def _rows(t: torch.Tensor, shape, dtype, index: int):
     """Pointer and row stride of rows [n, heads, head_dim] whose heads lie one after the other."""
-    if t.shape != shape or t.dtype is not dtype or not t.is_cuda:
-        raise ValueError("rows of one shape and type, on the device")
+    if t.shape != shape or t.dtype is not dtype:
+        raise ValueError("rows of one shape and type")
+    _at(t, index)
     row, head, one = t.stride()
     n, heads, dim = shape
     if (one != 1 and dim > 1) or (head != dim and heads > 1):
@@ -146,23 +153,30 @@ def _rows(t: torch.Tensor, shape, dtype):
     return t.data_ptr(), row if n > 1 else heads * dim
 
 
-def _int32(t: Optional[torch.Tensor], shape=None):
+def _int32(t: Optional[torch.Tensor], index: int, shape=None):
     if t is None:
         return None
     if t.dtype != torch.int32 or (shape is not None and tuple(t.shape) != shape):
         raise ValueError("an int32 tensor%s" % (" of shape %s" % (shape,) if shape else ""))
+    _at(t, index)
     return _ptr(t)
 
 
-def _float(t: Optional[torch.Tensor], size: int):
-    if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != (size,)):
+def _float(t: Optional[torch.Tensor], size: int, index: int):
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or tuple(t.shape) != (size,):
         raise ValueError("a float32 tensor of %d entries" % size)
+    _at(t, index)
     return _ptr(t)
 
 
-def _same(t: Optional[torch.Tensor], like: torch.Tensor):
-    if t is not None and (t.shape != like.shape or t.dtype != like.dtype):
+def _same(t: Optional[torch.Tensor], like: torch.Tensor, index: int):
+    if t is None:
+        return None
+    if t.shape != like.shape or t.dtype != like.dtype:
         raise ValueError("rows of one shape and type")
+    _at(t, index)
     return _ptr(t)
 
 
@@ -506,16 +520,18 @@ class Context:
         shape, dtype = q.shape, q.dtype
         n, heads, dim = shape
         kind = _type(q)
-        (qp, ld_q), (kp, ld_k), (vp, ld_v) = _rows(q, shape, dtype), _rows(k, shape, dtype), _rows(v, shape, dtype)
-        p = SegmentAttentionParams(n, heads, dim, kind, qp, kp, vp, ld_q, ld_k, ld_v, _int32(seg.order, (n,)), _int32(seg.start),
-                                   _int32(seg.num), seg.start.numel() - 1, seg.max_len, dim ** -0.5 if scale is None else scale, cap)
+        at = self._index
+        (qp, ld_q), (kp, ld_k), (vp, ld_v) = _rows(q, shape, dtype, at), _rows(k, shape, dtype, at), _rows(v, shape, dtype, at)
+        p = SegmentAttentionParams(n, heads, dim, kind, qp, kp, vp, ld_q, ld_k, ld_v, _int32(seg.order, at, (n,)), _int32(seg.start, at),
+                                   _int32(seg.num, at), seg.start.numel() - 1, seg.max_len, dim ** -0.5 if scale is None else scale, cap)
         if bias is not None:
             table = bias.table
             if table.shape[0] != heads:
                 raise ValueError("a bias for %d heads, and %d heads" % (table.shape[0], heads))
             if seg.coords is None:
                 raise ValueError("a relative position bias needs the segments' coords")
-            p.bias, p.buckets, p.coords, p.bucket_of, p.extent = (_ptr(table), table.shape[1], _int32(seg.coords, (n, 4)),
+            _at(table, at)
+            p.bias, p.buckets, p.coords, p.bucket_of, p.extent = (_ptr(table), table.shape[1], _int32(seg.coords, at, (n, 4)),
                                                                   bias._index_at, bias._extent)
         return p
 
@@ -527,7 +543,7 @@ class Context:
         p = self._segment_params(q, k, v, seg, bias, scale, cap)
         if out is None:
             out = self._new(q.shape, q.dtype)
-        rc = self.lib.dsvt_segment_attention(self._h, C.byref(p), *_rows(out, q.shape, q.dtype))
+        rc = self.lib.dsvt_segment_attention(self._h, C.byref(p), *_rows(out, q.shape, q.dtype, self._index))
         self._check(rc, "dsvt_segment_attention")
         return out
 
@@ -544,9 +560,11 @@ class Context:
             dbias = self._like(bias.table)
         if dbias is not None and (bias is None or dbias.shape != bias.table.shape or dbias.dtype != torch.float32):
             raise ValueError("dbias is a float32 tensor of the bias table's shape")
-        shape, dtype = q.shape, q.dtype
-        rc = self.lib.dsvt_segment_attention_backward(self._h, C.byref(p), *_rows(d_out, shape, dtype), *_rows(dq, shape, dtype),
-                                                      *_rows(dk, shape, dtype), *_rows(dv, shape, dtype), _ptr(dbias))
+        if dbias is not None:
+            _at(dbias, self._index)
+        like = (q.shape, q.dtype, self._index)
+        rc = self.lib.dsvt_segment_attention_backward(self._h, C.byref(p), *_rows(d_out, *like), *_rows(dq, *like),
+                                                      *_rows(dk, *like), *_rows(dv, *like), _ptr(dbias))
         self._check(rc, "dsvt_segment_attention_backward")
         return dq, dk, dv, dbias
 
@@ -554,11 +572,12 @@ class Context:
     def layer_norm(self, x: torch.Tensor, g: Optional[torch.Tensor], b: Optional[torch.Tensor],
                    residual: Optional[torch.Tensor] = None, eps: float = 1e-5, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """LayerNorm over the last dimension of x + residual ([n, C]); g and b float32, or None for ones and zeros."""
-        n, Cc = x.shape
+        (n, Cc), at = x.shape, self._index
+        _at(x, at)
         if out is None:
             out = self._like(x)
-        rc = self.lib.dsvt_layer_norm(self._h, _type(x), _ptr(x), _same(residual, x), n, Cc, _float(g, Cc), _float(b, Cc), eps,
-                                      _same(out, x))
+        rc = self.lib.dsvt_layer_norm(self._h, _type(x), _ptr(x), _same(residual, x, at), n, Cc, _float(g, Cc, at), _float(b, Cc, at),
+                                      eps, _same(out, x, at))
         self._check(rc, "dsvt_layer_norm")
         return out
 
@@ -566,15 +585,16 @@ class Context:
                             residual: Optional[torch.Tensor] = None, eps: float = 1e-5, out: Optional[torch.Tensor] = None,
                             dg: Optional[torch.Tensor] = None, db: Optional[torch.Tensor] = None):
         """(dx, dg, db) of layer_norm(x, g, b, residual); the residual's gradient is dx."""
-        n, Cc = x.shape
+        (n, Cc), at = x.shape, self._index
+        _at(x, at)
         if out is None:
             out = self._like(x)
         if dg is None:
             dg = self._new(Cc)
         if db is None:
             db = self._new(Cc)
-        rc = self.lib.dsvt_layer_norm_backward(self._h, _type(x), _ptr(x), _same(residual, x), _same(dy, x), n, Cc, _float(g, Cc),
-                                               eps, _same(out, x), _float(dg, Cc), _float(db, Cc))
+        rc = self.lib.dsvt_layer_norm_backward(self._h, _type(x), _ptr(x), _same(residual, x, at), _same(dy, x, at), n, Cc,
+                                               _float(g, Cc, at), eps, _same(out, x, at), _float(dg, Cc, at), _float(db, Cc, at))
         self._check(rc, "dsvt_layer_norm_backward")
         return out, dg, db
 
