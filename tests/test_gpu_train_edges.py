@@ -336,3 +336,60 @@ def test_layer_norms_of_two_threads_at_once():
         for name, got in zip(("dx", "dg", "db"), outs[i]):
             ref.check(got, want[name], name)
         own[i].close()
+
+
+# ---- between layers ----------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("C,hidden", [(192, 384), (128, 256)])
+def test_calls_between_fp32_layers(C, hidden):
+    """fp32 layers keep their weights' parts and intermediate rows where the backward passes keep their sums; kernels overlap their
+    neighbours' tails.  Together without a wait: the same bits as alone."""
+    n = 3000
+    case = di.random_case(C, n, (60, 60, 1), (12, 12, 1), 36, C, 8, hidden, layernorm=True)
+    own = api.Context(n, 25, C)
+    coords, x = dev(case["coords"]), dev(case["feats"])
+    table = own.partition(coords, 1, case["grid"], case["window"], 36, 0)
+    w = api.device_weights(case["blocks"][0][0], api.FP32, own.device)
+    p = Problem([36, 20, 200, 1, 50] * 5, 8, 24, torch.bfloat16, seed=8)
+    dy = torch.randn((n, C), device="cuda")
+    layer = lambda to: own.layer(x, table, w, to, coords=coords)
+    chain = lambda to: own.layers(x, [table, table], [w, w], to, coords=coords)
+    alone = []
+    for f in (layer, chain):
+        y = torch.empty_like(x)
+        f(y)
+        torch.cuda.synchronize()
+        alone.append(y)
+    grads = p.backward(own)
+    torch.cuda.synchronize()
+    norm = own.layer_norm_backward(x, dy, None)
+    torch.cuda.synchronize()
+    for order in ("lbn", "bln", "cbncb", "nlbcnl", "bcb", "ncn"):
+        got = []
+        for _ in range(4):
+            for c in order:
+                if c in "lc":
+                    y = torch.full_like(x, 5.0)
+                    (layer if c == "l" else chain)(y)
+                    got.append(((y,), (alone["lc".index(c)],)))
+                elif c == "b":
+                    got.append((p.backward(own), grads))
+                else:
+                    got.append((own.layer_norm_backward(x, dy, None), norm))
+        torch.cuda.synchronize()
+        for have, want in got:
+            assert all(torch.equal(a, b) for a, b in zip(have, want)), order
+    assert own.status_sync() == 0
+    own.close()
+
+
+@pytest.mark.parametrize("typ", TYPES)
+@pytest.mark.parametrize("C", [192, 250, 1028])
+def test_layer_norm_of_constant_rows_whose_sum_rounds(ctx, typ, C):
+    x = (torch.tensor([0.1, -0.7, 1 / 3, 5.1, 1e-3])[:, None] * torch.ones(C)).to(typ)
+    one = torch.ones(C, dtype=torch.float64)
+    y = ctx.layer_norm(x.cuda(), None, None, eps=1e-3)
+    ref.check(y, ref.layer_norm(x.double(), None, one, 0 * one, 1e-3, eps=EPS[typ]), "y")
+    dx, dg, db = ctx.layer_norm_backward(x.cuda(), x.cuda(), None, eps=1e-3)
+    want = ref.layer_norm(x.double(), None, one, 0 * one, 1e-3, x.double(), eps=EPS[typ])
+    for name, got in (("dx", dx), ("dg", dg), ("db", db)):
+        ref.check(got, want[name], name)
