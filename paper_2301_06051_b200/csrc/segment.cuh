@@ -52,13 +52,6 @@ __device__ __forceinline__ int voxel_at(const SegArgs& a, int row) {
   return -1;
 }
 
-__device__ __forceinline__ int bucket_of(const BucketMaps& m, int dx, int dy, int dz) {
-  dx = min(max(dx, 1 - m.extent[0]), m.extent[0] - 1) + m.extent[0] - 1;
-  dy = min(max(dy, 1 - m.extent[1]), m.extent[1] - 1) + m.extent[1] - 1 + m.at_y;
-  dz = min(max(dz, 1 - m.extent[2]), m.extent[2] - 1) + m.extent[2] - 1 + m.at_z;
-  return m.of[dx] + m.of[dy] + m.of[dz];
-}
-
 template <typename T>
 int launch_forward(dsvt_ctx* ctx, const SegArgs& a);
 template <typename T>

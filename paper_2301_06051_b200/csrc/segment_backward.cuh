@@ -836,7 +836,7 @@ int backward_of(dsvt_ctx* ctx, const SegArgs& a) {
   int batch = 96;
   BackLayout l = back_layout<T, DT>(a, limit, batch);
   while (l.bytes > kSmemHalf && batch > 48) l = back_layout<T, DT>(a, limit, batch -= 8);
-  while (l.bytes > kSmemMost) l = back_layout<T, DT>(a, limit = limit > 64 ? 64 : limit / 2, batch);
+  if (l.bytes > kSmemMost) l = back_layout<T, DT>(a, limit = 64, batch);  // (some heads of fp32 and large biases, from 81 rows on; 64 always fit)
   const Scoring sc = scoring_of(a);
   const int groups = (int)dsvt_ceil_div(a.heads, kBackHeads<T, DT>);
   BackWork w = {};

@@ -415,7 +415,7 @@ __device__ __forceinline__ void soften(Flow<DT>& f, float (&s)[NT][4]) {
 
 // ---- long segments ---------------------------------------------------------------------------------------------------
 struct Tile { int lo, hi, row; };  // a segment and the first row of a tile of it
-constexpr int kMaxTiles = 8;       // tiles that start in one block's rows (at most 128, of segments of more than 24 rows)
+constexpr int kMaxTiles = 8;       // tiles that start in one block's rows: at most three, of segments of more than 64 rows that do not overlap
 
 // The tiles of `tile` rows of segments longer than `above` that start in rows [base, base + tile).  Where an index was bad, in this call's
 // starts perhaps (the short ones' kernel has been through them all), every segment is looked at: the blocks of a segment's tiles, and in the

@@ -177,7 +177,7 @@ __global__ void __launch_bounds__(kShortThreads, DT <= 24 && sizeof(T) == 2 ? 3 
 struct LongLayout {
   int pitch_idx;
   uint32_t pitch, tile, chunk;  // bytes of a row, of an array of the tile's rows, of an array of a chunk's rows
-  uint32_t maps, bias, cells, passing_cells, ids, index, rows, passing, more, bytes;
+  uint32_t maps, bias, cells, passing_cells, ids, index, rows, passing, bytes;
 };
 
 template <typename T, int DT>
@@ -188,7 +188,7 @@ struct LongShape {
 };
 
 template <typename T, int DT>
-static LongLayout long_layout(const SegArgs& a, int own, int passing, size_t more) {
+static LongLayout long_layout(const SegArgs& a, int own, int passing) {
   using S = LongShape<T, DT>;
   LongLayout l = {};
   l.pitch = (uint32_t)(S::HG * a.dim * sizeof(T) + 16);
@@ -205,7 +205,6 @@ static LongLayout long_layout(const SegArgs& a, int own, int passing, size_t mor
     l.pitch_idx = S::chunk + 8;
     l.index = take((size_t)2 * S::rows * l.pitch_idx * 2);
   }
-  l.more = take(more);
   l.rows = take((size_t)own * l.tile + 64);
   l.passing = take((size_t)2 * passing * l.chunk + 64);
   l.bytes = at;
@@ -359,7 +358,7 @@ int forward_of(dsvt_ctx* ctx, const SegArgs& a) {
   DSVT_LAUNCHED(ctx);
   if (limit >= a.max_len) return DSVT_OK;
   using S = LongShape<T, DT>;
-  const LongLayout g = long_layout<T, DT>(a, 1, 2, 0);
+  const LongLayout g = long_layout<T, DT>(a, 1, 2);
   constexpr auto longer = long_forward_kernel<T, DT>;
   rc = allow_smem<longer>(ctx, kSmemMost);
   if (rc != DSVT_OK) return rc;

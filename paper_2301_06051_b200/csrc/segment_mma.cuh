@@ -354,20 +354,4 @@ __device__ __forceinline__ void cap_slope(float (&x)[NT][4], const float (&z)[NT
     }
 }
 
-// ---- loading -------------------------------------------------------------------------------------------------------
-// Smallest s with key <= at[s], or count; a warp together.  (Entries that do not ascend give some s in [0, count].)
-__device__ __forceinline__ int first_not_below(const int32_t* at, int count, int key) {
-  const int lane = threadIdx.x & 31;
-  int lo = 0, hi = count;
-  while (hi - lo > 32) {
-    const int step = (hi - lo + 31) >> 5, i = lo + lane * step;
-    const int below = __popc(__ballot_sync(kAll, i < hi && at[i] < key));
-    if (below == 0) return lo;
-    const int end = lo + below * step;
-    lo += (below - 1) * step + 1;
-    hi = end < hi ? end : hi;
-  }
-  return lo + __popc(__ballot_sync(kAll, lo + lane < hi && at[lo + lane] < key));
-}
-
 }  // namespace dsvt_train
