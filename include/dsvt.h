@@ -461,8 +461,8 @@ int dsvt_segment_attention(dsvt_ctx* ctx, const dsvt_segment_attention_params* p
  * The call works in the context's workspace, as partitions and layers do: calls of one context, captured ones among them, must not
  * overlap on the GPU.
  *
- * Needs heads * buckets <= 2^18 with dbias (else DSVT_ERR_UNSUPPORTED), and n <= 1,700,000 where max_len is above 24 (else
- * DSVT_ERR_CAPACITY).
+ * Needs heads * buckets <= 2^18 with dbias (else DSVT_ERR_UNSUPPORTED), and n <= 1,700,000 where max_len is above 120 (in some
+ * calls above 80: fp32 rows of head_dim > 80, 16-bit rows of 8 x 16 channels with more than 400 buckets; else DSVT_ERR_CAPACITY).
  */
 int dsvt_segment_attention_backward(dsvt_ctx* ctx, const dsvt_segment_attention_params* params, const void* d_out,
                                     int64_t ld_dout, void* dq, int64_t ld_dq, void* dk, int64_t ld_dk, void* dv, int64_t ld_dv,

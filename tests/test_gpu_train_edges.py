@@ -173,6 +173,28 @@ def test_no_voxels_with_a_bias(ctx, max_len):
     assert ctx.status_sync() == 0
 
 
+# ---- more voxels than statistics ------------------------------------------------------------------------------------------
+def test_segments_that_are_held_whole_take_any_number_of_voxels():
+    """1,800,000 voxels: the backward pass keeps statistics in the workspace for longer segments alone."""
+    n, each = 1800000, 60
+    own = api.Context(n, 1, 256)
+    p = Problem([each] * (n // each), 1, 8, torch.bfloat16, seed=5, packed=False, max_len=80)
+    p.segments = p.segments[:3] + p.segments[n // each // 2:][:3] + p.segments[-3:]
+    for p.seg.max_len in (80, 120):
+        out, (dq, dk, dv, _) = p.forward(own), p.backward(own)
+        want = {**p.want()[0], **p.want(back=True)[0]}
+        rows = torch.from_numpy(np.concatenate(p.segments))
+        for name, got in (("out", out), ("dq", dq), ("dk", dk), ("dv", dv)):
+            ref.check(got.cpu()[rows], tuple(t[rows] for t in want[name]), name)
+    p.seg.max_len = 121
+    p.forward(own)
+    with pytest.raises(api.DsvtError) as e:
+        p.backward(own)
+    assert e.value.code == -2
+    assert own.status_sync() == 0
+    own.close()
+
+
 # ---- the ends of float's range -----------------------------------------------------------------------------------------
 def _two_clusters(rest, near, dp, do):
     """Voxels 0 and 1 attend to each other alone (`near`: the bias between them), the `rest` others among themselves; the rows' products
