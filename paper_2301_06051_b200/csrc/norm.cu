@@ -3,8 +3,8 @@
 //   u = x + r,  y = (u - mean(u)) rstd(u) g + b,  h = (u - mean(u)) rstd(u),  w = dy g
 //   dx = rstd (w - mean(w) - h mean(w h)),  dg = sum over rows of dy h,  db = sum over rows of dy
 //
-// Bound by memory: x, r (and dy) are read once and y (dx) written once.  200,000 x 192 bfloat16: 39.6 us (5.8 TB/s, 89 % of a copy's rate),
-// backward 57 us (5.4 TB/s).  A row lies in the registers of a group of lanes, so the
+// Bound by memory: x, r (and dy) are read once and y (dx) written once.  200,000 x 192 bfloat16: 39.7 us in a graph of calls (5.8 TB/s, 89 %
+// of a copy's rate; 86 % by single calls), backward 59 us (5.2 TB/s).  A row lies in the registers of a group of lanes, so the
 // backward pass takes mean and rstd from the row again, which costs no memory, where reading saved ones would.  Statistics,
 // sums and gradients of the weights are fp32; the mean is subtracted before the squares are summed.
 // The weights' gradients: a lane adds up its columns over all rows of its group, the groups of a block meet in shared memory,
@@ -125,7 +125,7 @@ __global__ void __launch_bounds__(kThreads<BLOCK>) norm_kernel(const NormArgs<T>
   const int lanes = BLOCK ? kThreads<BLOCK> : a.lanes, groups = kThreads<BLOCK> / lanes;
   const int group = threadIdx.x / lanes, lane = threadIdx.x % lanes;
   const int nc = a.C / V;
-  const float C = (float)a.C;  // (divided by: the mean of a constant row is the constant)
+  const float C = (float)a.C;  // (divided by, which rounds once; a constant row's mean is off by what its sum is, and eps takes that up)
   int at[VPL];
   bool in[VPL];
   Num g[VPL][N], b[BACK ? 1 : VPL][N], dg[BACK ? VPL : 1][N], db[BACK ? VPL : 1][N];

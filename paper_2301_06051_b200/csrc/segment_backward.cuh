@@ -3,9 +3,10 @@
 //   by queries: maximum, sum and D of a row, then dq = scale dz k
 //   by keys:    p and dz again from those three, dk = scale dz^T q, dv = p^T do, and the bias's gradient
 //
-// Short segments do both in one block, long ones in two kernels.  Measured (bf16, dim 24, 8 heads): 32,000 pillars in sets of 36 96 us,
-// where the bytes that it cannot do without take 13; 60,000 voxels in whole windows of up to 850, 1195 us (bytes 25).  Bound by
-// instructions and their latencies: warps issue in 41 to 52 % of the cycles, the tensor pipe is busy for 5 to 10 %, DRAM for 1 to 7 %.
+// Short segments do both in one block, long ones in two kernels.  Measured (bf16, dim 24, 8 heads): 32,000 pillars in sets of 36 95 us,
+// where the bytes that it cannot do without take 13; 60,000 voxels in whole windows of up to 850, 1196 us (bytes 25).  Bound by
+// instructions and their latencies (long segments: 111 a score by queries, 97 by keys): warps issue in 41 to 52 % of the cycles, the tensor
+// pipe is busy for 5 to 10 %, DRAM for 1 to 7 %.
 // D = sum_j p dp is formed from the scores and not from the output: the output's rounding to 16 bits would reach the bias's gradient,
 // which is fp32.
 //
@@ -520,8 +521,9 @@ __global__ void __launch_bounds__(kThreads, DT <= 32 ? 2 : 1) short_backward_ker
           clear<DT>(dv);
           x.k = k0 + row * pitch + at_head; x.v = v0 + row * pitch + at_head;
           const uint32_t tile_rows = (uint32_t)real_rows(plan, row, min(16, item.len - 16 * item.tile));
-          // (Two tiles at a time and not four: half the code, and no spilled registers.  Kernels of this size miss in the instruction cache:
-          // 32,000 pillars bf16 148 us with four, 127 with two; fp32, 12,345 with a cap, 352 and 255.)
+          // (Two tiles at a time and not four: half the code and fewer registers.  Kernels of this size miss in the instruction cache: 32,000
+          // pillars bf16 148 us with four, 127 with two; fp32, 12,345 with a cap, 352 and 255.  With two, 16-bit types spill
+          // no registers; fp32 stores 64, 300 and 932 bytes of them at 16, 24 and 32 channels a head.)
           for (int j = 0; j < item.len; j += 16) {
             const int cols = min(16, item.len - j);
             const uint64_t queries = real_rows(plan, item.at + j, cols);

@@ -1,9 +1,9 @@
 // Segment attention, forward: softmax(q k^T + bias) v inside each segment.
 //
-// Measured (bf16, dim 24, 8 heads, bias of 121 and 567 buckets): 32,000 pillars in sets of 36 36 us, where q, k, v and the result take 8 at
-// a copy's rate; 120,000 voxels in whole windows of up to 1055 472 us (bytes 29, operations 14).  Bound by instructions and their
-// latencies, not by the tensor pipe (5 and 12 % busy) or DRAM (12 and 4 %): a score takes a look-up, an exponential and a dozen others
-// beside 2 x 24 multiply-adds.  In sets, a third of the warps' time goes to the barriers between planning, loading, looking up and
+// Measured (bf16, dim 24, 8 heads, bias of 121 and 567 buckets): 32,000 pillars in sets of 36 37 us, where q, k, v and the result take 8 at
+// a copy's rate; 120,000 voxels in whole windows of up to 1055 475 us (bytes 29, operations 14).  Bound by instructions and their
+// latencies, not by the tensor pipe (5 and 12 % busy) or DRAM (12 and 4 %): in the windows' tiles some 45 instructions a score (issue slots
+// times 32 lanes, by pairs and heads), of which its 2 x 24 multiply-adds are few; each group of four heads looks a pair's bucket up.  In sets, a third of the warps' time goes to the barriers between planning, loading, looking up and
 // attending; warps of their own for the first three, over a ring of batches, came to the same time (30 us where this took 32), and four
 // blocks of 128 threads or two of 256 with two heads to a warp to more.
 #pragma once
